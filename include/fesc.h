@@ -495,6 +495,84 @@ int fesc_scan_contract(fesc_ctx* ctx, const uint64_t* d_x, const uint64_t* d_a, 
                        const uint64_t* d_C, const fesc_scan_desc* desc, const fesc_scan_consts* consts,
                        uint64_t* d_m_out, void* stream);
 
+/*
+ * Operators on CLEARTEXT activations, beside the encrypted ones: the gated linear recurrence that fesc_scan_contract evaluates on ciphertexts
+ * and the norm around which fesc_norm_square / fesc_norm_scale are built, with the backward passes that training the served model needs and
+ * the single token that serving it in the clear needs.  They take no context: sizes, strides and workspace come with the call, nothing is kept
+ * between calls, and calls on different streams or in different threads do not meet (each needs a workspace of its own).
+ *   - Activations are bfloat16, float16 or float32 (desc->type); log decays, states, weights of norms and their gradients float32.  All sums
+ *     are held in float32 or more.  Results do not depend on the order in which anything runs.
+ *   - Strides are in elements and not negative; the innermost dimension is contiguous.  Any alignment of the type is taken; 16 bytes (addresses
+ *     and strides) are faster.  Outputs may not overlap inputs or one another, except where said.
+ *   - Device pointers belong to the device that is current.  Calls enqueue work on `stream`, allocate nothing and can be captured into a graph.
+ *   - Return value: FESC_OK, FESC_EINVAL or FESC_ECUDA; fesc_clear_last_error() gives the text of the calling thread's last refusal.
+ */
+enum { FESC_BF16 = 0, FESC_F16 = 1, FESC_F32 = 2 };
+const char* fesc_clear_last_error(void);
+
+/*
+ * Gated linear recurrence (Sec. 5.4, Eqs. fesc_recurrence / fesc_contract; g = log a), per sequence and head, h in R^{P x N}:
+ *   h_t = exp(g_t) h_{t-1} + x_t B_t^T,    y_t = h_t C_t + D x_t.
+ *   d_x, d_y [batch][L][H][P]   d_g [batch][L][H]   d_B, d_C [batch][L][G][N], G dividing H: heads h*G/H share a group's rows
+ *   d_skip   [H], D, or NULL (0)
+ *   d_h0     [batch][H][P][N], the states before the first token, or NULL (0)
+ *   d_lengths int32 [batch] (DEVICE), tokens of every sequence, taken into [0, L], or NULL (L): tokens behind are neither read nor written
+ *   d_h_out  [batch][H][P][N], the states behind the last token (length 0: before the first), or NULL; not d_h0
+ * A log decay of -inf (any below -300) drops the state.  N <= 128, P <= 4096, L < 2^30, batch <= 65535.
+ * Tokens of a chunk of 64 are multiplied with zeros among themselves: an infinity or NaN in a token reaches the other tokens of its chunk, and
+ * everything after it.
+ * Workspace: fesc_clear_scan_work(desc) bytes, 16-byte aligned (0: none needed).
+ */
+typedef struct fesc_clear_scan_desc {
+    uint32_t batch, L, H, P, G, N;
+    uint32_t type;                             /* FESC_BF16, FESC_F16 or FESC_F32: x, B, C, y and their gradients */
+    uint32_t reserved;
+    int64_t x[3], y[3], g[3], B[3], C[3];      /* strides of batch, token and head (B, C: group); y: of dy in the backward pass */
+    int64_t dx[3], dg[3], dB[3], dC[3];        /* backward pass only */
+} fesc_clear_scan_desc;
+size_t fesc_clear_scan_work(const fesc_clear_scan_desc* desc);
+int fesc_clear_scan(const fesc_clear_scan_desc* desc, const void* d_x, const float* d_g, const void* d_B, const void* d_C, const float* d_skip,
+                    const float* d_h0, const int32_t* d_lengths, void* d_y, float* d_h_out, void* d_work, size_t work_bytes, void* stream);
+/*
+ * Its gradients, from dy [batch][L][H][P] and the gradient of h_out (d_dh_out, or NULL: 0).  The inputs are those of the forward call; nothing of it is
+ * kept.  d_dx, d_dg, d_dB, d_dC like x, g, B, C (dB, dC summed over the heads of a group; rows behind a sequence's end left as they are);
+ * d_dskip [H] or NULL, summed over all sequences; d_dh0 [batch][H][P][N] or NULL.  Workspace: fesc_clear_scan_backward_work(desc) bytes.
+ */
+size_t fesc_clear_scan_backward_work(const fesc_clear_scan_desc* desc);
+int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const void* d_x, const float* d_g, const void* d_B, const void* d_C, const float* d_skip,
+                             const float* d_h0, const int32_t* d_lengths, const void* d_dy, const float* d_dh_out, void* d_dx, float* d_dg, void* d_dB,
+                             void* d_dC, float* d_dskip, float* d_dh0, void* d_work, size_t work_bytes, void* stream);
+/*
+ * One token of every sequence (desc->L is not read, nor are token strides): d_state [batch][H][P][N] -> d_state_out, which may be d_state itself.
+ */
+int fesc_clear_scan_step(const fesc_clear_scan_desc* desc, const void* d_x, const float* d_g, const void* d_B, const void* d_C, const float* d_skip,
+                         const float* d_state, float* d_state_out, void* d_y, void* stream);
+
+/*
+ * RMS norm with the gate before it and the residual around it (Alg. "one Block": gate, norm, out projection, residual, next norm):
+ *   v = y * silu(z),   h = r + s * v,   n = gamma * h / sqrt(mean_group(h^2) + eps).
+ * d_y [rows][d]; d_gate z [rows][d] or NULL (v = y); d_residual r [rows][d] or NULL (h = v); d_scale s [d] or NULL (1; only with a residual);
+ * d_gamma [d]; outputs d_n [rows][d] and d_h [rows][d] or NULL.  `groups` divides d into groups of neighbours with a mean each, of at most 8192
+ * channels.  n is formed from h before h is rounded.  eps > 0.
+ */
+typedef struct fesc_clear_norm_desc {
+    uint64_t rows;
+    uint32_t d, groups, type;
+    float eps;
+    int64_t y_stride, gate_stride, residual_stride, n_stride, h_stride;                       /* between rows */
+    int64_t dn_stride, dh_stride, dy_stride, dgate_stride, dresidual_stride;                  /* backward pass only */
+} fesc_clear_norm_desc;
+int fesc_clear_norm(const fesc_clear_norm_desc* desc, const void* d_y, const float* d_gamma, const void* d_gate, const void* d_residual,
+                    const float* d_scale, void* d_n, void* d_h, void* stream);
+/*
+ * Its gradients, from dn and the gradient dh of h (NULL: 0): d_dy; d_dgamma [d]; d_dgate, d_dresidual and d_dscale [d] exactly where gate, residual and
+ * scale are given.  The inputs are those of the forward call.  Workspace: fesc_clear_norm_backward_work(desc) bytes, 16-byte aligned.
+ */
+size_t fesc_clear_norm_backward_work(const fesc_clear_norm_desc* desc);
+int fesc_clear_norm_backward(const fesc_clear_norm_desc* desc, const void* d_y, const float* d_gamma, const void* d_gate, const void* d_residual,
+                             const float* d_scale, const void* d_dn, const void* d_dh, void* d_dy, float* d_dgamma, void* d_dgate,
+                             void* d_dresidual, float* d_dscale, void* d_work, size_t work_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

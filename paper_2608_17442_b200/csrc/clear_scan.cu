@@ -1,0 +1,424 @@
+// Cleartext gated linear recurrence, the operator that fesc_scan_contract evaluates on ciphertexts (Sec. 5.4, Eqs. fesc_recurrence /
+// fesc_contract):  h_t = exp(g_t) h_{t-1} + x_t B_t^T,  y_t = h_t C_t + D x_t; its backward pass, and one token of it.
+// clear_scan.cuh holds the sweep; here are the kernels around it and the entry points.
+//
+// The gradient of the log decays comes from what the sweeps give: with row_t = C_t . dC_t and col_t = B_t . dB_t of one head,
+//   dg_t = <h_t, dh_t>' summed back from the segment's end:  R_t = R_{t+1} + row_t - col_t,  R behind a segment = <h, dh> there,
+// so no state has to be kept per token.  Rounding adds up over a segment only, whose end is computed from the states themselves.
+#define FESC_DBG_FILE 20   // file id in the sites a debug build reports
+#include "clear_scan.cuh"
+
+static thread_local std::string clear_error;
+int clear_fail(int code, const char* what) {
+    try {
+        clear_error = what;
+    } catch (...) {      // no memory for the text: the code stands
+    }
+    return code;
+}
+extern "C" const char* fesc_clear_last_error(void) { return clear_error.c_str(); }
+
+// Chains the segments: slot s gets the state before segment s (in the sweep's direction) and what the segment adds goes into the chain.
+__global__ void __launch_bounds__(256) k_clear_combine(float* states, const float* decay, const float* init, uint32_t segments, uint32_t per_head,
+                                                       size_t per_b, uint32_t backwards) {
+    pdl_begin();
+    const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    const uint32_t b = blockIdx.y;
+    if (i >= per_b) return;
+    float* s = states + (size_t)b * segments * per_b + i;
+    const uint32_t H = (uint32_t)(per_b / per_head), n = (uint32_t)(per_b - i < 4 ? per_b - i : 4);
+    if (!DBG_REGION(decay + (size_t)b * segments * H, (size_t)segments * H * sizeof(float)) ||
+        !DBG_REGION(s, ((segments - 1) * per_b + n) * sizeof(float)) || (init && !DBG_REGION(init + b * per_b + i, n * sizeof(float))))
+        return;
+    const bool wide = per_b % 4 == 0 && per_head % 4 == 0 && ((size_t)init & 15) == 0;
+    float run[4] = {};
+    for (uint32_t e = 0; e < n && init; e++) run[e] = init[b * per_b + i + e];
+    for (uint32_t c = 0; c < segments; c++) {
+        const uint32_t at = backwards ? segments - 1 - c : c;
+        float* p = s + (size_t)at * per_b;
+        const float* d = decay + ((size_t)b * segments + at) * H;
+        if (wide) {
+            const float4 add = *reinterpret_cast<const float4*>(p);
+            *reinterpret_cast<float4*>(p) = make_float4(run[0], run[1], run[2], run[3]);
+            const float f = d[i / per_head];
+            run[0] = f * run[0] + add.x, run[1] = f * run[1] + add.y, run[2] = f * run[2] + add.z, run[3] = f * run[3] + add.w;
+        } else {
+            for (uint32_t e = 0; e < n; e++) {
+                const float add = p[e];
+                p[e] = run[e];
+                run[e] = d[(i + e) / per_head] * run[e] + add;
+            }
+        }
+    }
+}
+
+struct FinishArgs {
+    const float *part_b, *part_c, *row, *col, *ends, *diag, *g;
+    void *dB, *dC;
+    float *dg, *dskip;
+    const int* lengths;
+    long long Bb, Bt, Bg, Cb, Ct, Cg, gb, gt, gh, ib, it, ih;
+    uint32_t b, L, H, G, N, NP, tiles, segments, seg_chunks, sum_blocks, dg_blocks;
+};
+// What is left of the backward pass, by block: sums of dB and dC over the heads of a group; the gradient of the log decays; that of the skip.
+template <class T>
+__global__ void __launch_bounds__(256) k_clear_scan_finish(const FinishArgs a) {
+    pdl_begin();
+    const uint32_t vheads = a.H * a.tiles, tid = threadIdx.x;
+    if (blockIdx.x < a.sum_blocks) {
+        const uint32_t quads = a.NP / 4;
+        const size_t i = (size_t)blockIdx.x * 256 + tid, all = (size_t)a.b * a.L * a.G * quads;
+        if (i >= all) return;
+        const uint32_t n = (uint32_t)(i % quads) * 4, grp = (uint32_t)(i / quads % a.G), t = (uint32_t)(i / quads / a.G % a.L), b = (uint32_t)(i / quads / a.G / a.L);
+        const int length = a.lengths ? min(max(a.lengths[b], 0), (int)a.L) : (int)a.L;
+        if ((int)t >= length || n >= a.N) return;
+        const uint32_t per = vheads / a.G;
+        const size_t step = (size_t)a.L * a.NP;
+        const float* src = (blockIdx.y ? a.part_c : a.part_b) + (((size_t)b * vheads + grp * per) * a.L + t) * a.NP + n;
+        T* dst = blockIdx.y ? (T*)a.dC + b * a.Cb + t * a.Ct + grp * a.Cg + n : (T*)a.dB + b * a.Bb + t * a.Bt + grp * a.Bg + n;
+        if (!DBG_REGION(src, ((per - 1) * step + 4) * sizeof(float)) || !DBG_REGION(dst, min(4u, a.N - n) * sizeof(T))) return;
+        float s[4] = {};
+#pragma unroll 4
+        for (uint32_t h = 0; h < per; h++) {
+            const float4 v = *reinterpret_cast<const float4*>(src + h * step);
+            s[0] += v.x, s[1] += v.y, s[2] += v.z, s[3] += v.w;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            if (n + e < a.N) dst[e] = ClearType<T>::from(s[e]);
+        return;
+    }
+    if (blockIdx.y) return;
+    const uint32_t lane = tid & 31, blk = blockIdx.x - a.sum_blocks;
+    if (blk < a.dg_blocks) {                       // a warp per sequence, head and segment
+        const size_t w = (size_t)blk * 8 + (tid >> 5);
+        if (w >= (size_t)a.b * a.H * a.segments) return;
+        const uint32_t head = (uint32_t)(w % a.H), seg = (uint32_t)(w / a.H % a.segments), b = (uint32_t)(w / a.H / a.segments);
+        const int length = a.lengths ? min(max(a.lengths[b], 0), (int)a.L) : (int)a.L;
+        const int lo = (int)(seg * a.seg_chunks) * SCAN_Q, hi = min(length, lo + (int)a.seg_chunks * SCAN_Q);
+        if (lo >= hi) return;
+        const float* row = a.row + ((size_t)b * vheads + head * a.tiles) * a.L;
+        const float* col = a.col + ((size_t)b * vheads + head * a.tiles) * a.L;
+        float* dg = a.dg + b * a.gb + head * a.gh;
+        const float* g = a.g + b * a.ib + head * a.ih;
+        if (!DBG_REGION(dg + lo * a.gt, ((long long)(hi - 1 - lo) * a.gt + 1) * sizeof(float))) return;
+        double run = 0.0;
+        for (uint32_t s = 0; s < a.tiles; s++) run += a.ends[((size_t)b * a.segments + seg) * vheads + head * a.tiles + s];
+        for (int top = hi - 1; top >= lo; top -= 32) {
+            const int t = top - (int)lane;
+            double v = 0.0;
+            if (t >= lo)
+                for (uint32_t s = 0; s < a.tiles; s++) v += (double)row[(size_t)s * a.L + t] - (double)col[(size_t)s * a.L + t];
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const double u = __shfl_up_sync(~0u, v, o);
+                if ((int)lane >= o) v += u;
+            }
+            // a dropped state has the gradient zero, from which the sum goes on
+            const uint32_t drops = __ballot_sync(~0u, t >= lo && g[t * a.it] < SCAN_DROP) & (~0u >> (31 - lane));
+            const double from = __shfl_sync(~0u, v, drops ? 31 - __clz(drops) : 0);
+            v = drops ? v - from : run + v;
+            if (t >= lo) dg[t * a.gt] = (float)v;
+            run = __shfl_sync(~0u, v, 31);
+        }
+        return;
+    }
+    // the skip: a warp per head
+    const uint32_t head = (blk - a.dg_blocks) * 8 + (tid >> 5);
+    if (!a.dskip || head >= a.H) return;
+    double s = 0.0;
+    const size_t all = (size_t)a.b * a.segments * a.tiles;
+    for (size_t i = lane; i < all; i += 32) s += a.diag[i / a.tiles * vheads + head * a.tiles + i % a.tiles];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
+    if (lane == 0 && DBG_REGION(a.dskip + head, sizeof(float))) a.dskip[head] = (float)s;
+}
+
+// One token.  A warp takes rows of the state, a lane up to four of its columns; read and written once, bound by that.
+struct StepArgs {
+    const void *x, *B, *C;
+    const float *g, *skip, *state;
+    float* out;
+    void* y;
+    long long xb, xh, Bb, Bg, Cb, Cg, gb, gh, yb, yh;
+    uint32_t H, P, N, G, rows;     // rows of the state per warp
+    uint32_t wide;
+};
+template <class T, bool WIDE>
+__global__ void __launch_bounds__(256) k_clear_scan_step(const StepArgs a) {
+    pdl_begin();
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, head = blockIdx.x % a.H, b = blockIdx.x / a.H, group = head / (a.H / a.G);
+    const T* B = (const T*)a.B + b * a.Bb + group * a.Bg;
+    const T* C = (const T*)a.C + b * a.Cb + group * a.Cg;
+    const T* x = (const T*)a.x + b * a.xb + head * a.xh;
+    T* y = (T*)a.y + b * a.yb + head * a.yh;
+    const size_t at = ((size_t)b * a.H + head) * a.P * a.N;
+    if (!DBG_REGION(B, a.N * sizeof(T)) || !DBG_REGION(C, a.N * sizeof(T)) || !DBG_REGION(x, a.P * sizeof(T)) || !DBG_REGION(y, a.P * sizeof(T)) ||
+        !DBG_REGION(a.state + at, (size_t)a.P * a.N * 4) || !DBG_REGION(a.out + at, (size_t)a.P * a.N * 4) || !DBG_REGION(a.g + b * a.gb + head * a.gh, 4))
+        return;
+    const float keep = expf(a.g[b * a.gb + head * a.gh]), skip = a.skip ? a.skip[head] : 0.f;
+    float vB[4], vC[4];
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        const uint32_t n = WIDE ? lane * 4 + e : lane + 32 * e;
+        vB[e] = n < a.N ? ClearType<T>::to(B[n]) : 0.f, vC[e] = n < a.N ? ClearType<T>::to(C[n]) : 0.f;
+    }
+    const uint32_t first = (blockIdx.y * 8 + warp) * a.rows, end = min(first + a.rows, a.P);
+#pragma unroll 4
+    for (uint32_t p = first; p < end; p++) {
+        const float xv = ClearType<T>::to(x[p]);
+        const float* s = a.state + at + (size_t)p * a.N;
+        float* o = a.out + at + (size_t)p * a.N;
+        float h[4] = {}, sum = 0.f;
+        if (WIDE) {
+            if (lane * 4 < a.N) {
+                const float4 v = *reinterpret_cast<const float4*>(s + lane * 4);
+                h[0] = v.x, h[1] = v.y, h[2] = v.z, h[3] = v.w;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (lane + 32 * e < a.N) h[e] = s[lane + 32 * e];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            // a decay of zero drops what the state holds, also infinities
+            h[e] = (keep > 0.f || keep != keep ? keep * h[e] : 0.f) + xv * vB[e];
+            if ((WIDE ? lane * 4 : lane + 32 * e) < a.N) sum += h[e] * vC[e];
+        }
+        if (WIDE) {
+            if (lane * 4 < a.N) *reinterpret_cast<float4*>(o + lane * 4) = make_float4(h[0], h[1], h[2], h[3]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (lane + 32 * e < a.N) o[lane + 32 * e] = h[e];
+        }
+#pragma unroll
+        for (int w = 16; w; w >>= 1) sum += __shfl_xor_sync(~0u, sum, w);
+        if (lane == 0) y[p] = ClearType<T>::from(sum + skip * xv);
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------------------
+struct ScanShape {
+    uint32_t tiles, vheads, segments, seg_chunks, np;
+    size_t states, state_floats, decay_floats, part_floats, dot_floats, end_floats;
+};
+
+// Segments: as many as fill the SMs with three CTAs each, none shorter than two chunks (a segment adds a pass over its keys and values, and a state
+// written and read).
+static ScanShape scan_shape(const fesc_clear_scan_desc* d) {
+    ScanShape s;
+    s.tiles = (d->P + SCAN_TILE - 1) / SCAN_TILE, s.vheads = d->H * s.tiles, s.np = d->N > 64 ? 128 : 64;
+    const uint64_t chunks = (d->L + SCAN_Q - 1) / SCAN_Q, ctas = (uint64_t)d->batch * s.vheads;
+    uint64_t want = ctas ? (3 * 148 + ctas - 1) / ctas : 1;
+    if (want > (chunks + 1) / 2) want = (chunks + 1) / 2;
+    if (want < 1) want = 1;
+    s.seg_chunks = chunks ? (uint32_t)((chunks + want - 1) / want) : 1;
+    s.segments = chunks ? (uint32_t)((chunks + s.seg_chunks - 1) / s.seg_chunks) : 1;
+    s.states = (size_t)d->H * d->P * d->N;
+    auto whole = [](size_t floats) { return (floats + 63) / 64 * 64; };      // parts of the workspace start on 256 bytes
+    s.state_floats = s.segments > 1 ? whole((size_t)d->batch * s.segments * s.states) : 0;
+    s.decay_floats = s.segments > 1 ? whole((size_t)d->batch * s.segments * d->H) : 0;
+    s.part_floats = whole((size_t)d->batch * s.vheads * d->L * s.np);
+    s.dot_floats = whole((size_t)d->batch * s.vheads * d->L);
+    s.end_floats = whole((size_t)d->batch * s.segments * s.vheads);
+    return s;
+}
+
+static const char* scan_check(const fesc_clear_scan_desc* d) {
+    if (d->type > FESC_F32) return "clear_scan: unknown type";
+    if (!d->H || !d->P || !d->N || !d->G || d->H % d->G) return "clear_scan: an empty dimension, or groups that do not divide the heads";
+    if (d->N > SCAN_MAX_STATE) return "clear_scan: states of more than 128 columns";
+    if (d->P > 4096 || d->L >= (1u << 30)) return "clear_scan: more than 4096 channels of a head or 2^30 tokens";
+    const ScanShape s = scan_shape(d);
+    if ((uint64_t)d->batch * s.segments * s.vheads >= (1ull << 31) || d->batch > 65535 || (uint64_t)d->batch * d->L * d->G * 32 >= (1ull << 38))
+        return "clear_scan: too many sequences, heads or tokens for one call";
+    return nullptr;
+}
+
+// Strides of a buffer with rows of `inner` elements: none is negative; elements of a written buffer are distinct.
+static bool scan_strides(const int64_t (&s)[3], uint64_t b, uint64_t t, uint64_t h, uint64_t inner, bool written) {
+    uint64_t count[3] = {b, t, h};
+    for (int i = 0; i < 3; i++)
+        if (s[i] < 0 || s[i] > (int64_t)1 << 40) return false;
+    if (!written) return true;
+    int order[3] = {0, 1, 2};
+    for (int i = 0; i < 3; i++)
+        for (int j = i + 1; j < 3; j++)
+            if (s[order[j]] < s[order[i]]) std::swap(order[i], order[j]);
+    uint64_t span = inner;
+    for (int i = 0; i < 3; i++) {
+        const int k = order[i];
+        if (count[k] <= 1) continue;
+        if ((uint64_t)s[k] < span) return false;
+        span += (uint64_t)s[k] * (count[k] - 1);
+    }
+    return true;
+}
+static ScanOperand operand(const void* p, const int64_t (&s)[3], bool tiled, uint32_t bytes) {
+    ScanOperand o = {p, s[0], s[1], s[2], tiled, 0};
+    o.wide = ((size_t)p & 15) == 0 && s[0] * bytes % 16 == 0 && s[1] * bytes % 16 == 0 && s[2] * bytes % 16 == 0;
+    return o;
+}
+static ScanArgs scan_args(const fesc_clear_scan_desc* d, const ScanShape& s, const float* g, const int* lengths) {
+    ScanArgs a = {};
+    a.g = g, a.gb = d->g[0], a.gt = d->g[1], a.gh = d->g[2], a.lengths = lengths;
+    a.b = d->batch, a.L = d->L, a.H = d->H, a.P = d->P, a.G = d->G, a.N = d->N;
+    a.tiles = s.tiles, a.segments = s.segments, a.seg_chunks = s.seg_chunks;
+    return a;
+}
+static cudaError_t scan_go(const fesc_clear_scan_desc* d, const ScanArgs& a, int mode, cudaStream_t st) {
+    return d->type == FESC_BF16 ? scan_launch<__nv_bfloat16>(a, mode, st)
+         : d->type == FESC_F16  ? scan_launch<__half>(a, mode, st)
+                                : scan_launch<float>(a, mode, st);
+}
+static cudaError_t combine(const fesc_clear_scan_desc* d, const ScanShape& s, float* states, const float* decay, const float* init, bool backwards, cudaStream_t st) {
+    return launch(k_clear_combine, dim3((uint32_t)((s.states + 1023) / 1024), d->batch), dim3(256), 0, st, states, decay, init, s.segments, d->P * d->N, s.states,
+                  (uint32_t)backwards);
+}
+
+extern "C" size_t fesc_clear_scan_work(const fesc_clear_scan_desc* desc) {
+    if (!desc || scan_check(desc)) return 0;
+    const ScanShape s = scan_shape(desc);
+    return (s.state_floats + s.decay_floats) * sizeof(float);
+}
+extern "C" size_t fesc_clear_scan_backward_work(const fesc_clear_scan_desc* desc) {
+    if (!desc || scan_check(desc)) return 0;
+    const ScanShape s = scan_shape(desc);
+    return (2 * (s.state_floats + s.decay_floats + s.part_floats + s.dot_floats + s.end_floats)) * sizeof(float);
+}
+
+extern "C" int fesc_clear_scan(const fesc_clear_scan_desc* desc, const void* d_x, const float* d_g, const void* d_B, const void* d_C, const float* d_skip,
+                               const float* d_h0, const int32_t* d_lengths, void* d_y, float* d_h_out, void* d_work, size_t work_bytes, void* stream) {
+    if (!desc) return clear_fail(FESC_EINVAL, "clear_scan: no descriptor");
+    if (const char* what = scan_check(desc)) return clear_fail(FESC_EINVAL, what);
+    const fesc_clear_scan_desc& d = *desc;
+    if (d.batch == 0) return FESC_OK;
+    if (!scan_strides(d.x, d.batch, d.L, d.H, d.P, false) || !scan_strides(d.g, d.batch, d.L, d.H, 1, false) || !scan_strides(d.B, d.batch, d.L, d.G, d.N, false) ||
+        !scan_strides(d.C, d.batch, d.L, d.G, d.N, false) || !scan_strides(d.y, d.batch, d.L, d.H, d.P, true))
+        return clear_fail(FESC_EINVAL, "clear_scan: a stride is negative or beyond 2^40, or elements of y overlap");
+    if (d.L && (!d_x || !d_g || !d_B || !d_C || !d_y)) return clear_fail(FESC_EINVAL, "clear_scan: x, g, B, C and y have to be given");
+    if (same_buffer(d_y, d_x) || same_buffer(d_y, d_B) || same_buffer(d_y, d_C) || same_buffer(d_h_out, d_h0))
+        return clear_fail(FESC_EINVAL, "clear_scan: an output is an input");
+    const ScanShape s = scan_shape(desc);
+    const size_t need = fesc_clear_scan_work(desc);
+    if (need && (!d_work || ((size_t)d_work & 15) || work_bytes < need))
+        return clear_fail(FESC_EINVAL, "clear_scan: the workspace is too small or not aligned to 16 bytes");
+    cudaStream_t st = (cudaStream_t)stream;
+    const uint32_t bytes = clear_type_bytes(d.type);
+    ScanArgs a = scan_args(desc, s, d_g, d_lengths);
+    a.q = operand(d_C, d.C, false, bytes), a.k = operand(d_B, d.B, false, bytes), a.v = operand(d_x, d.x, true, bytes);
+    a.init = d_h0;
+    if (s.segments > 1) {
+        float* states = (float*)d_work;
+        float* decay = states + s.state_floats;
+        a.last = states, a.decay = decay;
+        CLEAR_CUDA(scan_go(desc, a, MODE_STATE, st));
+        CLEAR_CUDA(combine(desc, s, states, decay, d_h0, false, st));
+        a.init = states;
+    }
+    a.last = d_h_out, a.skip = d_skip, a.out = d_y, a.ob = d.y[0], a.ot = d.y[1], a.oh = d.y[2];
+    a.out_wide = operand(d_y, d.y, true, bytes).wide;
+    CLEAR_CUDA(scan_go(desc, a, MODE_OUT, st));
+    return FESC_OK;
+}
+
+extern "C" int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const void* d_x, const float* d_g, const void* d_B, const void* d_C, const float* d_skip,
+                                        const float* d_h0, const int32_t* d_lengths, const void* d_dy, const float* d_dh_out, void* d_dx, float* d_dg, void* d_dB,
+                                        void* d_dC, float* d_dskip, float* d_dh0, void* d_work, size_t work_bytes, void* stream) {
+    if (!desc) return clear_fail(FESC_EINVAL, "clear_scan_backward: no descriptor");
+    if (const char* what = scan_check(desc)) return clear_fail(FESC_EINVAL, what);
+    const fesc_clear_scan_desc& d = *desc;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (d.batch == 0) {
+        if (d_dskip) CLEAR_CUDA(cudaMemsetAsync(d_dskip, 0, d.H * sizeof(float), st));
+        return FESC_OK;
+    }
+    if (!scan_strides(d.x, d.batch, d.L, d.H, d.P, false) || !scan_strides(d.g, d.batch, d.L, d.H, 1, false) || !scan_strides(d.B, d.batch, d.L, d.G, d.N, false) ||
+        !scan_strides(d.C, d.batch, d.L, d.G, d.N, false) || !scan_strides(d.y, d.batch, d.L, d.H, d.P, false) ||
+        !scan_strides(d.dx, d.batch, d.L, d.H, d.P, true) || !scan_strides(d.dg, d.batch, d.L, d.H, 1, true) || !scan_strides(d.dB, d.batch, d.L, d.G, d.N, true) ||
+        !scan_strides(d.dC, d.batch, d.L, d.G, d.N, true))
+        return clear_fail(FESC_EINVAL, "clear_scan_backward: a stride is negative or beyond 2^40, or elements of an output overlap");
+    if (d.L && (!d_x || !d_g || !d_B || !d_C || !d_dy || !d_dx || !d_dg || !d_dB || !d_dC))
+        return clear_fail(FESC_EINVAL, "clear_scan_backward: x, g, B, C, dy, dx, dg, dB and dC have to be given");
+    const void* outs[6] = {d_dx, d_dg, d_dB, d_dC, d_dskip, d_dh0};
+    const void* ins[8] = {d_x, d_g, d_B, d_C, d_skip, d_h0, d_dy, d_dh_out};
+    for (int i = 0; i < 6; i++) {
+        for (int j = 0; j < 8; j++)
+            if (same_buffer(outs[i], ins[j])) return clear_fail(FESC_EINVAL, "clear_scan_backward: an output is an input");
+        for (int j = 0; j < i; j++)
+            if (same_buffer(outs[i], outs[j])) return clear_fail(FESC_EINVAL, "clear_scan_backward: two outputs are the same");
+    }
+    const ScanShape s = scan_shape(desc);
+    const size_t need = fesc_clear_scan_backward_work(desc);
+    if (!d_work || ((size_t)d_work & 15) || work_bytes < need)
+        return clear_fail(FESC_EINVAL, "clear_scan_backward: the workspace is too small or not aligned to 16 bytes");
+    float* w = (float*)d_work;
+    auto take = [&](size_t floats) { float* p = w; w += floats; return p; };
+    float *before = take(s.state_floats), *behind = take(s.state_floats), *decay = take(s.decay_floats), *decay_back = take(s.decay_floats);
+    float *part_b = take(s.part_floats), *part_c = take(s.part_floats), *row = take(s.dot_floats), *col = take(s.dot_floats);
+    float *ends = take(s.end_floats), *diag = take(s.end_floats);
+    const uint32_t bytes = clear_type_bytes(d.type);
+    const ScanOperand x = operand(d_x, d.x, true, bytes), B = operand(d_B, d.B, false, bytes), C = operand(d_C, d.C, false, bytes),
+                      dy = operand(d_dy, d.y, true, bytes);
+    const ScanArgs base = scan_args(desc, s, d_g, d_lengths);
+    const float *h = d_h0, *dh = d_dh_out;
+    if (s.segments > 1) {
+        ScanArgs a = base;
+        a.k = B, a.v = x, a.last = before, a.decay = decay;
+        CLEAR_CUDA(scan_go(desc, a, MODE_STATE, st));
+        a.k = C, a.v = dy, a.last = behind, a.decay = decay_back, a.backwards = 1;
+        CLEAR_CUDA(scan_go(desc, a, MODE_STATE, st));
+        CLEAR_CUDA(combine(desc, s, before, decay, d_h0, false, st));
+        CLEAR_CUDA(combine(desc, s, behind, decay_back, d_dh_out, true, st));
+        h = before, dh = behind;
+    }
+    ScanArgs a = base;                  // dC
+    a.q = dy, a.k = x, a.v = B, a.u = C, a.init = h, a.meet = dh, a.part = part_c, a.dots = row, a.ends = ends, a.diag = diag;
+    CLEAR_CUDA(scan_go(desc, a, MODE_GRAD, st));
+    a = base;                           // dB
+    a.q = x, a.k = dy, a.v = C, a.u = B, a.init = dh, a.part = part_b, a.dots = col, a.backwards = 1;
+    CLEAR_CUDA(scan_go(desc, a, MODE_GRAD, st));
+    a = base;                           // dx, and the gradient of the state before the first token
+    a.q = B, a.k = C, a.v = dy, a.init = dh, a.last = d_dh0, a.skip = d_skip, a.out = d_dx, a.ob = d.dx[0], a.ot = d.dx[1], a.oh = d.dx[2];
+    a.out_wide = operand(d_dx, d.dx, true, bytes).wide, a.backwards = 1;
+    CLEAR_CUDA(scan_go(desc, a, MODE_OUT, st));
+    FinishArgs f = {};
+    f.part_b = part_b, f.part_c = part_c, f.row = row, f.col = col, f.ends = ends, f.diag = diag;
+    f.dB = d_dB, f.dC = d_dC, f.dg = d_dg, f.dskip = d_dskip, f.lengths = d_lengths, f.g = d_g, f.ib = d.g[0], f.it = d.g[1], f.ih = d.g[2];
+    f.Bb = d.dB[0], f.Bt = d.dB[1], f.Bg = d.dB[2], f.Cb = d.dC[0], f.Ct = d.dC[1], f.Cg = d.dC[2], f.gb = d.dg[0], f.gt = d.dg[1], f.gh = d.dg[2];
+    f.b = d.batch, f.L = d.L, f.H = d.H, f.G = d.G, f.N = d.N, f.NP = s.np, f.tiles = s.tiles, f.segments = s.segments, f.seg_chunks = s.seg_chunks;
+    f.sum_blocks = (uint32_t)(((size_t)d.batch * d.L * d.G * (s.np / 4) + 255) / 256);
+    f.dg_blocks = (uint32_t)(((size_t)d.batch * d.H * s.segments + 7) / 8);
+    const dim3 grid(f.sum_blocks + f.dg_blocks + (d.H + 7) / 8, 2);
+    auto kernel = d.type == FESC_BF16 ? k_clear_scan_finish<__nv_bfloat16> : d.type == FESC_F16 ? k_clear_scan_finish<__half> : k_clear_scan_finish<float>;
+    CLEAR_CUDA(launch(kernel, grid, dim3(256), 0, st, f));
+    return FESC_OK;
+}
+
+extern "C" int fesc_clear_scan_step(const fesc_clear_scan_desc* desc, const void* d_x, const float* d_g, const void* d_B, const void* d_C, const float* d_skip,
+                                    const float* d_state, float* d_state_out, void* d_y, void* stream) {
+    if (!desc) return clear_fail(FESC_EINVAL, "clear_scan_step: no descriptor");
+    if (const char* what = scan_check(desc)) return clear_fail(FESC_EINVAL, what);
+    const fesc_clear_scan_desc& d = *desc;
+    if (d.batch == 0) return FESC_OK;
+    if (!d_x || !d_g || !d_B || !d_C || !d_state || !d_state_out || !d_y) return clear_fail(FESC_EINVAL, "clear_scan_step: x, g, B, C, the states and y have to be given");
+    if (!scan_strides(d.x, d.batch, 1, d.H, d.P, false) || !scan_strides(d.g, d.batch, 1, d.H, 1, false) || !scan_strides(d.B, d.batch, 1, d.G, d.N, false) ||
+        !scan_strides(d.C, d.batch, 1, d.G, d.N, false) || !scan_strides(d.y, d.batch, 1, d.H, d.P, true))
+        return clear_fail(FESC_EINVAL, "clear_scan_step: a stride is negative or beyond 2^40, or elements of y overlap");
+    if (same_buffer(d_y, d_x) || same_buffer(d_y, d_B) || same_buffer(d_y, d_C)) return clear_fail(FESC_EINVAL, "clear_scan_step: y is an input");
+    if ((uint64_t)d.batch * d.H >= (1ull << 31)) return clear_fail(FESC_EINVAL, "clear_scan_step: too many sequences and heads for one call");
+    StepArgs a = {d_x, d_B, d_C, d_g, d_skip, d_state, d_state_out, d_y, d.x[0], d.x[2], d.B[0], d.B[2], d.C[0], d.C[2], d.g[0], d.g[2], d.y[0], d.y[2],
+                  d.H, d.P, d.N, d.G, 0, 0};
+    const bool wide = d.N % 4 == 0 && ((size_t)d_state & 15) == 0 && ((size_t)d_state_out & 15) == 0;
+    // eight rows per warp share B and C; where that leaves SMs without a CTA, one
+    a.rows = (uint64_t)d.batch * d.H * ((d.P + 63) / 64) >= 4 * 148 ? 8 : 1;
+    const dim3 grid(d.batch * d.H, (d.P + 8 * a.rows - 1) / (8 * a.rows));
+    auto pick = [&](auto t) { return wide ? k_clear_scan_step<decltype(t), true> : k_clear_scan_step<decltype(t), false>; };
+    auto kernel = d.type == FESC_BF16 ? pick(__nv_bfloat16()) : d.type == FESC_F16 ? pick(__half()) : pick(float());
+    CLEAR_CUDA(launch(kernel, grid, dim3(256), 0, (cudaStream_t)stream, a));
+    return FESC_OK;
+}

@@ -1,0 +1,497 @@
+// The sweep behind the cleartext gated linear recurrence: over the tokens of a sequence, forwards or backwards in time,
+//   out_i = sum_{j<=i} G_ij (q_i . k_j) v_j + G_i state q_i,   G_ij = exp(sum of the log decays after j up to i),
+//   state <- G_last state + sum_j G_last,j v_j k_j^T.
+// The scan is the sweep with (q, k, v) = (C, B, x); of its backward pass dx is the sweep backwards with (B, C, dy), dB the one with
+// (x, dy, C) and dC the sweep forwards with (dy, x, B).  Heads of more than 64 channels are cut into tiles of 64, which act as heads of their own.
+//
+// Tokens go in chunks of 64.  Within a chunk the sum is two matrix products with the decays between them (64 x 64 scores); the state carries
+// everything before it.  The state of a head tile (64 channels x up to 128) stays in registers, a quarter per warp, in the accumulator layout of
+// mma.m16n8k16, which is also the layout of a left operand: the products are formed transposed (out^T = state q^T + v^T S^T) so that the state
+// multiplies q without going through memory.
+// A long sequence is cut into segments when there are too few heads to fill the SMs: k_clear_scan in MODE_STATE gives what every
+// segment adds to its state, k_clear_combine chains the segments, and every segment then runs with the state before it.
+//
+// Operands are sums of bfloat16 numbers ("planes"): bfloat16 inputs one, float16 two (exact), float32 three (24 bits).  What the kernel
+// computes itself (decayed scores, weighted values, states) is cut into two planes (17 bits) where only outputs of 16 bits depend on it, and
+// into three (25 bits) where a float32 result does: states and the gradient of the log decays.  One plane, as 16-bit results alone would
+// stand, doubles their error (each of three roundings adds as much as the one at the end).  All sums are in float32.
+//
+// Log decays are summed in float64 per chunk and kept as two floats: with |g| up to 300 a token (below that a decay is zero: also -inf), one
+// float would leave 2^-10 of an exponent behind a strong decay.
+#pragma once
+#include "clear.cuh"
+
+#define SCAN_Q 64            // tokens of a chunk
+#define SCAN_TILE 64         // channels of a head tile
+#define SCAN_MAX_STATE 128   // columns of a state
+#define SCAN_DROP (-300.f)   // log decays below this drop the state
+#define SCAN_PAD 8           // bfloat16 numbers behind a row in shared memory: eight rows start in different banks
+enum { MODE_STATE = 0, MODE_OUT = 1, MODE_GRAD = 2 };
+
+struct ScanOperand {
+    const void* p;
+    long long sb, st, sh;    // strides of batch, token and head (or group), in elements
+    uint32_t tiled;          // 1: a head's channels (64 of P from the tile), 0: a group's columns (N)
+    uint32_t wide;           // 16-byte accesses are possible
+};
+struct ScanArgs {
+    ScanOperand q, k, v, u;          // u (MODE_GRAD): the row that the output's row is multiplied with, for the gradient of the log decays
+    const float* g;
+    long long gb, gt, gh;
+    const int* lengths;              // tokens of every sequence, nullptr: L
+    const float* skip;               // MODE_OUT: out += skip[head] v
+    void* out;                       // MODE_OUT
+    long long ob, ot, oh;
+    uint32_t out_wide;
+    const float* init;               // state before the sweep (or before every segment): [b][H][P][N] (segments: [b][segment][H][P][N])
+    float* last;                     // state behind the sweep (MODE_STATE: what a segment adds), or nullptr
+    float* decay;                    // MODE_STATE: [b][segment][H], the decay over the segment
+    float* part;                     // MODE_GRAD: [b][head tile][L][NP], NP = 64 or 128
+    float* dots;                     // MODE_GRAD: [b][head tile][L], u . out
+    const float* meet;               // MODE_GRAD forwards: states of the sweep backwards, as `init`; their product with this one's at the segments' ends
+    float* ends;                     //   [b][segment][head tile]
+    float* diag;                     //   sum over a segment's tokens of q . k, [b][segment][head tile]
+    uint32_t b, L, H, P, G, N, tiles, segments, seg_chunks, backwards;
+};
+
+// the text of an operand's row: token t of sequence b for head h, tile s
+template <class T>
+__device__ __forceinline__ const T* scan_row(const ScanOperand& o, uint32_t b, long long t, uint32_t head, uint32_t group, uint32_t tile) {
+    return (const T*)o.p + b * o.sb + t * o.st + (o.tiled ? head * o.sh + tile * SCAN_TILE : group * o.sh);
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+// two numbers as sums of NM bfloat16 numbers each, largest first
+template <int NM>
+__device__ __forceinline__ void split(float a, float b, uint32_t (&p)[NM]) {
+#pragma unroll
+    for (int i = 0; i < NM; i++) {
+        p[i] = pack_bf16(a, b);
+        if (i + 1 < NM) a -= __uint_as_float(p[i] << 16), b -= __uint_as_float(p[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// SCAN_Q rows of up to D columns into shared memory, plane by plane; zeros beyond `rows` and `width`.  step: elements from one row to the next.
+template <class T, int D, int THREADS>
+__device__ __forceinline__ void load_tile(__nv_bfloat16* dst, const T* src, long long step, int rows, int width, bool wide) {
+    constexpr int NI = ClearType<T>::planes, STR = D + SCAN_PAD;
+    const uint32_t base = (uint32_t)__cvta_generic_to_shared(dst);
+#pragma unroll 4
+    for (int i = threadIdx.x; i < SCAN_Q * D / 8; i += THREADS) {
+        const int r = i / (D / 8), c = i % (D / 8) * 8, count = r < rows ? width - c : 0;
+        const T* p = src + r * step + c;
+        if (NI == 1 && wide && count >= 8) {
+            cp_async16(base + (r * STR + c) * 2, p);
+            continue;
+        }
+        float v[8];
+        clear_load8(p, count, wide, v);
+        uint32_t pl[4][NI];
+#pragma unroll
+        for (int e = 0; e < 4; e++) split<NI>(v[2 * e], v[2 * e + 1], pl[e]);
+#pragma unroll
+        for (int j = 0; j < NI; j++)
+            *reinterpret_cast<uint4*>(dst + j * SCAN_Q * STR + r * STR + c) = make_uint4(pl[0][j], pl[1][j], pl[2][j], pl[3][j]);
+    }
+}
+
+template <class T, int DK, int DV, int MODE>
+struct ScanShared {
+    static constexpr int NI = ClearType<T>::planes;
+    static constexpr int NO = MODE == MODE_GRAD || NI == 3 ? 3 : 2;   // planes of what only the outputs depend on
+    static constexpr int K_STR = DK + SCAN_PAD, V_STR = DV + SCAN_PAD, S_STR = SCAN_Q + SCAN_PAD;
+    static constexpr int k = 0, v = k + NI * SCAN_Q * K_STR, q = v + NI * SCAN_Q * V_STR, s = q + (MODE ? NI * SCAN_Q * K_STR : 0);
+    static constexpr int words = s + (MODE ? NO * SCAN_Q * S_STR : 0);                        // in bfloat16 numbers
+    static constexpr int O_STR = DV + 4;                                                       // floats; the outputs' rows lie over v .. s
+    static_assert(!MODE || (words - q) * 2 >= SCAN_Q * O_STR * 4, "outputs fit over q and the scores");
+    static constexpr size_t bytes = (size_t)words * 2;
+};
+
+template <class T, int DK, int DV, int MODE>
+__global__ void __launch_bounds__(128) k_clear_scan(const ScanArgs a) {
+    using S = ScanShared<T, DK, DV, MODE>;
+    constexpr int NI = S::NI, NO = S::NO, NS = 3, MT = DV / 64, KT = DK / 8;
+    extern __shared__ __align__(128) __nv_bfloat16 sm[];
+    __shared__ __align__(16) float2 cum[SCAN_Q];               // log2 of the decay up to a token of the chunk, as a sum of two floats
+    __shared__ __align__(16) float grow[SCAN_Q], fade[SCAN_Q]; // decay from the chunk's start to a token; from a token to the chunk's end
+    __shared__ float words[4];
+    pdl_begin();
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, q4 = lane & 3;
+    // heads vary fastest: neighbours in the grid share the rows of their group
+    const uint32_t vheads = a.H * a.tiles, vh = blockIdx.x % vheads, seg = blockIdx.x / vheads % a.segments, b = blockIdx.x / vheads / a.segments;
+    const uint32_t head = vh / a.tiles, tile = vh % a.tiles, group = head / (a.H / a.G);
+    const int length = a.lengths ? min(max(a.lengths[b], 0), (int)a.L) : (int)a.L;
+    const int seg_tokens = (int)a.seg_chunks * SCAN_Q, t_lo = (int)seg * seg_tokens, t_hi = min(length, t_lo + seg_tokens);
+    const int pw = min(SCAN_TILE, (int)a.P - (int)tile * SCAN_TILE);   // channels of this tile
+    const bool is_last = a.backwards ? seg == 0 : (t_hi == length && (t_lo < length || seg == 0));
+    const size_t state_at = (size_t)head * a.P * a.N + (size_t)tile * SCAN_TILE * a.N, states = (size_t)a.H * a.P * a.N;
+    const size_t slot = (size_t)b * a.segments + seg;
+    if (MODE != MODE_STATE && t_lo >= length && !is_last) {
+        // nothing of the sequence lies here; what later kernels read is zero
+        if (MODE == MODE_GRAD && a.ends && tid == 0) a.ends[slot * vheads + vh] = 0.f, a.diag[slot * vheads + vh] = 0.f;
+        return;
+    }
+    const int kw = a.k.tiled ? pw : (int)a.N, vw = a.v.tiled ? pw : (int)a.N;
+#ifdef FESC_DEBUG_BOUNDS
+    if (t_lo < t_hi) {
+        const long long n = t_hi - t_lo - 1;
+        bool ok = DBG_REGION(scan_row<T>(a.k, b, t_lo, head, group, tile), (n * a.k.st + kw) * sizeof(T)) &&
+                  DBG_REGION(scan_row<T>(a.v, b, t_lo, head, group, tile), (n * a.v.st + vw) * sizeof(T)) &&
+                  DBG_REGION(a.g + b * a.gb + t_lo * a.gt + head * a.gh, (n * a.gt + 1) * sizeof(float));
+        if (MODE) ok = ok && DBG_REGION(scan_row<T>(a.q, b, t_lo, head, group, tile), (n * a.q.st + kw) * sizeof(T));
+        if (MODE == MODE_OUT) ok = ok && DBG_REGION((T*)a.out + b * a.ob + t_lo * a.ot + head * a.oh + tile * SCAN_TILE, (n * a.ot + vw) * sizeof(T));
+        if (MODE == MODE_GRAD)
+            ok = ok && DBG_REGION(scan_row<T>(a.u, b, t_lo, head, group, tile), (n * a.u.st + vw) * sizeof(T)) &&
+                 DBG_REGION(a.part + (((size_t)b * vheads + vh) * a.L + t_lo) * DV, (n + 1) * DV * sizeof(float)) &&
+                 DBG_REGION(a.dots + ((size_t)b * vheads + vh) * a.L + t_lo, (n + 1) * sizeof(float));
+        if (!ok) return;
+    }
+    if ((MODE && a.init && !DBG_REGION(a.init + (a.segments > 1 ? slot : b) * states + state_at, (size_t)pw * a.N * 4)) ||
+        (a.last && !DBG_REGION(a.last + (MODE == MODE_STATE ? slot : b) * states + state_at, (size_t)pw * a.N * 4)) ||
+        (MODE == MODE_GRAD && a.meet && !DBG_REGION(a.meet + (a.segments > 1 ? slot : b) * states + state_at, (size_t)pw * a.N * 4)))
+        return;
+#endif
+    __nv_bfloat16 *sk = sm + S::k, *sv = sm + S::v, *sq = sm + S::q, *ss = sm + S::s;
+    const uint32_t ak = (uint32_t)__cvta_generic_to_shared(sk), av = (uint32_t)__cvta_generic_to_shared(sv);
+    const uint32_t aq = (uint32_t)__cvta_generic_to_shared(sq), as = (uint32_t)__cvta_generic_to_shared(ss);
+    // the rows and columns that this lane addresses in a 16 x 16 block: left operands and transposed right ones (blocks of 8 x 8 down, then
+    // right), right operands (right, then down)
+    const int row_l = lane & 15, col_l = lane >> 4 << 3, row_r = (lane & 7) | (lane >> 4 << 3), col_r = lane & 8;
+    const int row_t = (lane & 7) | (lane >> 4 << 3), col_t = lane & 8;   // transposed left operands
+
+    // this warp's quarter of the state: rows (of v) warp * DV/4 + 16 m + g8 (+ 8), columns (of k) 8 n + 2 q4 (+ 1)
+    float st[MT][KT][4];
+    const float* init = MODE && a.init ? a.init + (a.segments > 1 ? slot : b) * states + state_at : nullptr;
+    auto state_index = [&](int m, int n, int e) {   // -1: not part of the state
+        const int rv = warp * (DV / 4) + 16 * m + g8 + (e & 2 ? 8 : 0), ck = 8 * n + 2 * q4 + (e & 1);
+        const int p = a.v.tiled ? rv : ck, c = a.v.tiled ? ck : rv;
+        return p < pw && c < (int)a.N ? p * (int)a.N + c : -1;
+    };
+#pragma unroll
+    for (int m = 0; m < MT; m++)
+#pragma unroll
+        for (int n = 0; n < KT; n++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const int at = init ? state_index(m, n, e) : -1;
+                st[m][n][e] = at >= 0 ? init[at] : 0.f;
+            }
+
+    const int chunks = t_hi > t_lo ? (t_hi - t_lo + SCAN_Q - 1) / SCAN_Q : 0;
+    float diag = 0.f;
+    double through = 0.0;                        // log2 of the decay over the segment (thread 0)
+    for (int c = 0; c < chunks; c++) {
+        // token of position i of the chunk: t0 + dir * i
+        const int valid = min(SCAN_Q, t_hi - t_lo - c * SCAN_Q), dir = a.backwards ? -1 : 1, t0 = a.backwards ? t_hi - 1 - c * SCAN_Q : t_lo + c * SCAN_Q;
+        load_tile<T, DK, 128>(sk, scan_row<T>(a.k, b, t0, head, group, tile), dir * a.k.st, valid, kw, a.k.wide);
+        load_tile<T, DV, 128>(sv, scan_row<T>(a.v, b, t0, head, group, tile), dir * a.v.st, valid, vw, a.v.wide);
+        if (MODE) load_tile<T, DK, 128>(sq, scan_row<T>(a.q, b, t0, head, group, tile), dir * a.q.st, valid, kw, a.q.wide);
+        if (warp == 0) {
+            // the decay that applies on the way to a position is its own token's forwards, the token's behind it backwards (none at the end)
+            double sum[2];
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                const int pos = 2 * lane + i, t = t0 + dir * pos + (a.backwards ? 1 : 0);
+                float gv = pos < valid && t < length ? a.g[b * a.gb + t * a.gt + head * a.gh] : 0.f;
+                gv = gv < SCAN_DROP ? SCAN_DROP : gv;
+                sum[i] = (double)gv * 1.4426950408889634 + (i ? sum[0] : 0.0);
+            }
+            double run = sum[1];
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const double w = __shfl_up_sync(~0u, run, o);
+                if (lane >= o) run += w;
+            }
+            const double before = run - sum[1], total = __shfl_sync(~0u, run, 31);
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                const double v = before + sum[i];
+                const float hi = (float)v;
+                cum[2 * lane + i] = make_float2(hi, (float)(v - hi));
+                grow[2 * lane + i] = exp2f(hi) * exp2f((float)(v - hi));
+                const double f = total - v;
+                fade[2 * lane + i] = exp2f((float)f);
+            }
+            through += total;
+        }
+        cp_async_wait();
+        __syncthreads();
+
+        if (MODE) {
+            // scores of 16 rows i per warp, columns j <= i: S_ij = G_ij (q_i . k_j), cut into planes
+            uint32_t qf[NI][DK / 16][4];
+#pragma unroll
+            for (int p = 0; p < NI; p++)
+#pragma unroll
+                for (int kk = 0; kk < DK / 16; kk++)
+                    ldsm4(qf[p][kk], aq + (p * SCAN_Q * S::K_STR + (16 * warp + row_l) * S::K_STR + 16 * kk + col_l) * 2);
+            const int i0 = 16 * warp + g8;
+            const float2 ci[2] = {cum[i0], cum[i0 + 8]};
+            for (int j = 0; j <= (int)warp; j++) {
+                float d[2][4] = {};
+#pragma unroll
+                for (int kk = 0; kk < DK / 16; kk++)
+#pragma unroll
+                    for (int pk = 0; pk < NI; pk++) {
+                        uint32_t kf[4];
+                        ldsm4(kf, ak + (pk * SCAN_Q * S::K_STR + (16 * j + row_r) * S::K_STR + 16 * kk + col_r) * 2);
+#pragma unroll
+                        for (int pq = 0; pq < NI; pq++)
+                            if (pk + pq < 3) mma(d[0], qf[pq][kk], kf[0], kf[1]), mma(d[1], qf[pq][kk], kf[2], kf[3]);
+                    }
+#pragma unroll
+                for (int n = 0; n < 2; n++) {
+                    const int jc = 16 * j + 8 * n + 2 * q4;
+                    const float2 c0 = cum[jc], c1 = cum[jc + 1];
+#pragma unroll
+                    for (int h = 0; h < 2; h++) {
+                        const int i = i0 + 8 * h;
+                        if (MODE == MODE_GRAD) diag += (i == jc ? d[n][2 * h] : 0.f) + (i == jc + 1 ? d[n][2 * h + 1] : 0.f);
+                        const float e0 = exp2f((ci[h].x - c0.x) + (ci[h].y - c0.y)), e1 = exp2f((ci[h].x - c1.x) + (ci[h].y - c1.y));
+                        uint32_t pl[NO];
+                        split<NO>(jc <= i ? d[n][2 * h] * e0 : 0.f, jc + 1 <= i ? d[n][2 * h + 1] * e1 : 0.f, pl);
+#pragma unroll
+                        for (int p = 0; p < NO; p++) *reinterpret_cast<uint32_t*>(ss + p * SCAN_Q * S::S_STR + i * S::S_STR + jc) = pl[p];
+                    }
+                }
+            }
+            __syncthreads();
+        }
+
+        // out^T = state q^T, columns times the decay since the chunk's start, + v^T S^T
+        float acc[MODE ? MT : 1][MODE ? 8 : 1][4];
+        if (MODE) {
+#pragma unroll
+            for (int m = 0; m < MT; m++)
+#pragma unroll
+                for (int n = 0; n < 8; n++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) acc[m][n][e] = 0.f;
+#pragma unroll
+            for (int kk = 0; kk < DK / 16; kk++) {
+                uint32_t sf[MT][NO][4];
+#pragma unroll
+                for (int m = 0; m < MT; m++)
+#pragma unroll
+                    for (int r = 0; r < 4; r++) {
+                        uint32_t pl[NO];
+                        const float(&x)[4] = st[m][2 * kk + (r >> 1)];
+                        split<NO>(x[2 * (r & 1)], x[2 * (r & 1) + 1], pl);
+#pragma unroll
+                        for (int p = 0; p < NO; p++) sf[m][p][r] = pl[p];
+                    }
+#pragma unroll
+                for (int n = 0; n < 4; n++)
+#pragma unroll
+                    for (int pq = 0; pq < NI; pq++) {
+                        uint32_t qf[4];
+                        ldsm4(qf, aq + (pq * SCAN_Q * S::K_STR + (16 * n + row_r) * S::K_STR + 16 * kk + col_r) * 2);
+#pragma unroll
+                        for (int p = 0; p < NO; p++)
+                            if (p + pq < NO || NI == 1)
+#pragma unroll
+                                for (int m = 0; m < MT; m++) mma(acc[m][2 * n], sf[m][p], qf[0], qf[1]), mma(acc[m][2 * n + 1], sf[m][p], qf[2], qf[3]);
+                    }
+            }
+#pragma unroll
+            for (int n = 0; n < 8; n++) {
+                const float2 e = *reinterpret_cast<const float2*>(grow + 8 * n + 2 * q4);
+#pragma unroll
+                for (int m = 0; m < MT; m++) acc[m][n][0] *= e.x, acc[m][n][1] *= e.y, acc[m][n][2] *= e.x, acc[m][n][3] *= e.y;
+            }
+        }
+        // state <- G_last state + (fade v)^T k
+        {
+            const float keep = grow[SCAN_Q - 1];
+#pragma unroll
+            for (int m = 0; m < MT; m++)
+#pragma unroll
+                for (int n = 0; n < KT; n++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) st[m][n][e] *= keep;
+        }
+#pragma unroll
+        for (int kk = 0; kk < SCAN_Q / 16; kk++) {
+            uint32_t vf[MT][NI][4], wf[MT][NS][4];
+#pragma unroll
+            for (int m = 0; m < MT; m++) {
+#pragma unroll
+                for (int p = 0; p < NI; p++)
+                    ldsm4t(vf[m][p], av + (p * SCAN_Q * S::V_STR + (16 * kk + row_t) * S::V_STR + warp * (DV / 4) + 16 * m + col_t) * 2);
+                // rows of the block are positions 16 kk + 2 q4 (+ 1), + 8 for the right half
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    float x = 0.f, y = 0.f;
+#pragma unroll
+                    for (int p = NI - 1; p >= 0; p--) x += __uint_as_float(vf[m][p][r] << 16), y += __uint_as_float(vf[m][p][r] & 0xFFFF0000u);
+                    const float2 f = *reinterpret_cast<const float2*>(fade + 16 * kk + 2 * q4 + (r & 2 ? 8 : 0));
+                    uint32_t pl[NS];
+                    split<NS>(x * f.x, y * f.y, pl);
+#pragma unroll
+                    for (int p = 0; p < NS; p++) wf[m][p][r] = pl[p];
+                }
+            }
+            if (MODE) {
+#pragma unroll
+                for (int n = 0; n < 4; n++) {
+                    if (n < kk) continue;             // positions i before all of these j
+#pragma unroll
+                    for (int p = 0; p < NO; p++) {
+                        uint32_t sf[4];
+                        ldsm4(sf, as + (p * SCAN_Q * S::S_STR + (16 * n + row_r) * S::S_STR + 16 * kk + col_r) * 2);
+#pragma unroll
+                        for (int pv = 0; pv < NI; pv++)
+                            if (p + pv < NO || NI == 1)
+#pragma unroll
+                                for (int m = 0; m < MT; m++) mma(acc[m][2 * n], vf[m][pv], sf[0], sf[1]), mma(acc[m][2 * n + 1], vf[m][pv], sf[2], sf[3]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < DK / 16; n++)
+#pragma unroll
+                for (int pk = 0; pk < NI; pk++) {
+                    uint32_t kf[4];
+                    ldsm4t(kf, ak + (pk * SCAN_Q * S::K_STR + (16 * kk + row_l) * S::K_STR + 16 * n + col_l) * 2);
+#pragma unroll
+                    for (int p = 0; p < NS; p++)
+                        if (p + pk < NS)
+#pragma unroll
+                            for (int m = 0; m < MT; m++) mma(st[m][2 * n], wf[m][p], kf[0], kf[1]), mma(st[m][2 * n + 1], wf[m][p], kf[2], kf[3]);
+                }
+        }
+
+        if (MODE) {
+            // out through shared memory (over q and the scores) for whole rows
+            __syncthreads();
+            float* so = reinterpret_cast<float*>(sq);
+#pragma unroll
+            for (int m = 0; m < MT; m++)
+#pragma unroll
+                for (int n = 0; n < 8; n++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        so[(8 * n + 2 * q4 + (e & 1)) * S::O_STR + warp * (DV / 4) + 16 * m + g8 + (e & 2 ? 8 : 0)] = acc[m][n][e];
+            __syncthreads();
+            if (MODE == MODE_OUT) {
+                T* out = (T*)a.out + b * a.ob + head * a.oh + tile * SCAN_TILE;
+                const float skip = a.skip ? a.skip[head] : 0.f;
+#pragma unroll
+                for (int i = tid; i < SCAN_Q * DV / 8; i += 128) {
+                    const int r = i / (DV / 8), cc = i % (DV / 8) * 8;
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; e++) v[e] = so[r * S::O_STR + cc + e];
+                    if (a.skip) {
+#pragma unroll
+                        for (int p = NI - 1; p >= 0; p--)
+#pragma unroll
+                            for (int e = 0; e < 8; e++) v[e] += skip * __bfloat162float(sv[p * SCAN_Q * S::V_STR + r * S::V_STR + cc + e]);
+                    }
+                    if (r < valid) clear_store8(out + (long long)(t0 + dir * r) * a.ot + cc, vw - cc, a.out_wide, v);
+                }
+            } else {
+                constexpr int E = DV / 32;
+                float* part = a.part + ((size_t)b * vheads + vh) * a.L * DV;
+                float* dots = a.dots + ((size_t)b * vheads + vh) * a.L;
+                for (int r = warp; r < valid; r += 4) {
+                    const int t = t0 + dir * r;
+                    const T* u = scan_row<T>(a.u, b, t, head, group, tile) + lane * E;
+                    float v[E], dot = 0.f;
+#pragma unroll
+                    for (int e = 0; e < E; e++) {
+                        v[e] = so[r * S::O_STR + lane * E + e];
+                        if ((int)lane * E + e < vw) dot += v[e] * ClearType<T>::to(u[e]);
+                    }
+                    if constexpr (E == 4) *reinterpret_cast<float4*>(part + (size_t)t * DV + lane * E) = make_float4(v[0], v[1], v[2], v[3]);
+                    else *reinterpret_cast<float2*>(part + (size_t)t * DV + lane * E) = make_float2(v[0], v[1]);
+#pragma unroll
+                    for (int o = 16; o; o >>= 1) dot += __shfl_xor_sync(~0u, dot, o);
+                    if (lane == 0) dots[t] = dot;
+                }
+            }
+        }
+        __syncthreads();
+    }
+
+    // the state behind the sweep
+    if (a.last && (MODE == MODE_STATE || is_last)) {
+        float* last = a.last + (MODE == MODE_STATE ? slot : b) * states + state_at;
+        // backwards the state belongs to the first token: the gradient of the state before it is one decay further
+        const float f = MODE && a.backwards && length > 0 ? expf(a.g[b * a.gb + head * a.gh]) : 1.f;
+#pragma unroll
+        for (int m = 0; m < MT; m++)
+#pragma unroll
+            for (int n = 0; n < KT; n++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const int at = state_index(m, n, e);
+                    if (at >= 0) last[at] = st[m][n][e] * f;
+                }
+    }
+    if (MODE == MODE_STATE && tid == 0 && tile == 0) a.decay[slot * a.H + head] = (float)exp2(through);
+    if (MODE == MODE_GRAD && a.ends) {
+        // <state, gradient of the state> at the segment's end, one decay on from what the sweep backwards starts this segment with
+        float sum = 0.f;
+        const float* meet = a.meet ? a.meet + (a.segments > 1 ? slot : b) * states + state_at : nullptr;
+        if (meet) {
+#pragma unroll
+            for (int m = 0; m < MT; m++)
+#pragma unroll
+                for (int n = 0; n < KT; n++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        const int at = state_index(m, n, e);
+                        if (at >= 0) sum += st[m][n][e] * meet[at];
+                    }
+            if (t_hi < length) sum *= expf(a.g[b * a.gb + t_hi * a.gt + head * a.gh]);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o), diag += __shfl_xor_sync(~0u, diag, o);
+        __shared__ float dw[4];
+        if (lane == 0) words[warp] = sum, dw[warp] = diag;
+        __syncthreads();
+        if (tid == 0) {
+            a.ends[slot * vheads + vh] = (words[0] + words[1]) + (words[2] + words[3]);
+            a.diag[slot * vheads + vh] = (dw[0] + dw[1]) + (dw[2] + dw[3]);
+        }
+    }
+}
+
+// one type's kernels, by mode and by whether states have more than 64 columns
+template <class T>
+cudaError_t scan_launch(const ScanArgs& a, int mode, cudaStream_t st) {
+    auto go = [&](auto kernel, size_t smem) {
+        cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        return e != cudaSuccess ? e : launch(kernel, dim3(a.b * a.segments * a.H * a.tiles), dim3(128), smem, st, a);
+    };
+    const bool big = a.N > 64;
+    switch (mode) {
+        case MODE_STATE: return big ? go(k_clear_scan<T, 128, 64, MODE_STATE>, ScanShared<T, 128, 64, MODE_STATE>::bytes)
+                                    : go(k_clear_scan<T, 64, 64, MODE_STATE>, ScanShared<T, 64, 64, MODE_STATE>::bytes);
+        case MODE_OUT: return big ? go(k_clear_scan<T, 128, 64, MODE_OUT>, ScanShared<T, 128, 64, MODE_OUT>::bytes)
+                                  : go(k_clear_scan<T, 64, 64, MODE_OUT>, ScanShared<T, 64, 64, MODE_OUT>::bytes);
+        default: return big ? go(k_clear_scan<T, 64, 128, MODE_GRAD>, ScanShared<T, 64, 128, MODE_GRAD>::bytes)
+                            : go(k_clear_scan<T, 64, 64, MODE_GRAD>, ScanShared<T, 64, 64, MODE_GRAD>::bytes);
+    }
+}
+extern template cudaError_t scan_launch<__nv_bfloat16>(const ScanArgs&, int, cudaStream_t);
+extern template cudaError_t scan_launch<__half>(const ScanArgs&, int, cudaStream_t);
+extern template cudaError_t scan_launch<float>(const ScanArgs&, int, cudaStream_t);
