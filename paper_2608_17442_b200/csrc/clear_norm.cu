@@ -2,16 +2,15 @@
 //   v = y * silu(z),  h = r + s * v,  n = gamma * h / sqrt(mean h^2 + eps)      (mean over a group of channels)
 // the products that the encrypted path forms in fesc_norm_square and fesc_norm_scale, with the gate and residual of the block.
 //
-// One pass: a group of a row is read once into registers, its sums go through shuffles (and shared memory between warps), and what depends on
-// them is written from the registers.  Bound by memory.  A thread holds up to NV x 8 neighbours; a CTA deals out as many rows as it has
-// teams of threads.
+// One pass: a thread holds eight neighbours of a row, as many warps as a group of channels needs form a team (3 for 768 channels, 6 for
+// 1536), sums go through shuffles and one exchange in shared memory, and what depends on them is written from the registers.  Bound by memory.
 // The gradients of gamma and s are sums over rows: a CTA adds up its own rows in a fixed order, a second kernel adds up the CTAs, so the
-// results do not depend on the order in which CTAs run.
+// results do not depend on the order in which CTAs run.  There the next row's loads are under way while a row is computed.
 #define FESC_DBG_FILE 16   // file id in the sites a debug build reports
 #include "clear.cuh"
 
-#define NORM_THREADS 256
-#define NORM_MAX_WIDTH 8192     // channels of a group: 512 threads x 16 registers
+#define NORM_WARPS 8            // of a CTA, unless a team is larger
+#define NORM_MAX_WIDTH 8192     // channels of a group: 32 warps of 256
 
 struct NormArgs {
     const void *y, *gate, *residual, *dn, *dh;
@@ -22,187 +21,203 @@ struct NormArgs {
     uint32_t rows, d, width;     // width: channels of a group
     float eps;
     uint32_t wide;               // every buffer allows 16-byte accesses
+    uint32_t team_warps;
 };
 
-// The sums of a and b over a team of TPR threads, in the same order for every thread.  `turn` alternates between calls: the words of a turn are
-// written again only after the barrier of the next.
-template <int TPR, int TEAMS>
-__device__ __forceinline__ void team_sum(float& a, float& b, float2 (*words)[TEAMS][TPR / 32], uint32_t turn) {
+// The sums of a and b over a team of warps, in the same order for every thread.  The words of a turn are written again two turns later, behind the
+// barrier of the next.
+__device__ __forceinline__ void team_sum(float& a, float& b, float2* words, uint32_t team_warps) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(~0u, a, o), b += __shfl_xor_sync(~0u, b, o);
-    if constexpr (TPR > 32) {
-        const uint32_t team = threadIdx.x / TPR, warp = threadIdx.x % TPR / 32;
-        float2(&w)[TPR / 32] = words[turn & 1][team];
-        if (threadIdx.x % 32 == 0) w[warp] = make_float2(a, b);
-        __syncthreads();
-        a = b = 0.f;
-#pragma unroll
-        for (int i = 0; i < TPR / 32; i++) a += w[i].x, b += w[i].y;
+    if (team_warps == 1) return;
+    const uint32_t warp = threadIdx.x >> 5, first = warp / team_warps * team_warps;
+    if ((threadIdx.x & 31) == 0) words[warp] = make_float2(a, b);
+    __syncthreads();
+    a = b = 0.f;
+    for (uint32_t i = 0; i < team_warps; i++) {
+        const float2 w = words[first + i];
+        a += w.x, b += w.y;
     }
 }
 
 __device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
 
-template <class T, int TPR, int NV>
-__global__ void __launch_bounds__(TPR > NORM_THREADS ? TPR : NORM_THREADS) k_clear_norm(const NormArgs a) {
-    constexpr int TEAMS = TPR > NORM_THREADS ? 1 : NORM_THREADS / TPR;
-    __shared__ float2 words[2][TEAMS][TPR / 32];
-    pdl_begin();
-    const uint32_t row = blockIdx.x * TEAMS + threadIdx.x / TPR, lane = threadIdx.x % TPR, first = blockIdx.y * a.width;
-    const T* y = (const T*)a.y + (long long)row * a.sy + first;
-    const T* z = a.gate ? (const T*)a.gate + (long long)row * a.sgate + first : nullptr;
-    const T* r = a.residual ? (const T*)a.residual + (long long)row * a.sresidual + first : nullptr;
-    T* n = (T*)a.n + (long long)row * a.sn + first;
-    T* ho = a.h ? (T*)a.h + (long long)row * a.sh + first : nullptr;
-    const size_t bytes = a.width * sizeof(T);
-    bool live = row < a.rows;
-    if (live) live = DBG_REGION(y, bytes) && (!z || DBG_REGION(z, bytes)) && (!r || DBG_REGION(r, bytes)) && DBG_REGION(n, bytes) &&
-                     (!ho || DBG_REGION(ho, bytes)) && DBG_REGION(a.gamma, a.d * sizeof(float)) && (!a.scale || DBG_REGION(a.scale, a.d * sizeof(float)));
-    float h[NV][8], sum = 0.f, unused = 0.f;
+// Eight neighbours of a row as they are in memory: what a thread keeps between its two looks at them (half the registers of float32 for 16-bit types)
+template <class T>
+struct Eight {
+    uint4 w[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* p, int count, bool wide) {
+        if (wide && count >= 8) {
 #pragma unroll
-    for (int i = 0; i < NV; i++) {
-        const int c = (i * TPR + lane) * 8, count = live ? (int)a.width - c : 0;
-        clear_load8(y + c, count, a.wide, h[i]);
-        if (z) {
-            float g[8];
-            clear_load8(z + c, count, a.wide, g);
+            for (int i = 0; i < (int)sizeof(T) / 2; i++) w[i] = reinterpret_cast<const uint4*>(p)[i];
+        } else {
+            T v[8];
 #pragma unroll
-            for (int e = 0; e < 8; e++) h[i][e] *= g[e] * sigmoid(g[e]);
+            for (int i = 0; i < 8; i++) v[i] = i < count ? p[i] : ClearType<T>::from(0.f);
+            memcpy(w, v, sizeof(v));
         }
-        if (a.scale) {
-            float s[8];
-            clear_load8(a.scale + first + c, count, a.wide, s);
-#pragma unroll
-            for (int e = 0; e < 8; e++) h[i][e] *= s[e];
-        }
-        if (r) {
-            float v[8];
-            clear_load8(r + c, count, a.wide, v);
-#pragma unroll
-            for (int e = 0; e < 8; e++) h[i][e] += v[e];
-        }
-        if (ho) clear_store8(ho + c, count, a.wide, h[i]);
-#pragma unroll
-        for (int e = 0; e < 8; e++) sum += e < count ? h[i][e] * h[i][e] : 0.f;
     }
-    team_sum<TPR, TEAMS>(sum, unused, words, 0);
+    __device__ __forceinline__ float operator[](int i) const {      // i known when compiled
+        const uint32_t u[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
+        if constexpr (sizeof(T) == 4) {
+            const uint32_t x[4] = {w[sizeof(T) / 2 - 1].x, w[sizeof(T) / 2 - 1].y, w[sizeof(T) / 2 - 1].z, w[sizeof(T) / 2 - 1].w};
+            return __uint_as_float(i < 4 ? u[i & 3] : x[i & 3]);
+        } else if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+            return __uint_as_float(i & 1 ? u[i >> 1] & 0xFFFF0000u : u[i >> 1] << 16);
+        } else {
+            const __half2 h = *reinterpret_cast<const __half2*>(&u[i >> 1]);
+            return i & 1 ? __high2float(h) : __low2float(h);
+        }
+    }
+};
+
+template <class T, bool GATE, bool RESIDUAL>
+__global__ void __launch_bounds__(1024) k_clear_norm(const NormArgs a) {
+    __shared__ float2 words[32];
+    pdl_begin();
+    const uint32_t teams = (blockDim.x >> 5) / a.team_warps, team = (threadIdx.x >> 5) / a.team_warps, first = blockIdx.y * a.width;
+    const uint32_t row = blockIdx.x * teams + team;
+    const int c = (int)(threadIdx.x - team * a.team_warps * 32) * 8, count = row < a.rows ? (int)a.width - c : 0;
+    const T* y = (const T*)a.y + (long long)row * a.sy + first + c;
+    const T* z = GATE ? (const T*)a.gate + (long long)row * a.sgate + first + c : nullptr;
+    const T* r = RESIDUAL ? (const T*)a.residual + (long long)row * a.sresidual + first + c : nullptr;
+    T* n = (T*)a.n + (long long)row * a.sn + first + c;
+    T* ho = a.h ? (T*)a.h + (long long)row * a.sh + first + c : nullptr;
+    const size_t bytes = (size_t)min(max(count, 0), 8) * sizeof(T);
+    bool live = count > 0;
+    if (live) live = DBG_REGION(y, bytes) && (!GATE || DBG_REGION(z, bytes)) && (!RESIDUAL || DBG_REGION(r, bytes)) && DBG_REGION(n, bytes) &&
+                     (!ho || DBG_REGION(ho, bytes)) && DBG_REGION(a.gamma, a.d * sizeof(float)) && (!a.scale || DBG_REGION(a.scale, a.d * sizeof(float)));
+    const int some = live ? count : 0;
+    float h[8], g[8], sum = 0.f, unused = 0.f;
+    clear_load8(y, some, a.wide, h);
+    if (GATE) {
+        float v[8];
+        clear_load8(z, some, a.wide, v);
+#pragma unroll
+        for (int e = 0; e < 8; e++) h[e] *= v[e] * sigmoid(v[e]);
+    }
+    if (RESIDUAL) {
+        float v[8], s[8];
+        clear_load8(r, some, a.wide, v);
+        if (a.scale) clear_load8(a.scale + first + c, some, a.wide, s);
+#pragma unroll
+        for (int e = 0; e < 8; e++) h[e] = v[e] + (a.scale ? s[e] * h[e] : h[e]);
+    }
+    clear_load8(a.gamma + first + c, some, a.wide, g);
+    if (ho) clear_store8(ho, some, a.wide, h);
+#pragma unroll
+    for (int e = 0; e < 8; e++) sum += h[e] * h[e];      // zeros behind the row's end
+    team_sum(sum, unused, words, a.team_warps);
     const float rho = rsqrtf(sum / (float)a.width + a.eps);
 #pragma unroll
-    for (int i = 0; i < NV; i++) {
-        const int c = (i * TPR + lane) * 8, count = live ? (int)a.width - c : 0;
-        float g[8];
-        clear_load8(a.gamma + first + c, count, a.wide, g);
-#pragma unroll
-        for (int e = 0; e < 8; e++) g[e] *= h[i][e] * rho;
-        clear_store8(n + c, count, a.wide, g);
-    }
+    for (int e = 0; e < 8; e++) g[e] *= h[e] * rho;
+    clear_store8(n, some, a.wide, g);
 }
 
 // dh_tot = dh + rho w - h rho^3 mean(w h),  w = gamma dn;  dr = dh_tot;  ds = sum_rows dh_tot v;  dv = s dh_tot;
 // dy = dv silu(z);  dz = dv y sigma (1 + z (1 - sigma));  dgamma = sum_rows dn h rho
-template <class T, int TPR, int NV>
-__global__ void __launch_bounds__(TPR > NORM_THREADS ? TPR : NORM_THREADS) k_clear_norm_backward(const NormArgs a) {
-    constexpr int TEAMS = TPR > NORM_THREADS ? 1 : NORM_THREADS / TPR;
-    __shared__ float2 words[2][TEAMS][TPR / 32];
-    __shared__ float cols[TEAMS > 1 ? TEAMS : 1][TEAMS > 1 ? TPR * 8 : 1];
+template <class T, bool GATE, bool RESIDUAL, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : 2) k_clear_norm_backward(const NormArgs a) {
+    __shared__ float2 words[2][32];
+    __shared__ float cols[NORM_WARPS * 256];
     pdl_begin();
-    const uint32_t team = threadIdx.x / TPR, lane = threadIdx.x % TPR, first = blockIdx.y * a.width;
-    const size_t bytes = a.width * sizeof(T);
-    float dgamma[NV][8] = {}, dscale[NV][8] = {};
+    const uint32_t teams = (blockDim.x >> 5) / a.team_warps, team = (threadIdx.x >> 5) / a.team_warps, first = blockIdx.y * a.width;
+    const int c = (int)(threadIdx.x - team * a.team_warps * 32) * 8, width = (int)a.width - c;
+    const T *py = (const T*)a.y + first + c, *pz = (const T*)a.gate + first + c, *pr = (const T*)a.residual + first + c, *pn = (const T*)a.dn + first + c,
+            *ph = (const T*)a.dh + first + c;
+    const bool dh = RESIDUAL && a.dh;
+    float g[8], s[8], dgamma[8] = {}, dscale[8] = {};
+    const bool ok = DBG_REGION(a.gamma, a.d * sizeof(float)) && (!a.scale || DBG_REGION(a.scale, a.d * sizeof(float)));
+    clear_load8(a.gamma + first + c, ok ? width : 0, a.wide, g);
+    if (RESIDUAL && a.scale) clear_load8(a.scale + first + c, ok ? width : 0, a.wide, s);
+    Eight<T> y, z, r, w, hh, ny, nz, nr, nw, nh;
+    auto fetch = [&](uint32_t row, Eight<T>& vy, Eight<T>& vz, Eight<T>& vr, Eight<T>& vw, Eight<T>& vh) {
+        int count = row < a.rows && width > 0 ? width : 0;
+        const size_t bytes = (size_t)min(count, 8) * sizeof(T);
+        if (count && !(DBG_REGION(py + row * a.sy, bytes) && DBG_REGION(pn + row * a.sdn, bytes) && (!GATE || DBG_REGION(pz + row * a.sgate, bytes)) &&
+                       (!RESIDUAL || DBG_REGION(pr + row * a.sresidual, bytes)) && (!dh || DBG_REGION(ph + row * a.sdh, bytes))))
+            count = 0;
+        vy.load(py + row * a.sy, count, a.wide), vw.load(pn + row * a.sdn, count, a.wide);
+        if (GATE) vz.load(pz + row * a.sgate, count, a.wide);
+        if (RESIDUAL) vr.load(pr + row * a.sresidual, count, a.wide);
+        if (dh) vh.load(ph + row * a.sdh, count, a.wide);
+    };
+    fetch(blockIdx.x * teams + team, ny, nz, nr, nw, nh);
     uint32_t turn = 0;
     // the same number of turns for every team: barriers inside
-    for (uint32_t base = blockIdx.x * TEAMS; base < a.rows; base += gridDim.x * TEAMS, turn++) {
+    for (uint32_t base = blockIdx.x * teams; base < a.rows; base += gridDim.x * teams, turn ^= 1) {
         const uint32_t row = base + team;
-        const T* y = (const T*)a.y + (long long)row * a.sy + first;
-        const T* z = a.gate ? (const T*)a.gate + (long long)row * a.sgate + first : nullptr;
-        const T* r = a.residual ? (const T*)a.residual + (long long)row * a.sresidual + first : nullptr;
-        const T* dn = (const T*)a.dn + (long long)row * a.sdn + first;
-        const T* dh = a.dh ? (const T*)a.dh + (long long)row * a.sdh + first : nullptr;
-        T* dy = (T*)a.dy + (long long)row * a.sdy + first;
-        T* dz = a.dgate ? (T*)a.dgate + (long long)row * a.sdgate + first : nullptr;
-        T* dr = a.dresidual ? (T*)a.dresidual + (long long)row * a.sdresidual + first : nullptr;
-        bool live = row < a.rows;
-        if (live) live = DBG_REGION(y, bytes) && (!z || DBG_REGION(z, bytes)) && (!r || DBG_REGION(r, bytes)) && DBG_REGION(dn, bytes) &&
-                         (!dh || DBG_REGION(dh, bytes)) && DBG_REGION(dy, bytes) && (!dz || DBG_REGION(dz, bytes)) && (!dr || DBG_REGION(dr, bytes));
-        float yv[NV][8], zv[NV][8], h[NV][8], w[NV][8], sum = 0.f, dot = 0.f;
+        y = ny, z = nz, r = nr, w = nw, hh = nh;
+        fetch(row + gridDim.x * teams, ny, nz, nr, nw, nh);
+        float h[8], sig[8], sum = 0.f, dot = 0.f;
 #pragma unroll
-        for (int i = 0; i < NV; i++) {
-            const int c = (i * TPR + lane) * 8, count = live ? (int)a.width - c : 0;
-            clear_load8(y + c, count, a.wide, yv[i]);
-            clear_load8(dn + c, count, a.wide, w[i]);
-            if (z) clear_load8(z + c, count, a.wide, zv[i]);
-            if (r) clear_load8(r + c, count, a.wide, h[i]);
+        for (int e = 0; e < 8; e++) {
+            sig[e] = GATE ? sigmoid(z[e]) : 1.f;
+            float v = y[e];
+            if (GATE) v *= z[e] * sig[e];
+            if (RESIDUAL) v = r[e] + (a.scale ? s[e] * v : v);
+            h[e] = v;
+            sum += v * v, dot += g[e] * w[e] * v;
         }
-#pragma unroll
-        for (int i = 0; i < NV; i++) {
-            const int c = (i * TPR + lane) * 8, count = live ? (int)a.width - c : 0;
-            float s[8], g[8];
-            if (a.scale) clear_load8(a.scale + first + c, count, a.wide, s);
-            clear_load8(a.gamma + first + c, count, a.wide, g);
-#pragma unroll
-            for (int e = 0; e < 8; e++) {
-                float v = yv[i][e];
-                if (z) v *= zv[i][e] * sigmoid(zv[i][e]);
-                if (a.scale) v *= s[e];
-                h[i][e] = r ? h[i][e] + v : v;
-                if (e < count) sum += h[i][e] * h[i][e], dot += g[e] * w[i][e] * h[i][e];
-            }
-        }
-        team_sum<TPR, TEAMS>(sum, dot, words, turn);
+        team_sum(sum, dot, words[turn], a.team_warps);
         const float rho = rsqrtf(sum / (float)a.width + a.eps), k = rho * rho * rho * (dot / (float)a.width);
+        int count = row < a.rows ? width : 0;
+        T* dy = (T*)a.dy + (long long)row * a.sdy + first + c;
+        T* dz = GATE ? (T*)a.dgate + (long long)row * a.sdgate + first + c : nullptr;
+        T* dr = RESIDUAL ? (T*)a.dresidual + (long long)row * a.sdresidual + first + c : nullptr;
+        const size_t bytes = (size_t)min(max(count, 0), 8) * sizeof(T);
+        if (count > 0 && !(DBG_REGION(dy, bytes) && (!GATE || DBG_REGION(dz, bytes)) && (!RESIDUAL || DBG_REGION(dr, bytes)))) count = 0;
+        float d[8];
 #pragma unroll
-        for (int i = 0; i < NV; i++) {
-            const int c = (i * TPR + lane) * 8, count = live ? (int)a.width - c : 0;
-            float s[8], g[8], d[8];
-            if (a.scale) clear_load8(a.scale + first + c, count, a.wide, s);
-            clear_load8(a.gamma + first + c, count, a.wide, g);
-            if (dh) clear_load8(dh + c, count, a.wide, d);
-#pragma unroll
-            for (int e = 0; e < 8; e++) {
-                const float t = rho * g[e] * w[i][e] - k * h[i][e];
-                d[e] = dh ? d[e] + t : t;
-                if (e < count) dgamma[i][e] += w[i][e] * h[i][e] * rho;
-            }
-            if (dr) clear_store8(dr + c, count, a.wide, d);
-#pragma unroll
-            for (int e = 0; e < 8; e++) {
-                const float sig = z ? sigmoid(zv[i][e]) : 1.f, gate = z ? zv[i][e] * sig : 1.f, yy = yv[i][e];
-                if (a.scale && e < count) dscale[i][e] += d[e] * yy * gate;
-                if (a.scale) d[e] *= s[e];
-                yv[i][e] = d[e] * gate;
-                if (z) zv[i][e] = d[e] * yy * sig * (1.f + zv[i][e] * (1.f - sig));
-            }
-            clear_store8(dy + c, count, a.wide, yv[i]);
-            if (dz) clear_store8(dz + c, count, a.wide, zv[i]);
+        for (int e = 0; e < 8; e++) {
+            d[e] = rho * g[e] * w[e] - k * h[e];
+            if (dh) d[e] += hh[e];
+            dgamma[e] += w[e] * h[e] * rho;
         }
+        if (RESIDUAL) {
+            clear_store8(dr, count, a.wide, d);
+            if (a.scale) {
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    dscale[e] += d[e] * (GATE ? y[e] * z[e] * sig[e] : y[e]);
+                    d[e] *= s[e];
+                }
+            }
+        }
+        if (GATE) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                v[e] = d[e] * y[e] * sig[e] * (1.f + z[e] * (1.f - sig[e]));
+                d[e] *= z[e] * sig[e];
+            }
+            clear_store8(dz, count, a.wide, v);
+        }
+        clear_store8(dy, count, a.wide, d);
     }
     // the teams' sums, team by team
     float* part = a.part + (size_t)blockIdx.x * 2 * a.d + first;
     if (!DBG_REGION(part, (a.d + a.width) * sizeof(float))) return;
+    auto leave = [&](const float(&v)[8], float* out) {
+        if (teams == 1) {
 #pragma unroll
-    for (int q = 0; q < 2; q++) {
-        if (q && !a.scale) break;
-#pragma unroll
-        for (int i = 0; i < NV; i++) {
-            float(&v)[8] = q ? dscale[i] : dgamma[i];
-            const int c = (i * TPR + lane) * 8;
-            if constexpr (TEAMS > 1) {
-                __syncthreads();
-#pragma unroll
-                for (int e = 0; e < 8; e++) cols[team][lane * 8 + e] = v[e];
-                __syncthreads();
-                for (uint32_t j = threadIdx.x; j < TPR * 8; j += NORM_THREADS) {
-                    float t = 0.f;
-                    for (int m = 0; m < TEAMS; m++) t += cols[m][j];
-                    if (i * TPR * 8 + j < a.width) part[(size_t)q * a.d + i * TPR * 8 + j] = t;
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; e++)
-                    if (c + e < (int)a.width) part[(size_t)q * a.d + c + e] = v[e];
-            }
+            for (int e = 0; e < 8; e++)
+                if (e < width) out[c + e] = v[e];
+            return;
         }
-    }
+        const uint32_t span = a.team_warps * 256;       // a CTA of several teams has at most NORM_WARPS warps
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 8; e++) cols[team * span + c + e] = v[e];
+        __syncthreads();
+        for (uint32_t j = threadIdx.x; j < a.width; j += blockDim.x) {
+            float t = 0.f;
+            for (uint32_t m = 0; m < teams; m++) t += cols[m * span + j];
+            out[j] = t;
+        }
+    };
+    leave(dgamma, part);
+    if (RESIDUAL && a.scale) leave(dscale, part + a.d);
 }
 
 // out[c] = the CTAs' sums of channel c: 8 threads take every eighth CTA each, then add up
@@ -227,13 +242,13 @@ __global__ void __launch_bounds__(256) k_clear_norm_columns(const float* part, f
 // ---------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------
-// threads of a row and vectors of a thread: as few threads as keep at most `most` vectors each
+// warps of a group of channels, and teams of them in a CTA
 struct NormShape {
-    uint32_t tpr, nv;
+    uint32_t warps, teams;
 };
-static NormShape norm_shape(uint32_t width, uint32_t small, uint32_t middle, uint32_t most) {
-    const uint32_t tpr = width <= small * 8 * most ? small : width <= middle * 8 * most ? middle : 512;
-    return {tpr, (width + tpr * 8 - 1) / (tpr * 8)};
+static NormShape norm_shape(const fesc_clear_norm_desc* desc) {
+    const uint32_t warps = (desc->d / desc->groups + 255) / 256;
+    return {warps, warps < NORM_WARPS ? NORM_WARPS / warps : 1};
 }
 
 static int norm_check(const fesc_clear_norm_desc* desc, const char** what) {
@@ -257,20 +272,14 @@ static bool norm_wide(const fesc_clear_norm_desc* desc, const void* p, int64_t s
 }
 
 template <class T>
-static void (*norm_kernel(NormShape s))(NormArgs) {
-#define NORM_PICK(t, v) \
-    if (s.tpr == t && s.nv == v) return k_clear_norm<T, t, v>;
-    NORM_PICK(32, 1) NORM_PICK(32, 2) NORM_PICK(32, 3) NORM_PICK(32, 4) NORM_PICK(64, 3) NORM_PICK(64, 4) NORM_PICK(512, 1) NORM_PICK(512, 2)
-#undef NORM_PICK
-    return nullptr;
+static void (*norm_kernel(bool gate, bool residual))(NormArgs) {
+    return gate ? residual ? k_clear_norm<T, true, true> : k_clear_norm<T, true, false> : residual ? k_clear_norm<T, false, true> : k_clear_norm<T, false, false>;
 }
-template <class T>
-static void (*norm_backward_kernel(NormShape s))(NormArgs) {
-#define NORM_PICK(t, v) \
-    if (s.tpr == t && s.nv == v) return k_clear_norm_backward<T, t, v>;
-    NORM_PICK(32, 1) NORM_PICK(32, 2) NORM_PICK(128, 1) NORM_PICK(128, 2) NORM_PICK(512, 1) NORM_PICK(512, 2)
-#undef NORM_PICK
-    return nullptr;
+// CTAs of more than 256 threads (rows of more than 2048 channels) have 64 registers a thread and keep some of a row's words in local memory
+template <class T, int THREADS>
+static void (*norm_backward_kernel(bool gate, bool residual))(NormArgs) {
+    return gate ? residual ? k_clear_norm_backward<T, true, true, THREADS> : k_clear_norm_backward<T, true, false, THREADS>
+                : residual ? k_clear_norm_backward<T, false, true, THREADS> : k_clear_norm_backward<T, false, false, THREADS>;
 }
 template <class F>
 static auto by_type(uint32_t type, F f) {
@@ -279,9 +288,9 @@ static auto by_type(uint32_t type, F f) {
 
 // CTAs of the backward pass per group of channels: rows are dealt out to at most this many, whose column sums are added up afterwards
 static uint32_t norm_ctas(const fesc_clear_norm_desc* desc, const NormShape& s) {
-    const uint32_t teams = s.tpr > NORM_THREADS ? 1 : NORM_THREADS / s.tpr, all = (desc->rows + teams - 1) / teams;
+    const uint64_t all = (desc->rows + s.teams - 1) / s.teams;
     const uint32_t most = 4 * 148;
-    return all < most ? all : most;
+    return all < most ? (uint32_t)all : most;
 }
 
 extern "C" int fesc_clear_norm(const fesc_clear_norm_desc* desc, const void* d_y, const float* d_gamma, const void* d_gate, const void* d_residual,
@@ -306,18 +315,17 @@ extern "C" int fesc_clear_norm(const fesc_clear_norm_desc* desc, const void* d_y
     a.wide = width * bytes % 16 == 0 && width % 4 == 0 && norm_wide(desc, d_y, a.sy, bytes) && norm_wide(desc, d_gate, a.sgate, bytes) &&
              norm_wide(desc, d_residual, a.sresidual, bytes) && norm_wide(desc, d_n, a.sn, bytes) && norm_wide(desc, d_h, a.sh, bytes) &&
              norm_wide(desc, d_gamma, 0, 4) && norm_wide(desc, d_scale, 0, 4);
-    const NormShape s = norm_shape(width, 32, 64, 4);
-    const uint32_t teams = s.tpr > NORM_THREADS ? 1 : NORM_THREADS / s.tpr;
-    auto kernel = by_type(desc->type, [&](auto t) { return norm_kernel<decltype(t)>(s); });
-    if (!kernel) return clear_fail(FESC_EINVAL, "clear_norm: no kernel for this width");
-    CLEAR_CUDA(launch(kernel, dim3((a.rows + teams - 1) / teams, desc->groups), dim3(s.tpr > NORM_THREADS ? s.tpr : NORM_THREADS), 0, (cudaStream_t)stream, a));
+    const NormShape s = norm_shape(desc);
+    a.team_warps = s.warps;
+    auto kernel = by_type(desc->type, [&](auto t) { return norm_kernel<decltype(t)>(d_gate, d_residual); });
+    CLEAR_CUDA(launch(kernel, dim3((a.rows + s.teams - 1) / s.teams, desc->groups), dim3(s.teams * s.warps * 32), 0, (cudaStream_t)stream, a));
     return FESC_OK;
 }
 
 extern "C" size_t fesc_clear_norm_backward_work(const fesc_clear_norm_desc* desc) {
     const char* what;
     if (!desc || norm_check(desc, &what) != FESC_OK) return 0;
-    return (size_t)norm_ctas(desc, norm_shape(desc->d / desc->groups, 32, 128, 2)) * 2 * desc->d * sizeof(float);
+    return (size_t)norm_ctas(desc, norm_shape(desc)) * 2 * desc->d * sizeof(float);
 }
 
 extern "C" int fesc_clear_norm_backward(const fesc_clear_norm_desc* desc, const void* d_y, const float* d_gamma, const void* d_gate,
@@ -362,11 +370,13 @@ extern "C" int fesc_clear_norm_backward(const fesc_clear_norm_desc* desc, const 
              norm_wide(desc, d_residual, a.sresidual, bytes) && norm_wide(desc, d_dn, a.sdn, bytes) && norm_wide(desc, d_dh, a.sdh, bytes) &&
              norm_wide(desc, d_dy, a.sdy, bytes) && norm_wide(desc, d_dgate, a.sdgate, bytes) && norm_wide(desc, d_dresidual, a.sdresidual, bytes) &&
              norm_wide(desc, d_gamma, 0, 4) && norm_wide(desc, d_scale, 0, 4);
-    const NormShape s = norm_shape(width, 32, 128, 2);
+    const NormShape s = norm_shape(desc);
+    a.team_warps = s.warps;
     const uint32_t ctas = norm_ctas(desc, s);
-    auto kernel = by_type(desc->type, [&](auto t) { return norm_backward_kernel<decltype(t)>(s); });
-    if (!kernel) return clear_fail(FESC_EINVAL, "clear_norm_backward: no kernel for this width");
-    CLEAR_CUDA(launch(kernel, dim3(ctas, desc->groups), dim3(s.tpr > NORM_THREADS ? s.tpr : NORM_THREADS), 0, st, a));
+    auto kernel = by_type(desc->type, [&](auto t) { 
+        return s.warps > NORM_WARPS ? norm_backward_kernel<decltype(t), 1024>(d_gate, d_residual) : norm_backward_kernel<decltype(t), 256>(d_gate, d_residual);
+    });
+    CLEAR_CUDA(launch(kernel, dim3(ctas, desc->groups), dim3(s.teams * s.warps * 32), 0, st, a));
     CLEAR_CUDA(launch(k_clear_norm_columns, dim3((desc->d + 31) / 32, d_dscale ? 2 : 1), dim3(256), 0, st, (const float*)a.part, d_dgamma, d_dscale, ctas, desc->d));
     return FESC_OK;
 }
