@@ -509,6 +509,8 @@ int fesc_scan_contract(fesc_ctx* ctx, const uint64_t* d_x, const uint64_t* d_a, 
  */
 enum { FESC_BF16 = 0, FESC_F16 = 1, FESC_F32 = 2 };
 const char* fesc_clear_last_error(void);
+/* Wait for `stream`; FESC_ETIMEOUT if a kernel's bounded wait gave up since the last such call on this device (its results are worth nothing). */
+int fesc_clear_sync(void* stream);
 
 /*
  * Gated linear recurrence (Sec. 5.4, Eqs. fesc_recurrence / fesc_contract; g = log a), per sequence and head, h in R^{P x N}:
@@ -521,7 +523,7 @@ const char* fesc_clear_last_error(void);
  * A log decay of -inf (any below -300) drops the state.  N <= 128, P <= 4096, L < 2^30, batch <= 65535.
  * Tokens of a chunk of 64 are multiplied with zeros among themselves: an infinity or NaN in a token reaches the other tokens of its chunk, and
  * everything after it.
- * Workspace: fesc_clear_scan_work(desc) bytes, 16-byte aligned (0: none needed).
+ * Workspace: fesc_clear_scan_work(desc) bytes, aligned to 256 (0: none needed).
  */
 typedef struct fesc_clear_scan_desc {
     uint32_t batch, L, H, P, G, N;
@@ -536,7 +538,8 @@ int fesc_clear_scan(const fesc_clear_scan_desc* desc, const void* d_x, const flo
 /*
  * Its gradients, from dy [batch][L][H][P] and the gradient of h_out (d_dh_out, or NULL: 0).  The inputs are those of the forward call; nothing of it is
  * kept.  d_dx, d_dg, d_dB, d_dC like x, g, B, C (dB, dC summed over the heads of a group; rows behind a sequence's end left as they are);
- * d_dskip [H] or NULL, summed over all sequences; d_dh0 [batch][H][P][N] or NULL.  Workspace: fesc_clear_scan_backward_work(desc) bytes.
+ * d_dskip [H] or NULL, summed over all sequences; d_dh0 [batch][H][P][N] or NULL.  Workspace: fesc_clear_scan_backward_work(desc) bytes,
+ * aligned to 256.
  */
 size_t fesc_clear_scan_backward_work(const fesc_clear_scan_desc* desc);
 int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const void* d_x, const float* d_g, const void* d_B, const void* d_C, const float* d_skip,

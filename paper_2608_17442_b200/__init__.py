@@ -116,6 +116,7 @@ def lib():
             "fesc_clear_scan": [c.POINTER(ClearScanDesc)] + [vp] * 10 + [sz, vp],
             "fesc_clear_scan_backward": [c.POINTER(ClearScanDesc)] + [vp] * 16 + [sz, vp],
             "fesc_clear_scan_step": [c.POINTER(ClearScanDesc)] + [vp] * 9,
+            "fesc_clear_sync": [vp],
             "fesc_clear_norm": [c.POINTER(ClearNormDesc)] + [vp] * 8,
             "fesc_clear_norm_backward": [c.POINTER(ClearNormDesc)] + [vp] * 13 + [sz, vp],
             "fesc_debug_bounds_register": [vp, sz],
@@ -491,6 +492,13 @@ def clear_scan(x, g, B, C, y, skip=None, h0=None, h_out=None, lengths=None, work
     last = c.ptr("h_out", h_out, (d.batch, d.H, d.P, d.N), torch.float32, True)
     w, n, keep = c.work(work, lib().fesc_clear_scan_work(d))
     c.go(lib().fesc_clear_scan, d, *a, out, last, w, n)
+
+
+def clear_sync():
+    """Wait for the current stream; raises FescError(ETIMEOUT) after a kernel's bounded wait gave up."""
+    rc = lib().fesc_clear_sync(_stream())
+    if rc != OK:
+        raise FescError(rc, lib().fesc_clear_last_error().decode())
 
 
 def clear_scan_backward(x, g, B, C, dy, dx, dg, dB, dC, skip=None, dskip=None, h0=None, dh_out=None, dh0=None, lengths=None, work=None):

@@ -59,6 +59,7 @@ struct FinishArgs {
     const int* lengths;
     long long Bb, Bt, Bg, Cb, Ct, Cg, gb, gt, gh, ib, it, ih;
     uint32_t b, L, H, G, N, NP, tiles, segments, seg_chunks, sum_blocks, dg_blocks;
+    uint32_t dots;                 // parts of row and col per head
 };
 // What is left of the backward pass, by block: sums of dB and dC over the heads of a group; the gradient of the log decays; that of the skip.
 template <class T>
@@ -97,8 +98,8 @@ __global__ void __launch_bounds__(256) k_clear_scan_finish(const FinishArgs a) {
         const int length = a.lengths ? min(max(a.lengths[b], 0), (int)a.L) : (int)a.L;
         const int lo = (int)(seg * a.seg_chunks) * SCAN_Q, hi = min(length, lo + (int)a.seg_chunks * SCAN_Q);
         if (lo >= hi) return;
-        const float* row = a.row + ((size_t)b * vheads + head * a.tiles) * a.L;
-        const float* col = a.col + ((size_t)b * vheads + head * a.tiles) * a.L;
+        const float* row = a.row + ((size_t)b * a.H + head) * a.dots * a.L;
+        const float* col = a.col + ((size_t)b * a.H + head) * a.dots * a.L;
         float* dg = a.dg + b * a.gb + head * a.gh;
         const float* g = a.g + b * a.ib + head * a.ih;
         if (!DBG_REGION(dg + lo * a.gt, ((long long)(hi - 1 - lo) * a.gt + 1) * sizeof(float))) return;
@@ -108,7 +109,7 @@ __global__ void __launch_bounds__(256) k_clear_scan_finish(const FinishArgs a) {
             const int t = top - (int)lane;
             double v = 0.0;
             if (t >= lo)
-                for (uint32_t s = 0; s < a.tiles; s++) v += (double)row[(size_t)s * a.L + t] - (double)col[(size_t)s * a.L + t];
+                for (uint32_t s = 0; s < a.dots; s++) v += (double)row[(size_t)s * a.L + t] - (double)col[(size_t)s * a.L + t];
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const double u = __shfl_up_sync(~0u, v, o);
@@ -204,26 +205,30 @@ __global__ void __launch_bounds__(256) k_clear_scan_step(const StepArgs a) {
 // ---------------------------------------------------------------------------------------
 struct ScanShape {
     uint32_t tiles, vheads, segments, seg_chunks, np;
+    bool tc;                   // the sweeps run on tcgen05 if the operands' alignment allows
     size_t states, state_floats, decay_floats, part_floats, dot_floats, end_floats;
 };
 
-// Segments: as many as fill the SMs with three CTAs each, none shorter than two chunks (a segment adds a pass over its keys and values, and a state
-// written and read).
+// Segments: as many as fill the SMs, with three CTAs each on mma.sync (none shorter than two chunks of 64: a segment adds a pass over its keys and
+// values, and a state written and read) or one on tcgen05 (chunks of 128).
 static ScanShape scan_shape(const fesc_clear_scan_desc* d) {
     ScanShape s;
+    s.tc = d->type == FESC_BF16 && d->N > 64;
     s.tiles = (d->P + SCAN_TILE - 1) / SCAN_TILE, s.vheads = d->H * s.tiles, s.np = d->N > 64 ? 128 : 64;
-    const uint64_t chunks = (d->L + SCAN_Q - 1) / SCAN_Q, ctas = (uint64_t)d->batch * s.vheads;
-    uint64_t want = ctas ? (3 * 148 + ctas - 1) / ctas : 1;
-    if (want > (chunks + 1) / 2) want = (chunks + 1) / 2;
+    // in pieces of 128 tokens
+    const uint64_t pieces = ((uint64_t)d->L + 127) / 128, ctas = (uint64_t)d->batch * s.vheads;
+    uint64_t want = !ctas ? 1 : s.tc ? 148 / ctas : (3 * 148 + ctas - 1) / ctas;
+    if (want > pieces) want = pieces;
     if (want < 1) want = 1;
-    s.seg_chunks = chunks ? (uint32_t)((chunks + want - 1) / want) : 1;
-    s.segments = chunks ? (uint32_t)((chunks + s.seg_chunks - 1) / s.seg_chunks) : 1;
+    const uint64_t each = pieces ? (pieces + want - 1) / want : 1;
+    s.seg_chunks = (uint32_t)(each * (128 / SCAN_Q));
+    s.segments = pieces ? (uint32_t)((pieces + each - 1) / each) : 1;
     s.states = (size_t)d->H * d->P * d->N;
     auto whole = [](size_t floats) { return (floats + 63) / 64 * 64; };      // parts of the workspace start on 256 bytes
     s.state_floats = s.segments > 1 ? whole((size_t)d->batch * s.segments * s.states) : 0;
     s.decay_floats = s.segments > 1 ? whole((size_t)d->batch * s.segments * d->H) : 0;
     s.part_floats = whole((size_t)d->batch * s.vheads * d->L * s.np);
-    s.dot_floats = whole((size_t)d->batch * s.vheads * d->L);
+    s.dot_floats = whole((size_t)d->batch * s.vheads * (s.tc ? 2 : 1) * d->L);
     s.end_floats = whole((size_t)d->batch * s.segments * s.vheads);
     return s;
 }
@@ -263,6 +268,10 @@ static ScanOperand operand(const void* p, const int64_t (&s)[3], bool tiled, uin
     o.wide = ((size_t)p & 15) == 0 && s[0] * bytes % 16 == 0 && s[1] * bytes % 16 == 0 && s[2] * bytes % 16 == 0;
     return o;
 }
+static uint32_t out_width(const void* p, const int64_t (&s)[3], uint32_t bytes) {
+    auto fits = [&](int64_t to) { return (int64_t)((size_t)p % to) == 0 && s[0] * bytes % to == 0 && s[1] * bytes % to == 0 && s[2] * bytes % to == 0; };
+    return fits(32) ? 2 : fits(16) ? 1 : 0;
+}
 static ScanArgs scan_args(const fesc_clear_scan_desc* d, const ScanShape& s, const float* g, const int* lengths) {
     ScanArgs a = {};
     a.g = g, a.gb = d->g[0], a.gt = d->g[1], a.gh = d->g[2], a.lengths = lengths;
@@ -270,8 +279,9 @@ static ScanArgs scan_args(const fesc_clear_scan_desc* d, const ScanShape& s, con
     a.tiles = s.tiles, a.segments = s.segments, a.seg_chunks = s.seg_chunks;
     return a;
 }
-static cudaError_t scan_go(const fesc_clear_scan_desc* d, const ScanArgs& a, int mode, cudaStream_t st) {
-    return d->type == FESC_BF16 ? scan_launch<__nv_bfloat16>(a, mode, st)
+static cudaError_t scan_go(const fesc_clear_scan_desc* d, bool tc, const ScanArgs& a, int mode, cudaStream_t st) {
+    return tc                    ? scan_tc_launch(a, mode, st)
+         : d->type == FESC_BF16 ? scan_launch<__nv_bfloat16>(a, mode, st)
          : d->type == FESC_F16  ? scan_launch<__half>(a, mode, st)
                                 : scan_launch<float>(a, mode, st);
 }
@@ -305,24 +315,25 @@ extern "C" int fesc_clear_scan(const fesc_clear_scan_desc* desc, const void* d_x
         return clear_fail(FESC_EINVAL, "clear_scan: an output is an input");
     const ScanShape s = scan_shape(desc);
     const size_t need = fesc_clear_scan_work(desc);
-    if (need && (!d_work || ((size_t)d_work & 15) || work_bytes < need))
-        return clear_fail(FESC_EINVAL, "clear_scan: the workspace is too small or not aligned to 16 bytes");
+    if (need && (!d_work || ((size_t)d_work & 255) || work_bytes < need))
+        return clear_fail(FESC_EINVAL, "clear_scan: the workspace is too small or not aligned to 256 bytes");
     cudaStream_t st = (cudaStream_t)stream;
     const uint32_t bytes = clear_type_bytes(d.type);
     ScanArgs a = scan_args(desc, s, d_g, d_lengths);
     a.q = operand(d_C, d.C, false, bytes), a.k = operand(d_B, d.B, false, bytes), a.v = operand(d_x, d.x, true, bytes);
+    const bool tc = s.tc && a.q.wide && a.k.wide && a.v.wide;
     a.init = d_h0;
     if (s.segments > 1) {
         float* states = (float*)d_work;
         float* decay = states + s.state_floats;
         a.last = states, a.decay = decay;
-        CLEAR_CUDA(scan_go(desc, a, MODE_STATE, st));
+        CLEAR_CUDA(scan_go(desc, tc, a, MODE_STATE, st));
         CLEAR_CUDA(combine(desc, s, states, decay, d_h0, false, st));
         a.init = states;
     }
     a.last = d_h_out, a.skip = d_skip, a.out = d_y, a.ob = d.y[0], a.ot = d.y[1], a.oh = d.y[2];
-    a.out_wide = operand(d_y, d.y, true, bytes).wide;
-    CLEAR_CUDA(scan_go(desc, a, MODE_OUT, st));
+    a.out_wide = out_width(d_y, d.y, bytes);
+    CLEAR_CUDA(scan_go(desc, tc, a, MODE_OUT, st));
     return FESC_OK;
 }
 
@@ -354,8 +365,8 @@ extern "C" int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const 
     }
     const ScanShape s = scan_shape(desc);
     const size_t need = fesc_clear_scan_backward_work(desc);
-    if (!d_work || ((size_t)d_work & 15) || work_bytes < need)
-        return clear_fail(FESC_EINVAL, "clear_scan_backward: the workspace is too small or not aligned to 16 bytes");
+    if (!d_work || ((size_t)d_work & 255) || work_bytes < need)
+        return clear_fail(FESC_EINVAL, "clear_scan_backward: the workspace is too small or not aligned to 256 bytes");
     float* w = (float*)d_work;
     auto take = [&](size_t floats) { float* p = w; w += floats; return p; };
     float *before = take(s.state_floats), *behind = take(s.state_floats), *decay = take(s.decay_floats), *decay_back = take(s.decay_floats);
@@ -364,33 +375,34 @@ extern "C" int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const 
     const uint32_t bytes = clear_type_bytes(d.type);
     const ScanOperand x = operand(d_x, d.x, true, bytes), B = operand(d_B, d.B, false, bytes), C = operand(d_C, d.C, false, bytes),
                       dy = operand(d_dy, d.y, true, bytes);
+    const bool tc = s.tc && x.wide && B.wide && C.wide && dy.wide;
     const ScanArgs base = scan_args(desc, s, d_g, d_lengths);
     const float *h = d_h0, *dh = d_dh_out;
     if (s.segments > 1) {
         ScanArgs a = base;
         a.k = B, a.v = x, a.last = before, a.decay = decay;
-        CLEAR_CUDA(scan_go(desc, a, MODE_STATE, st));
+        CLEAR_CUDA(scan_go(desc, tc, a, MODE_STATE, st));
         a.k = C, a.v = dy, a.last = behind, a.decay = decay_back, a.backwards = 1;
-        CLEAR_CUDA(scan_go(desc, a, MODE_STATE, st));
+        CLEAR_CUDA(scan_go(desc, tc, a, MODE_STATE, st));
         CLEAR_CUDA(combine(desc, s, before, decay, d_h0, false, st));
         CLEAR_CUDA(combine(desc, s, behind, decay_back, d_dh_out, true, st));
         h = before, dh = behind;
     }
     ScanArgs a = base;                  // dC
     a.q = dy, a.k = x, a.v = B, a.u = C, a.init = h, a.meet = dh, a.part = part_c, a.dots = row, a.ends = ends, a.diag = diag;
-    CLEAR_CUDA(scan_go(desc, a, MODE_GRAD, st));
+    CLEAR_CUDA(scan_go(desc, tc, a, MODE_GRAD, st));
     a = base;                           // dB
     a.q = x, a.k = dy, a.v = C, a.u = B, a.init = dh, a.part = part_b, a.dots = col, a.backwards = 1;
-    CLEAR_CUDA(scan_go(desc, a, MODE_GRAD, st));
+    CLEAR_CUDA(scan_go(desc, tc, a, MODE_GRAD, st));
     a = base;                           // dx, and the gradient of the state before the first token
     a.q = B, a.k = C, a.v = dy, a.init = dh, a.last = d_dh0, a.skip = d_skip, a.out = d_dx, a.ob = d.dx[0], a.ot = d.dx[1], a.oh = d.dx[2];
-    a.out_wide = operand(d_dx, d.dx, true, bytes).wide, a.backwards = 1;
-    CLEAR_CUDA(scan_go(desc, a, MODE_OUT, st));
+    a.out_wide = out_width(d_dx, d.dx, bytes), a.backwards = 1;
+    CLEAR_CUDA(scan_go(desc, tc, a, MODE_OUT, st));
     FinishArgs f = {};
     f.part_b = part_b, f.part_c = part_c, f.row = row, f.col = col, f.ends = ends, f.diag = diag;
     f.dB = d_dB, f.dC = d_dC, f.dg = d_dg, f.dskip = d_dskip, f.lengths = d_lengths, f.g = d_g, f.ib = d.g[0], f.it = d.g[1], f.ih = d.g[2];
     f.Bb = d.dB[0], f.Bt = d.dB[1], f.Bg = d.dB[2], f.Cb = d.dC[0], f.Ct = d.dC[1], f.Cg = d.dC[2], f.gb = d.dg[0], f.gt = d.dg[1], f.gh = d.dg[2];
-    f.b = d.batch, f.L = d.L, f.H = d.H, f.G = d.G, f.N = d.N, f.NP = s.np, f.tiles = s.tiles, f.segments = s.segments, f.seg_chunks = s.seg_chunks;
+    f.b = d.batch, f.L = d.L, f.H = d.H, f.G = d.G, f.N = d.N, f.NP = s.np, f.tiles = s.tiles, f.segments = s.segments, f.seg_chunks = s.seg_chunks, f.dots = s.tiles * (tc ? 2 : 1);
     f.sum_blocks = (uint32_t)(((size_t)d.batch * d.L * d.G * (s.np / 4) + 255) / 256);
     f.dg_blocks = (uint32_t)(((size_t)d.batch * d.H * s.segments + 7) / 8);
     const dim3 grid(f.sum_blocks + f.dg_blocks + (d.H + 7) / 8, 2);

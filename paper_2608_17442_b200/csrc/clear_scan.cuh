@@ -42,7 +42,7 @@ struct ScanArgs {
     const float* skip;               // MODE_OUT: out += skip[head] v
     void* out;                       // MODE_OUT
     long long ob, ot, oh;
-    uint32_t out_wide;
+    uint32_t out_wide;               // 16-byte accesses are possible (2: 32-byte ones)
     const float* init;               // state before the sweep (or before every segment): [b][H][P][N] (segments: [b][segment][H][P][N])
     float* last;                     // state behind the sweep (MODE_STATE: what a segment adds), or nullptr
     float* decay;                    // MODE_STATE: [b][segment][H], the decay over the segment
@@ -495,3 +495,5 @@ cudaError_t scan_launch(const ScanArgs& a, int mode, cudaStream_t st) {
 extern template cudaError_t scan_launch<__nv_bfloat16>(const ScanArgs&, int, cudaStream_t);
 extern template cudaError_t scan_launch<__half>(const ScanArgs&, int, cudaStream_t);
 extern template cudaError_t scan_launch<float>(const ScanArgs&, int, cudaStream_t);
+// the same on tcgen05: bfloat16, states of 65 to 128 columns, operands with 16-byte rows (clear_scan_tc.cu); dots then has two parts a head tile
+cudaError_t scan_tc_launch(const ScanArgs& a, int mode, cudaStream_t st);

@@ -18,7 +18,9 @@ CASES = [
     case(1, 128, 1, 128, 128, 1, "fp16"), case(3, 70, 2, 5, 3, 1, "bf16", True), case(1, 100, 2, 33, 127, 1, "bf16"), case(1, 192, 6, 64, 128, 2, "bf16", True),
     case(5, 150, 2, 64, 128, 1, "bf16", True, [150, 0, 1, 64, 97]), case(4, 90, 4, 40, 24, 2, "fp32", True, [0, 90, 65, 1]),
     case(3, 77, 2, 64, 64, 1, "fp16", False, [77, 0, 500]), case(1, 1500, 2, 64, 128, 1, "bf16", True), case(2, 700, 1, 70, 40, 1, "fp32", True, [700, 333]),
-    case(1, 40, 2, 200, 16, 1, "bf16"),
+    case(1, 40, 2, 200, 16, 1, "bf16"), case(1, 128, 1, 64, 128, 1, "bf16", True), case(3, 400, 50, 64, 128, 2, "bf16", True), case(1, 1000, 4, 72, 96, 2, "bf16", True),
+    case(5, 300, 30, 40, 72, 1, "bf16", True, [300, 129, 128, 1, 0]), case(1, 257, 2, 200, 128, 1, "bf16"), case(2, 640, 2, 8, 80, 1, "bf16", True, [600, 7]),
+    case(1, 900, 150, 16, 128, 1, "bf16", True), case(40, 130, 4, 64, 72, 4, "bf16"),
 ]
 IDS = ["-".join(str(v) for v in c.values()).replace(" ", "") for c in CASES]
 
@@ -49,6 +51,7 @@ def dead(s, L):
 
 
 def check_forward(s, c, y, h):
+    fesc.clear_sync()
     T = s["x"].dtype
     want, hw = scan(*(wide(s[k]) for k in ("x", "g", "B", "C", "skip", "h0")), s["lengths"])
     m = magnitudes(s)
@@ -63,6 +66,7 @@ def check_forward(s, c, y, h):
 
 
 def check_backward(s, c, o):
+    fesc.clear_sync()
     T = s["x"].dtype
     want, m = gradients(s), gradients(magnitudes(s))
     sums, cut = share(c)
@@ -114,7 +118,7 @@ def test_options_may_be_left_out():
 @pytest.mark.parametrize("kind", ["drop", "strong", "none", "mixed"])
 @pytest.mark.parametrize("t", ["bf16", "fp32"])
 def test_decays_of_zero_of_one_and_strong_ones(kind, t):
-    c = case(2, 150, 2, 40, 64, 1, t, True)
+    c = case(2, 150, 2, 40, 72, 1, t, True)
     s = make(c, 4)
     if kind == "drop":
         s["g"][:, 10::37] = -float("inf")
