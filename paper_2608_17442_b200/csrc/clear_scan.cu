@@ -228,7 +228,7 @@ static ScanShape scan_shape(const fesc_clear_scan_desc* d) {
     s.state_floats = s.segments > 1 ? whole((size_t)d->batch * s.segments * s.states) : 0;
     s.decay_floats = s.segments > 1 ? whole((size_t)d->batch * s.segments * d->H) : 0;
     s.part_floats = whole((size_t)d->batch * s.vheads * d->L * s.np);
-    s.dot_floats = whole((size_t)d->batch * s.vheads * (s.tc ? 2 : 1) * d->L);
+    s.dot_floats = whole((size_t)d->batch * s.vheads * (s.tc ? SCAN_DOTS : 1) * d->L);
     s.end_floats = whole((size_t)d->batch * s.segments * s.vheads);
     return s;
 }
@@ -402,7 +402,7 @@ extern "C" int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const 
     f.part_b = part_b, f.part_c = part_c, f.row = row, f.col = col, f.ends = ends, f.diag = diag;
     f.dB = d_dB, f.dC = d_dC, f.dg = d_dg, f.dskip = d_dskip, f.lengths = d_lengths, f.g = d_g, f.ib = d.g[0], f.it = d.g[1], f.ih = d.g[2];
     f.Bb = d.dB[0], f.Bt = d.dB[1], f.Bg = d.dB[2], f.Cb = d.dC[0], f.Ct = d.dC[1], f.Cg = d.dC[2], f.gb = d.dg[0], f.gt = d.dg[1], f.gh = d.dg[2];
-    f.b = d.batch, f.L = d.L, f.H = d.H, f.G = d.G, f.N = d.N, f.NP = s.np, f.tiles = s.tiles, f.segments = s.segments, f.seg_chunks = s.seg_chunks, f.dots = s.tiles * (tc ? 2 : 1);
+    f.b = d.batch, f.L = d.L, f.H = d.H, f.G = d.G, f.N = d.N, f.NP = s.np, f.tiles = s.tiles, f.segments = s.segments, f.seg_chunks = s.seg_chunks, f.dots = s.tiles * (tc ? SCAN_DOTS : 1);
     f.sum_blocks = (uint32_t)(((size_t)d.batch * d.L * d.G * (s.np / 4) + 255) / 256);
     f.dg_blocks = (uint32_t)(((size_t)d.batch * d.H * s.segments + 7) / 8);
     const dim3 grid(f.sum_blocks + f.dg_blocks + (d.H + 7) / 8, 2);

@@ -10,9 +10,11 @@
 // out = decay since the chunk's start * O1 + O2.  A tile of 128 tokens x 64 columns in shared memory (a panel, 16 KB, 128-byte swizzle) is the
 // K-major operand of one product and the MN-major operand of another, so nothing is stored twice or transposed.
 //
-// Eight warps compute (a thread owns a row and half of the columns), one issues the products, one sums up the log decays of the next chunk.  The
-// products of a chunk run while the threads are at something else: S and O1 while the faded values are formed, H while the scores are
-// decayed, O2 while the state is updated; the next chunk's S while the outputs are written.
+// Sixteen warps compute (a thread owns a row and a quarter of the columns), one issues the products, one sums up the log decays of the next chunks.
+// The products of a chunk run while the threads are at something else: O1 while the faded values are formed, H while the scores are decayed,
+// O2 while the state is updated; the next chunk's S while the outputs are written.  Reading operands from shared memory (128 bytes a cycle) is
+// what a product of these widths takes, so the planes of one right operand are multiplied side by side where tensor memory has room
+// (H 1150 -> 640 cycles a chunk, O1 770 -> 510) and the sums over planes are left to the threads.
 //
 // Decays of pairs in different blocks of 32 tokens are products of two factors not above one (from the earlier token to its block's end,
 // from there to the later one): one exponential per row and block; only the blocks on the diagonal take one per pair.
@@ -21,19 +23,20 @@
 
 #define TC_Q 128
 #define PANEL 16384u
-#define TC_THREADS 320          // 8 computing warps, one that issues, one for the decays
+#define TC_WARPS 16             // that compute; one more issues, one more sums decays
+#define TC_THREADS (32 * (TC_WARPS + 2))
 
 template <int MODE>
 struct TcLayout {
-    static constexpr int NO = MODE == MODE_GRAD ? 3 : 2;            // planes of scores and states
+    static constexpr bool GRAD = MODE == MODE_GRAD, OUT = MODE == MODE_OUT;
+    static constexpr int NO = GRAD ? 3 : 2;                        // planes of scores and states
     // panels in shared memory; k and v have two sets
-    static constexpr int q = 0, QP = MODE == MODE_STATE ? 0 : MODE == MODE_OUT ? 2 : 1;
-    static constexpr int broad = QP, narrow = broad + (MODE == MODE_STATE ? 2 : 4), w = narrow + (MODE == MODE_STATE ? 1 : 2), st = w + 3;
-    static constexpr int panels = st + (MODE == MODE_STATE ? 0 : NO);
-    // columns of tensor memory.  MODE_GRAD needs all 512: there the planes of the scores lie over the scores themselves
-    static constexpr uint32_t DV = MODE == MODE_GRAD ? 128 : 64;
-    static constexpr uint32_t S = MODE == MODE_GRAD ? 64 : 0, P = MODE == MODE_GRAD ? 0 : 128, O1 = MODE == MODE_GRAD ? 192 : 256, O2 = O1 + DV,
-                              H = MODE == MODE_STATE ? 0 : O2 + DV, columns = MODE == MODE_STATE ? 64 : 512;
+    static constexpr int q = 0, QP = OUT ? 2 : GRAD ? 1 : 0;
+    static constexpr int broad = QP, narrow = broad + 4, w = narrow + 2, st = w + 3, panels = st + (MODE ? NO : 0);
+    // columns of tensor memory, all 512 with outputs: the planes of the scores lie over the scores themselves
+    static constexpr uint32_t DV = GRAD ? 128 : 64, O1_PARTS = OUT ? 2 : 1, H_PARTS = GRAD ? 1 : 3;      // accumulators side by side, one per plane
+    static constexpr uint32_t P = 0, S = GRAD ? 64 : 0, O1 = GRAD ? 192 : 128, O2 = O1 + O1_PARTS * DV, H = MODE ? O2 + DV : 0, columns = MODE ? 512 : 256;
+    static_assert(H + 64 * H_PARTS <= columns, "accumulators fit");
     static constexpr size_t bytes = (size_t)panels * PANEL + 1024;  // panels start on 1024 bytes
 };
 
@@ -73,6 +76,13 @@ __device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint32_t b, ui
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+__device__ __forceinline__ void tc_ld16(uint32_t (&r)[16], uint32_t addr) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                   "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(addr)
+                 : "memory");
+}
 __device__ __forceinline__ void tc_ld32(uint32_t (&r)[32], uint32_t addr) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, "
@@ -83,10 +93,9 @@ __device__ __forceinline__ void tc_ld32(uint32_t (&r)[32], uint32_t addr) {
         : "r"(addr)
         : "memory");
 }
-__device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t (&r)[16]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr), "r"(r[0]),
-                 "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]),
-                 "r"(r[14]), "r"(r[15])
+__device__ __forceinline__ void tc_st8(uint32_t addr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]),
+                 "r"(r[5]), "r"(r[6]), "r"(r[7])
                  : "memory");
 }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -94,6 +103,41 @@ __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sy
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void bar_sync(uint32_t id, uint32_t threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+// two at a time
+struct f2 {
+    float x, y;
+};
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+    f2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+    f2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+    f2 d;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ f2 both(uint32_t bf16x2) { return {__uint_as_float(bf16x2 << 16), __uint_as_float(bf16x2 & 0xFFFF0000u)}; }
+// v as a sum of NM pairs of bfloat16 numbers
+template <int NM>
+__device__ __forceinline__ void split2(f2 v, uint32_t (&p)[NM]) {
+#pragma unroll
+    for (int i = 0; i < NM; i++) {
+        p[i] = pack_bf16(v.x, v.y);
+        if (i + 1 < NM) {
+            const f2 t = both(p[i]);
+            v = add2(v, {-t.x, -t.y});
+        }
+    }
+}
 __device__ __forceinline__ void cp_async16_part(uint32_t dst, const void* src, uint32_t bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
@@ -113,7 +157,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
     __shared__ __align__(8) u64 bars[12];
     __shared__ uint32_t tmem_base;
     __shared__ volatile uint32_t dead;          // a wait gave up: the rest of the chunks goes through without waiting, with nothing of worth in it
-    __shared__ float words[2][8];
+    __shared__ float words[2][TC_WARPS];
     pdl_begin();
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t vheads = a.H * a.tiles, vh = blockIdx.x % vheads, seg = blockIdx.x / vheads % a.segments, b = blockIdx.x / vheads / a.segments;
@@ -143,7 +187,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
         if (MODE == MODE_GRAD)
             ok = ok && DBG_REGION(scan_row<T>(a.u, b, t_lo, head, group, tile), (n * a.u.st + a.N) * sizeof(T)) &&
                  DBG_REGION(a.part + (((size_t)b * vheads + vh) * a.L + t_lo) * 128, (n + 1) * 128 * sizeof(float)) &&
-                 DBG_REGION(a.dots + ((size_t)b * vheads + vh) * 2 * a.L, 2 * (size_t)a.L * sizeof(float));
+                 DBG_REGION(a.dots + ((size_t)b * vheads + vh) * SCAN_DOTS * a.L, SCAN_DOTS * (size_t)a.L * sizeof(float));
         if (!ok) return;
     }
     if ((MODE && a.init && !DBG_REGION(a.init + (a.segments > 1 ? slot : b) * states + state_at, (size_t)pw * a.N * 4)) ||
@@ -153,18 +197,18 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
 #endif
     const uint32_t base = ((uint32_t)__cvta_generic_to_shared(tc_smem) + 1023) & ~1023u, bar = (uint32_t)__cvta_generic_to_shared(bars);
     uint8_t* const panels = tc_smem + (base - (uint32_t)__cvta_generic_to_shared(tc_smem));
-    const uint32_t b_load = bar, b_wv = bar + 8, b_p = bar + 16, b_epi = bar + 24, b_so = bar + 32, b_h = bar + 40, b_o = bar + 48, drained = bar + 56;
+    const uint32_t b_load = bar, b_wv = bar + 8, b_p = bar + 16, b_epi = bar + 24, b_s = bar + 32, b_h = bar + 40, b_o = bar + 48, drained = bar + 56;
     // of the two sets of decays: filled, and used; a set has barriers of its own because the warp that fills them runs up to two chunks ahead
     const uint32_t b_g = bar + 64, b_used = bar + 80;
-    if (warp == 8) {
+    if (warp == TC_WARPS) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"((uint32_t)__cvta_generic_to_shared(&tmem_base)), "n"(Lay::columns)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     if (tid == 0) {
-        mbar_init(b_load, 8), mbar_init(b_wv, 8), mbar_init(b_p, 8), mbar_init(b_epi, 8);
-        for (uint32_t i = 0; i < 2; i++) mbar_init(b_g + 8 * i, 1), mbar_init(b_used + 8 * i, 8);
-        mbar_init(b_so, 1), mbar_init(b_h, 1), mbar_init(b_o, 1), mbar_init(drained, 1);
+        mbar_init(b_load, TC_WARPS), mbar_init(b_wv, TC_WARPS), mbar_init(b_p, TC_WARPS), mbar_init(b_epi, TC_WARPS);
+        for (uint32_t i = 0; i < 2; i++) mbar_init(b_g + 8 * i, 1), mbar_init(b_used + 8 * i, TC_WARPS);
+        mbar_init(b_s, 1), mbar_init(b_h, 1), mbar_init(b_o, 1), mbar_init(drained, 1);
         dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -177,46 +221,44 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
         if (!dead && mbar_wait_bounded(which, parity & 1)) dead = 1, g_clear_status = 1;
     };
 
-    if (warp == 8) {
+    if (warp == TC_WARPS) {
         // issues the products
         constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 24);        // bfloat16 x bfloat16 -> float32, 128 rows
-        constexpr uint32_t I_S = IDESC | (16u << 17), I_H = IDESC | (1u << 15) | (1u << 16) | (8u << 17);
-        constexpr uint32_t I_O1 = IDESC | (MODE == MODE_GRAD ? 16u << 17 : (8u << 17) | (1u << 16)), I_O2 = IDESC | (1u << 16) | ((Lay::DV / 8) << 17);
+        constexpr uint32_t I_S = IDESC | (16u << 17), I_H = IDESC | (1u << 15) | (1u << 16) | ((8u * Lay::H_PARTS) << 17);
+        constexpr uint32_t I_O1 = IDESC | (16u << 17) | (Lay::GRAD ? 0 : 1u << 16), I_O2 = IDESC | (1u << 16) | ((Lay::DV / 8) << 17);
+        constexpr uint32_t STEP = PANEL >> 4, QK = Lay::OUT ? 8 : 4;                        // steps of 16 along q's columns
         if (lane == 0) {
             const uint32_t pq = tc_desc(base + Lay::q * PANEL), pw_ = tc_desc(base + Lay::w * PANEL), ps = tc_desc(base + Lay::st * PANEL);
-            constexpr uint32_t STEP = PANEL >> 4;
             for (int c = 0; c < chunks; c++) {
-                const uint32_t set = MODE == MODE_STATE ? 0 : c & 1;
+                const uint32_t set = c & 1;
                 const uint32_t pb = tc_desc(base + (Lay::broad + 2 * set) * PANEL), pn = tc_desc(base + (Lay::narrow + set) * PANEL);
                 if (MODE) {
                     wait(b_load, c);
-                    if (MODE == MODE_GRAD && c) wait(b_o, c - 1);        // the scores' planes lie over the scores
+                    if (c) wait(b_o, c - 1);                             // the scores' planes lie over the scores
                     tc_after();
                     if (!dead) {
 #pragma unroll
-                        for (uint32_t k = 0; k < (MODE == MODE_OUT ? 8 : 4); k++) {
+                        for (uint32_t k = 0; k < QK; k++) {
                             const uint32_t at = (k >> 2) * STEP + (k & 3) * 2;
-                            tc_mma_ss(tmem + Lay::S, pq + at, (MODE == MODE_OUT ? pb : pn) + at, I_S, k);
+                            tc_mma_ss(tmem + Lay::S, pq + at, (Lay::OUT ? pb : pn) + at, I_S, k);
                         }
                     }
                     if (c) wait(b_epi, c - 1);
                     tc_after();
                     if (!dead) {
 #pragma unroll
-                        for (uint32_t p = 0; p < NO; p++)
+                        for (uint32_t p = 0; p < (Lay::OUT ? 1 : NO); p++)
 #pragma unroll
-                            for (uint32_t k = 0; k < (MODE == MODE_OUT ? 8 : 4); k++) {
-                                const uint32_t at = (k >> 2) * STEP + (k & 3) * 2;
-                                tc_mma_ss(tmem + Lay::O1, pq + at, ps + p * STEP + (MODE == MODE_OUT ? k * 128 : (k & 3) * 2), I_O1, p || k);
-                            }
-                        tc_commit(b_so);
+                            for (uint32_t k = 0; k < QK; k++)
+                                tc_mma_ss(tmem + Lay::O1, pq + (k >> 2) * STEP + (k & 3) * 2, ps + p * STEP + (Lay::OUT ? k * 128 : k * 2), I_O1, p || k);
+                        tc_commit(b_s);
                     }
                 }
                 wait(b_wv, c);
                 tc_after();
                 if (!dead) {
 #pragma unroll
-                    for (uint32_t p = 0; p < NS; p++)
+                    for (uint32_t p = 0; p < (Lay::H_PARTS == 1 ? NS : 1); p++)
 #pragma unroll
                         for (uint32_t k = 0; k < 8; k++) tc_mma_ss(tmem + Lay::H, pb + k * 128, pw_ + p * STEP + k * 128, I_H, p || k);
                     tc_commit(b_h);
@@ -229,7 +271,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
                         for (uint32_t p = 0; p < NO; p++)
 #pragma unroll
                             for (uint32_t k = 0; k < 8; k++)
-                                tc_mma_ts(tmem + Lay::O2, tmem + Lay::P + 64 * p + 8 * k, (MODE == MODE_GRAD ? pb : pn) + k * 128, I_O2, p || k);
+                                tc_mma_ts(tmem + Lay::O2, tmem + Lay::P + 64 * p + 8 * k, (Lay::GRAD ? pb : pn) + k * 128, I_O2, p || k);
                         tc_commit(b_o);
                     }
                 }
@@ -238,21 +280,25 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
             mbar_wait_bounded(drained, 0);
         }
         __syncwarp();
-    } else if (warp == 9) {
+    } else if (warp == TC_WARPS + 1) {
         // log decays of a chunk, four tokens a lane
         const float* g = a.g + b * a.gb + head * a.gh;
         double through = 0.0;
-        for (int c = 0; c < chunks; c++) {
+        float gv[4];
+        auto read = [&](int c) {
             const int valid = min(TC_Q, t_hi - t_lo - c * TC_Q), t0 = a.backwards ? t_hi - 1 - c * TC_Q : t_lo + c * TC_Q;
-            float gv[4];
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 const int pos = 4 * lane + i, t = t0 + dir * pos + (a.backwards ? 1 : 0);
                 gv[i] = pos < valid && t < length ? g[t * a.gt] : 0.f;
             }
+        };
+        if (chunks) read(0);
+        for (int c = 0; c < chunks; c++) {
             double sum[4];
 #pragma unroll
             for (int i = 0; i < 4; i++) sum[i] = (double)(gv[i] < SCAN_DROP ? SCAN_DROP : gv[i]) * 1.4426950408889634 + (i ? sum[i - 1] : 0.0);
+            if (c + 1 < chunks) read(c + 1);
             double run = sum[3];
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -277,230 +323,223 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
         }
         if (MODE == MODE_STATE && lane == 0 && tile == 0) a.decay[slot * a.H + head] = (float)exp2(through);
     } else {
-        const uint32_t quarter = warp & 3, half = warp >> 2, row = 32 * quarter + lane;     // row: token of the chunk, or column of the state
-        const uint32_t lanes = tmem + (quarter << 21);
-        float st[32];                                                                        // state[channel 32 half + i][column row]
+        const uint32_t quarter = warp & 3, part = warp >> 2, row = 32 * quarter + lane;     // row: token of the chunk, or column of the state
+        const uint32_t lanes = tmem + (quarter << 21), at0 = panel_at(row, 2 * part), at1 = panel_at(row, 2 * part + 1);   // this thread's 16 of 64 columns
+        f2 st[8];                                                                            // state[channel 16 part + i][column row]
         const float* init = MODE && a.init ? a.init + (a.segments > 1 ? slot : b) * states + state_at : nullptr;
 #pragma unroll
-        for (int i = 0; i < 32; i++) {
-            const int p = 32 * half + i;
-            st[i] = init && p < pw && row < a.N ? init[(size_t)p * a.N + row] : 0.f;
+        for (int i = 0; i < 16; i++) {
+            const int p = 16 * part + i;
+            const float v = init && p < pw && row < a.N ? init[(size_t)p * a.N + row] : 0.f;
+            if (i & 1) st[i / 2].y = v;
+            else st[i / 2].x = v;
         }
+        auto put = [&](int first, const uint32_t (&pl)[8][3], int planes) {
+#pragma unroll
+            for (int p = 0; p < planes; p++) {
+                *reinterpret_cast<uint4*>(panels + (first + p) * PANEL + at0) = make_uint4(pl[0][p], pl[1][p], pl[2][p], pl[3][p]);
+                *reinterpret_cast<uint4*>(panels + (first + p) * PANEL + at1) = make_uint4(pl[4][p], pl[5][p], pl[6][p], pl[7][p]);
+            }
+        };
         auto put_state = [&]() {
+            uint32_t pl[8][3];
 #pragma unroll
-            for (int k = 0; k < 4; k++) {
-                uint32_t pl[4][NO];
+            for (int e = 0; e < 8; e++) {
+                uint32_t s[NO];
+                split2<NO>(st[e], s);
 #pragma unroll
-                for (int e = 0; e < 4; e++) split<NO>(st[8 * k + 2 * e], st[8 * k + 2 * e + 1], pl[e]);
-#pragma unroll
-                for (int p = 0; p < NO; p++)
-                    *reinterpret_cast<uint4*>(panels + (Lay::st + p) * PANEL + panel_at(row, 4 * half + k)) = make_uint4(pl[0][p], pl[1][p], pl[2][p], pl[3][p]);
+                for (int p = 0; p < NO; p++) pl[e][p] = s[p];
             }
+            put(Lay::st, pl, NO);
         };
-        // `n` panels of an operand's rows for chunk c: a thread copies chunks of 16 bytes, eight threads a row of 128
-        auto fetch = [&](const ScanOperand& o, int width, int first, int n, int c) {
-            const int valid = min(TC_Q, t_hi - t_lo - c * TC_Q), t0 = a.backwards ? t_hi - 1 - c * TC_Q : t_lo + c * TC_Q;
-            const T* src = scan_row<T>(o, b, t0, head, group, tile);
-            const long long step = dir * o.st;
+        // Panels of an operand's rows for a chunk: a thread copies two chunks of 16 bytes a panel, eight threads a row of 128 bytes.  What does not
+        // change from chunk to chunk: the place in the panel, the bytes that exist, the row to start from.
+        const int r0 = (int)(tid >> 3), col = (int)(tid & 7) * 8;
+        const uint32_t to = base + panel_at(r0, tid & 7);
+        const int t_first = a.backwards ? t_hi - 1 : t_lo;
+        struct Rows {
+            const T* p;
+            long long step;      // 64 rows on
+            int width;
+        };
+        auto rows = [&](const ScanOperand& o, int width) {
+            return Rows{chunks ? scan_row<T>(o, b, t_first + dir * r0, head, group, tile) + col : nullptr, (long long)dir * 64 * o.st, width - col};
+        };
+        auto fetch = [&](Rows& r, uint32_t panel, int n, int valid) {
 #pragma unroll
-            for (int i = 0; i < n * 4; i++) {
-                const int r = (int)(tid >> 3) + 32 * (i & 3), col = (int)(tid & 7) * 8 + 64 * (i >> 2), left = r < valid ? min(width - col, 8) : 0;
-                cp_async16_part(base + (first + (i >> 2)) * PANEL + panel_at(r, tid & 7), left > 0 ? src + r * step + col : src, left > 0 ? left * 2 : 0);
+            for (int j = 0; j < n; j++) {
+                const int bytes = min(max(r.width - 64 * j, 0), 8) * 2;
+                const uint32_t dst = to + (panel + j) * PANEL;
+                if (valid == TC_Q && bytes == 16) {
+                    cp_async16(dst, r.p + 64 * j), cp_async16(dst + 8192, r.p + r.step + 64 * j);
+                } else {
+                    // a row that does not exist is not read: zero bytes of an address that does
+                    const int n0 = r0 < valid ? bytes : 0, n1 = r0 + 64 < valid ? bytes : 0;
+                    cp_async16_part(dst, n0 ? r.p + 64 * j : (const T*)a.g, n0), cp_async16_part(dst + 8192, n1 ? r.p + r.step + 64 * j : (const T*)a.g, n1);
+                }
             }
+            r.p += 2 * r.step;
         };
+        auto left = [&](int c) { return min(TC_Q, t_hi - t_lo - c * TC_Q); };
+        Rows fb = rows(ob, (int)a.N), fn = rows(on, pw), fq = MODE ? rows(a.q, qw) : Rows{nullptr, 0, 0};
         auto arrive = [&](uint32_t which) {
             __syncwarp();
             if (lane == 0) mbar_arrive(which);
         };
         float diag = 0.f;
         if (chunks) {
-            if (MODE) fetch(a.q, qw, Lay::q, Lay::QP, 0);
-            fetch(ob, (int)a.N, Lay::broad, 2, 0);
-            fetch(on, pw, Lay::narrow, 1, 0);
-            if (MODE) {
-                put_state();
-                if (MODE == MODE_OUT) {
-                    // blocks above the diagonal are zero for good
-                    uint32_t zero[16] = {};
-                    for (uint32_t J = quarter + 1; J < 4; J++)
-                        if ((J & 1) == half)
-                            for (int p = 0; p < NO; p++) tc_st16(lanes + Lay::P + 64 * p + 16 * J, zero);
-                    tc_wait_st();
-                }
-            }
+            if (MODE) fetch(fq, Lay::q, Lay::QP, left(0));
+            fetch(fb, Lay::broad, 2, left(0));
+            fetch(fn, Lay::narrow, 1, left(0));
+            if (MODE) put_state();
             cp_async_wait();
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            tc_before();
             if (MODE) arrive(b_load);
         }
         for (int c = 0; c < chunks; c++) {
-            const int valid = min(TC_Q, t_hi - t_lo - c * TC_Q), t0 = a.backwards ? t_hi - 1 - c * TC_Q : t_lo + c * TC_Q;
-            const int set = MODE == MODE_STATE ? 0 : c & 1, nset = MODE == MODE_STATE ? 0 : set ^ 1;
-            const TcDecays& d = decays[c & 1];
-            bar_sync(1, 256);                    // everyone's copies have landed, everyone is done with the chunk before
-            if (MODE && c + 1 < chunks) {
-                fetch(ob, (int)a.N, Lay::broad + 2 * nset, 2, c + 1);
-                fetch(on, pw, Lay::narrow + nset, 1, c + 1);
+            const int valid = left(c), set = c & 1;
+            const TcDecays& d = decays[set];
+            bar_sync(1, 32 * TC_WARPS);          // everyone's copies have landed, everyone is done with the chunk before
+            if (c + 1 < chunks) {
+                fetch(fb, Lay::broad + 2 * (set ^ 1), 2, left(c + 1));
+                fetch(fn, Lay::narrow + (set ^ 1), 1, left(c + 1));
             }
-            wait(b_g + 8 * (c & 1), c >> 1);
+            wait(b_g + 8 * set, c >> 1);
             {
                 const float f = d.fade[row];
                 const uint8_t* src = panels + (Lay::narrow + set) * PANEL;
+                const uint4 v0 = *reinterpret_cast<const uint4*>(src + at0), v1 = *reinterpret_cast<const uint4*>(src + at1);
+                const uint32_t u[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+                uint32_t pl[8][3];
 #pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(src + panel_at(row, 4 * half + k));
-                    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-                    uint32_t pl[4][NS];
-#pragma unroll
-                    for (int e = 0; e < 4; e++) split<NS>(__uint_as_float(u[e] << 16) * f, __uint_as_float(u[e] & 0xFFFF0000u) * f, pl[e]);
-#pragma unroll
-                    for (int p = 0; p < NS; p++)
-                        *reinterpret_cast<uint4*>(panels + (Lay::w + p) * PANEL + panel_at(row, 4 * half + k)) = make_uint4(pl[0][p], pl[1][p], pl[2][p], pl[3][p]);
-                }
+                for (int e = 0; e < 8; e++) split2<NS>(mul2(both(u[e]), {f, f}), pl[e]);
+                put(Lay::w, pl, NS);
             }
             const float keep = d.keep;
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             arrive(b_wv);
             if (MODE) {
-                wait(b_so, c);
+                // decayed scores of this row and the columns 32 part .. 32 part + 31
+                wait(b_s, c);                       // S and O1
                 tc_after();
-                // decayed scores of this row, blocks half and half + 2 of 32 columns
-                const float2 ci = d.cum[row];
-                uint32_t x[2][32];
-#pragma unroll
-                for (int B = 0; B < 2; B++)
-                    if (2 * B + half <= quarter) tc_ld32(x[B], lanes + Lay::S + 32 * (2 * B + half));
-                tc_wait_ld();
-                if (MODE == MODE_GRAD) {
-                    tc_before();
-                    bar_sync(2 + quarter, 64);      // the other warp of these rows has its scores too
-                    tc_after();
+                uint32_t x[32];
+                if (part <= quarter) {
+                    tc_ld32(x, lanes + Lay::S + 32 * part);
+                    tc_wait_ld();
                 }
+                tc_before();
+                bar_sync(2 + quarter, 128);         // the other warps of these rows have their scores too
+                tc_after();
+                if (c + 1 < chunks) fetch(fq, Lay::q, Lay::QP, left(c + 1));     // O1 is done, too
+                const float2 ci = d.cum[row];
+                const float2 ref = d.ref[part];
+                const float r = ex2((ci.x - ref.x) + (ci.y - ref.y));
 #pragma unroll
-                for (int B = 0; B < 2; B++) {
-                    const uint32_t J = 2 * B + half;
-                    uint32_t pl[NO][16];
-                    if (J > quarter) {
-                        if (MODE == MODE_OUT) continue;
+                for (int h = 0; h < 2; h++) {
+                    uint32_t pl[NO][8];
+                    if (part > quarter) {
 #pragma unroll
                         for (int p = 0; p < NO; p++)
 #pragma unroll
-                            for (int e = 0; e < 16; e++) pl[p][e] = 0;
-                    } else if (J < quarter) {
-                        const float2 ref = d.ref[J];
-                        const float r = ex2((ci.x - ref.x) + (ci.y - ref.y));
-#pragma unroll
-                        for (int e = 0; e < 16; e++) {
-                            const float2 t = *reinterpret_cast<const float2*>(&d.tail[32 * J + 2 * e]);
-                            uint32_t q[NO];
-                            split<NO>(__uint_as_float(x[B][2 * e]) * (r * t.x), __uint_as_float(x[B][2 * e + 1]) * (r * t.y), q);
-#pragma unroll
-                            for (int p = 0; p < NO; p++) pl[p][e] = q[p];
-                        }
+                            for (int e = 0; e < 8; e++) pl[p][e] = 0;
                     } else {
 #pragma unroll
-                        for (int e = 0; e < 16; e++) {
-                            const float4 cj = *reinterpret_cast<const float4*>(&d.cum[32 * J + 2 * e]);
-                            const float s0 = __uint_as_float(x[B][2 * e]), s1 = __uint_as_float(x[B][2 * e + 1]);
-                            const float g0 = ex2((ci.x - cj.x) + (ci.y - cj.y)), g1 = ex2((ci.x - cj.z) + (ci.y - cj.w));
-                            if (MODE == MODE_GRAD) diag += (lane == 2 * e ? s0 : 0.f) + (lane == 2 * e + 1 ? s1 : 0.f);
+                        for (int e = 0; e < 8; e++) {
+                            const int j = 16 * h + 2 * e;
+                            f2 v = {__uint_as_float(x[j]), __uint_as_float(x[j + 1])};
+                            if (part < quarter) {
+                                const float2 tl = *reinterpret_cast<const float2*>(&d.tail[32 * part + j]);
+                                v = mul2(v, mul2({r, r}, {tl.x, tl.y}));
+                            } else {
+                                const float4 cj = *reinterpret_cast<const float4*>(&d.cum[32 * part + j]);
+                                const f2 d0 = add2({ci.x, ci.y}, {-cj.x, -cj.y}), d1 = add2({ci.x, ci.y}, {-cj.z, -cj.w});
+                                if (Lay::GRAD) diag += (lane == j ? v.x : 0.f) + (lane == j + 1 ? v.y : 0.f);
+                                v = mul2(v, {ex2(d0.x + d0.y), ex2(d1.x + d1.y)});
+                                v.x = j <= lane ? v.x : 0.f, v.y = j + 1 <= lane ? v.y : 0.f;
+                            }
                             uint32_t q[NO];
-                            split<NO>(2 * e <= lane ? s0 * g0 : 0.f, 2 * e + 1 <= lane ? s1 * g1 : 0.f, q);
+                            split2<NO>(v, q);
 #pragma unroll
                             for (int p = 0; p < NO; p++) pl[p][e] = q[p];
                         }
                     }
 #pragma unroll
-                    for (int p = 0; p < NO; p++) tc_st16(lanes + Lay::P + 64 * p + 16 * J, pl[p]);
+                    for (int p = 0; p < NO; p++) tc_st8(lanes + Lay::P + 64 * p + 16 * part + 8 * h, pl[p]);
                 }
                 tc_wait_st();
                 tc_before();
                 arrive(b_p);
-                if (c + 1 < chunks) fetch(a.q, qw, Lay::q, Lay::QP, c + 1);
             }
             wait(b_h, c);
             tc_after();
             {
-                uint32_t x[32];
-                tc_ld32(x, lanes + Lay::H + 32 * half);
+                uint32_t x[Lay::H_PARTS][16];
+#pragma unroll
+                for (int p = 0; p < (int)Lay::H_PARTS; p++) tc_ld16(x[p], lanes + Lay::H + 64 * p + 16 * part);
                 tc_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 32; i++) st[i] = fmaf(st[i], keep, __uint_as_float(x[i]));
-            }
-            if (MODE == MODE_STATE) {
-                if (c + 1 < chunks) {
-                    fetch(ob, (int)a.N, Lay::broad, 2, c + 1);
-                    fetch(on, pw, Lay::narrow, 1, c + 1);
-                    cp_async_wait();
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                for (int e = 0; e < 8; e++) {
+                    auto pair = [&](int p) { return f2{__uint_as_float(x[p][2 * e]), __uint_as_float(x[p][2 * e + 1])}; };
+                    f2 v = pair(Lay::H_PARTS - 1);
+#pragma unroll
+                    for (int p = Lay::H_PARTS - 2; p >= 0; p--) v = add2(v, pair(p));
+                    st[e] = fma2(st[e], {keep, keep}, v);
                 }
-                tc_before();
-                arrive(b_used + 8 * (c & 1));
-                continue;
             }
-            if (c + 1 < chunks) put_state();
+            if (MODE && c + 1 < chunks) put_state();
             cp_async_wait();
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             tc_before();
-            if (c + 1 < chunks) arrive(b_load);
-
+            if (MODE && c + 1 < chunks) arrive(b_load);
             const float grow = d.grow[row];
-            arrive(b_used + 8 * (c & 1));
+            arrive(b_used + 8 * set);
+            if (!MODE) continue;
+
             const bool live = (int)row < valid;
-            const long long t = t0 + (long long)dir * (int)row;
-            if (MODE == MODE_OUT) {
-                uint32_t skipped[4][4] = {};
+            const long long t = t_first + (long long)dir * (c * TC_Q + (int)row);
+            if (Lay::OUT) {
+                uint32_t skipped[8] = {};
                 const float skip = a.skip ? a.skip[head] : 0.f;
                 if (a.skip) {
-#pragma unroll
-                    for (int k = 0; k < 4; k++) {
-                        const uint4 v = *reinterpret_cast<const uint4*>(panels + (Lay::narrow + set) * PANEL + panel_at(row, 4 * half + k));
-                        skipped[k][0] = v.x, skipped[k][1] = v.y, skipped[k][2] = v.z, skipped[k][3] = v.w;
-                    }
+                    const uint8_t* src = panels + (Lay::narrow + set) * PANEL;
+                    const uint4 v0 = *reinterpret_cast<const uint4*>(src + at0), v1 = *reinterpret_cast<const uint4*>(src + at1);
+                    skipped[0] = v0.x, skipped[1] = v0.y, skipped[2] = v0.z, skipped[3] = v0.w, skipped[4] = v1.x, skipped[5] = v1.y, skipped[6] = v1.z, skipped[7] = v1.w;
                 }
                 wait(b_o, c);
                 tc_after();
-                uint32_t x[32], y[32];
-                tc_ld32(x, lanes + Lay::O1 + 32 * half);
-                tc_ld32(y, lanes + Lay::O2 + 32 * half);
+                uint32_t x[16], x1[16], y[16];
+                tc_ld16(x, lanes + Lay::O1 + 16 * part);
+                tc_ld16(x1, lanes + Lay::O1 + 64 + 16 * part);
+                tc_ld16(y, lanes + Lay::O2 + 16 * part);
                 tc_wait_ld();
                 tc_before();
                 arrive(b_epi);
-                T* out = (T*)a.out + b * a.ob + t * a.ot + head * a.oh + tile * SCAN_TILE + 32 * half;
-                const int count = live ? vw - 32 * (int)half : 0;
-                uint32_t o[16];
+                T* out = (T*)a.out + b * a.ob + t * a.ot + head * a.oh + tile * SCAN_TILE + 16 * part;
+                const int count = live ? vw - 16 * (int)part : 0;
+                uint32_t o[8];
 #pragma unroll
-                for (int e = 0; e < 16; e++) {
-                    const uint32_t s = skipped[e >> 2][e & 3];
-                    const float o0 = fmaf(grow, __uint_as_float(x[2 * e]), __uint_as_float(y[2 * e])) + skip * __uint_as_float(s << 16);
-                    const float o1 = fmaf(grow, __uint_as_float(x[2 * e + 1]), __uint_as_float(y[2 * e + 1])) + skip * __uint_as_float(s & 0xFFFF0000u);
-                    o[e] = pack_bf16(o0, o1);
+                for (int e = 0; e < 8; e++) {
+                    const f2 s = add2({__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])}, {__uint_as_float(x1[2 * e]), __uint_as_float(x1[2 * e + 1])});
+                    const f2 v = fma2({skip, skip}, both(skipped[e]), fma2({grow, grow}, s, {__uint_as_float(y[2 * e]), __uint_as_float(y[2 * e + 1])}));
+                    o[e] = pack_bf16(v.x, v.y);
                 }
-                if (a.out_wide > 1 && count >= 32) {
-                    st32(out, o), st32(out + 16, o + 8);
-                } else if (a.out_wide) {
-#pragma unroll
-                    for (int k = 0; k < 4; k++) {
-                        if (count >= 8 * k + 8) {
-                            *reinterpret_cast<uint4*>(out + 8 * k) = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
-                            continue;
-                        }
-#pragma unroll
-                        for (int e = 0; e < 8; e++)
-                            if (8 * k + e < count) reinterpret_cast<uint16_t*>(out)[8 * k + e] = (uint16_t)(o[4 * k + e / 2] >> (e & 1 ? 16 : 0));
-                    }
+                if (a.out_wide > 1 && count >= 16) {
+                    st32(out, o);
+                } else if (a.out_wide && count % 8 == 0) {
+                    if (count >= 8) *reinterpret_cast<uint4*>(out) = make_uint4(o[0], o[1], o[2], o[3]);
+                    if (count >= 16) *reinterpret_cast<uint4*>(out + 8) = make_uint4(o[4], o[5], o[6], o[7]);
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 32; e++)
+                    for (int e = 0; e < 16; e++)
                         if (e < count) reinterpret_cast<uint16_t*>(out)[e] = (uint16_t)(o[e / 2] >> (e & 1 ? 16 : 0));
                 }
             } else {
-                // u's half row is on its way while the products finish
-                uint32_t u[32];
-                const T* pu = scan_row<T>(a.u, b, t0 + dir * min((int)row, valid - 1), head, group, tile) + 64 * half;
+                // u's part of the row is on its way while the products finish
+                uint32_t u[16];
+                const T* pu = scan_row<T>(a.u, b, t_first + (long long)dir * (c * TC_Q + min((int)row, valid - 1)), head, group, tile) + 32 * part;
 #pragma unroll
-                for (int k = 0; k < 8; k++) {
-                    const int count = (int)a.N - 64 * (int)half - 8 * k;
+                for (int k = 0; k < 4; k++) {
+                    const int count = (int)a.N - 32 * (int)part - 8 * k;
                     uint4 v = make_uint4(0, 0, 0, 0);
                     if (a.u.wide && count >= 8) v = *reinterpret_cast<const uint4*>(pu + 8 * k);
                     else {
@@ -515,59 +554,56 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
                 }
                 wait(b_o, c);
                 tc_after();
-                float dot = 0.f;
-                float* part = a.part + (((size_t)b * vheads + vh) * a.L + t) * 128 + 64 * half;
+                f2 dot = {0.f, 0.f};
+                float* to_part = a.part + (((size_t)b * vheads + vh) * a.L + t) * 128 + 32 * part;
 #pragma unroll
                 for (int k = 0; k < 2; k++) {
-                    uint32_t x[32], y[32];
-                    tc_ld32(x, lanes + Lay::O1 + 64 * half + 32 * k);
-                    tc_ld32(y, lanes + Lay::O2 + 64 * half + 32 * k);
+                    uint32_t x[16], y[16];
+                    tc_ld16(x, lanes + Lay::O1 + 32 * part + 16 * k);
+                    tc_ld16(y, lanes + Lay::O2 + 32 * part + 16 * k);
                     tc_wait_ld();
                     if (k == 1) {
                         tc_before();
                         arrive(b_epi);
                     }
 #pragma unroll
-                    for (int e = 0; e < 32; e++) {
-                        const float v = fmaf(grow, __uint_as_float(x[e]), __uint_as_float(y[e]));
-                        const uint32_t w = u[16 * k + e / 2];
-                        dot = fmaf(v, __uint_as_float(e & 1 ? w & 0xFFFF0000u : w << 16), dot);
-                        x[e] = __float_as_uint(v);
+                    for (int e = 0; e < 8; e++) {
+                        const f2 v = fma2({grow, grow}, {__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])}, {__uint_as_float(y[2 * e]), __uint_as_float(y[2 * e + 1])});
+                        dot = fma2(v, both(u[8 * k + e]), dot);
+                        x[2 * e] = __float_as_uint(v.x), x[2 * e + 1] = __float_as_uint(v.y);
                     }
-                    if (live)
-#pragma unroll
-                        for (int e = 0; e < 4; e++) st32(part + 32 * k + 8 * e, x + 8 * e);
+                    if (live) st32(to_part + 16 * k, x), st32(to_part + 16 * k + 8, x + 8);
                 }
-                if (live) a.dots[(((size_t)b * vheads + vh) * 2 + half) * a.L + t] = dot;
+                if (live) a.dots[(((size_t)b * vheads + vh) * SCAN_DOTS + part) * a.L + t] = dot.x + dot.y;
             }
         }
         if (a.last && (MODE == MODE_STATE || is_last)) {
             float* last = a.last + (MODE == MODE_STATE ? slot : b) * states + state_at;
             const float f = MODE && a.backwards && length > 0 ? expf(a.g[b * a.gb + head * a.gh]) : 1.f;
 #pragma unroll
-            for (int i = 0; i < 32; i++) {
-                const int p = 32 * half + i;
-                if (p < pw && row < a.N) last[(size_t)p * a.N + row] = st[i] * f;
+            for (int i = 0; i < 16; i++) {
+                const int p = 16 * part + i;
+                if (p < pw && row < a.N) last[(size_t)p * a.N + row] = (i & 1 ? st[i / 2].y : st[i / 2].x) * f;
             }
         }
-        if (MODE == MODE_GRAD && a.ends) {
+        if (Lay::GRAD && a.ends) {
             float sum = 0.f;
             const float* meet = a.meet ? a.meet + (a.segments > 1 ? slot : b) * states + state_at : nullptr;
             if (meet) {
 #pragma unroll
-                for (int i = 0; i < 32; i++) {
-                    const int p = 32 * half + i;
-                    if (p < pw && row < a.N) sum += st[i] * meet[(size_t)p * a.N + row];
+                for (int i = 0; i < 16; i++) {
+                    const int p = 16 * part + i;
+                    if (p < pw && row < a.N) sum += (i & 1 ? st[i / 2].y : st[i / 2].x) * meet[(size_t)p * a.N + row];
                 }
                 if (t_hi < length) sum *= expf(a.g[b * a.gb + t_hi * a.gt + head * a.gh]);
             }
 #pragma unroll
             for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o), diag += __shfl_xor_sync(~0u, diag, o);
             if (lane == 0) words[0][warp] = sum, words[1][warp] = diag;
-            bar_sync(1, 256);
+            bar_sync(1, 32 * TC_WARPS);
             if (tid == 0) {
                 float s0 = 0.f, s1 = 0.f;
-                for (int w = 0; w < 8; w++) s0 += words[0][w], s1 += words[1][w];
+                for (int w = 0; w < TC_WARPS; w++) s0 += words[0][w], s1 += words[1][w];
                 a.ends[slot * vheads + vh] = s0, a.diag[slot * vheads + vh] = s1;
             }
         }
@@ -575,7 +611,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
     tc_before();
     __syncthreads();
     tc_after();
-    if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(Lay::columns));
+    if (warp == TC_WARPS) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(Lay::columns));
 }
 
 cudaError_t scan_tc_launch(const ScanArgs& a, int mode, cudaStream_t st) {
