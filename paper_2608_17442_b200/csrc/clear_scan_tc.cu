@@ -133,8 +133,7 @@ __device__ __forceinline__ void split2(f2 v, uint32_t (&p)[NM]) {
     for (int i = 0; i < NM; i++) {
         p[i] = pack_bf16(v.x, v.y);
         if (i + 1 < NM) {
-            const f2 t = both(p[i]);
-            v = add2(v, {-t.x, -t.y});
+            v = fma2(both(p[i]), {-1.f, -1.f}, v);
         }
     }
 }
@@ -218,6 +217,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
     const uint32_t tmem = tmem_base;
     const int chunks = t_hi > t_lo ? (t_hi - t_lo + TC_Q - 1) / TC_Q : 0, dir = a.backwards ? -1 : 1;
     auto wait = [&](uint32_t which, uint32_t parity) {
+        if (mbar_try_wait(which, parity & 1)) return;
         if (!dead && mbar_wait_bounded(which, parity & 1)) dead = 1, g_clear_status = 1;
     };
 
@@ -387,6 +387,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
             if (lane == 0) mbar_arrive(which);
         };
         float diag = 0.f;
+        const float skip = Lay::OUT && a.skip ? a.skip[head] : 0.f;
         if (chunks) {
             if (MODE) fetch(fq, Lay::q, Lay::QP, left(0));
             fetch(fb, Lay::broad, 2, left(0));
@@ -394,12 +395,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
             if (MODE) put_state();
             cp_async_wait();
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            if (MODE) arrive(b_load);
+            arrive(b_load);
         }
         for (int c = 0; c < chunks; c++) {
             const int valid = left(c), set = c & 1;
             const TcDecays& d = decays[set];
-            bar_sync(1, 32 * TC_WARPS);          // everyone's copies have landed, everyone is done with the chunk before
+            wait(b_load, c);                     // everyone's copies have landed, no one needs the other set any more
             if (c + 1 < chunks) {
                 fetch(fb, Lay::broad + 2 * (set ^ 1), 2, left(c + 1));
                 fetch(fn, Lay::narrow + (set ^ 1), 1, left(c + 1));
@@ -432,39 +433,50 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
                 tc_after();
                 if (c + 1 < chunks) fetch(fq, Lay::q, Lay::QP, left(c + 1));     // O1 is done, too
                 const float2 ci = d.cum[row];
-                const float2 ref = d.ref[part];
-                const float r = ex2((ci.x - ref.x) + (ci.y - ref.y));
+                // whole loops per case: a branch inside would keep the columns from overlapping
+                auto store = [&](const uint32_t (&pl)[8][NO], int h) {
 #pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    uint32_t pl[NO][8];
-                    if (part > quarter) {
+                    for (int p = 0; p < NO; p++) {
+                        uint32_t q[8];
 #pragma unroll
-                        for (int p = 0; p < NO; p++)
+                        for (int e = 0; e < 8; e++) q[e] = pl[e][p];
+                        tc_st8(lanes + Lay::P + 64 * p + 16 * part + 8 * h, q);
+                    }
+                };
+                if (part < quarter) {
+                    const float r = ex2((ci.x - d.ref[part].x) + (ci.y - d.ref[part].y));
 #pragma unroll
-                            for (int e = 0; e < 8; e++) pl[p][e] = 0;
-                    } else {
+                    for (int h = 0; h < 2; h++) {
+                        uint32_t pl[8][NO];
+#pragma unroll
+                        for (int e = 0; e < 8; e += 2) {
+                            const int j = 16 * h + 2 * e;
+                            const float4 tl = *reinterpret_cast<const float4*>(&d.tail[32 * part + j]);
+                            split2<NO>(mul2({__uint_as_float(x[j]), __uint_as_float(x[j + 1])}, mul2({r, r}, {tl.x, tl.y})), pl[e]);
+                            split2<NO>(mul2({__uint_as_float(x[j + 2]), __uint_as_float(x[j + 3])}, mul2({r, r}, {tl.z, tl.w})), pl[e + 1]);
+                        }
+                        store(pl, h);
+                    }
+                } else if (part == quarter) {
+#pragma unroll
+                    for (int h = 0; h < 2; h++) {
+                        uint32_t pl[8][NO];
 #pragma unroll
                         for (int e = 0; e < 8; e++) {
                             const int j = 16 * h + 2 * e;
+                            const float4 cj = *reinterpret_cast<const float4*>(&d.cum[32 * part + j]);
+                            const f2 d0 = fma2({cj.x, cj.y}, {-1.f, -1.f}, {ci.x, ci.y}), d1 = fma2({cj.z, cj.w}, {-1.f, -1.f}, {ci.x, ci.y});
                             f2 v = {__uint_as_float(x[j]), __uint_as_float(x[j + 1])};
-                            if (part < quarter) {
-                                const float2 tl = *reinterpret_cast<const float2*>(&d.tail[32 * part + j]);
-                                v = mul2(v, mul2({r, r}, {tl.x, tl.y}));
-                            } else {
-                                const float4 cj = *reinterpret_cast<const float4*>(&d.cum[32 * part + j]);
-                                const f2 d0 = add2({ci.x, ci.y}, {-cj.x, -cj.y}), d1 = add2({ci.x, ci.y}, {-cj.z, -cj.w});
-                                if (Lay::GRAD) diag += (lane == j ? v.x : 0.f) + (lane == j + 1 ? v.y : 0.f);
-                                v = mul2(v, {ex2(d0.x + d0.y), ex2(d1.x + d1.y)});
-                                v.x = j <= lane ? v.x : 0.f, v.y = j + 1 <= lane ? v.y : 0.f;
-                            }
-                            uint32_t q[NO];
-                            split2<NO>(v, q);
-#pragma unroll
-                            for (int p = 0; p < NO; p++) pl[p][e] = q[p];
+                            if (Lay::GRAD) diag += (lane == j ? v.x : 0.f) + (lane == j + 1 ? v.y : 0.f);
+                            v = mul2(v, {ex2(d0.x + d0.y), ex2(d1.x + d1.y)});
+                            v.x = j <= lane ? v.x : 0.f, v.y = j + 1 <= lane ? v.y : 0.f;
+                            split2<NO>(v, pl[e]);
                         }
+                        store(pl, h);
                     }
-#pragma unroll
-                    for (int p = 0; p < NO; p++) tc_st8(lanes + Lay::P + 64 * p + 16 * part + 8 * h, pl[p]);
+                } else {
+                    const uint32_t pl[8][NO] = {};
+                    store(pl, 0), store(pl, 1);
                 }
                 tc_wait_st();
                 tc_before();
@@ -487,10 +499,16 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
                 }
             }
             if (MODE && c + 1 < chunks) put_state();
+            uint32_t skipped[8] = {};
+            if (Lay::OUT && a.skip) {
+                const uint8_t* src = panels + (Lay::narrow + set) * PANEL;
+                const uint4 v0 = *reinterpret_cast<const uint4*>(src + at0), v1 = *reinterpret_cast<const uint4*>(src + at1);
+                skipped[0] = v0.x, skipped[1] = v0.y, skipped[2] = v0.z, skipped[3] = v0.w, skipped[4] = v1.x, skipped[5] = v1.y, skipped[6] = v1.z, skipped[7] = v1.w;
+            }
             cp_async_wait();
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             tc_before();
-            if (MODE && c + 1 < chunks) arrive(b_load);
+            if (c + 1 < chunks) arrive(b_load);
             const float grow = d.grow[row];
             arrive(b_used + 8 * set);
             if (!MODE) continue;
@@ -498,13 +516,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
             const bool live = (int)row < valid;
             const long long t = t_first + (long long)dir * (c * TC_Q + (int)row);
             if (Lay::OUT) {
-                uint32_t skipped[8] = {};
-                const float skip = a.skip ? a.skip[head] : 0.f;
-                if (a.skip) {
-                    const uint8_t* src = panels + (Lay::narrow + set) * PANEL;
-                    const uint4 v0 = *reinterpret_cast<const uint4*>(src + at0), v1 = *reinterpret_cast<const uint4*>(src + at1);
-                    skipped[0] = v0.x, skipped[1] = v0.y, skipped[2] = v0.z, skipped[3] = v0.w, skipped[4] = v1.x, skipped[5] = v1.y, skipped[6] = v1.z, skipped[7] = v1.w;
-                }
                 wait(b_o, c);
                 tc_after();
                 uint32_t x[16], x1[16], y[16];
