@@ -381,117 +381,31 @@ class Context:
 # Tensors may be views with strides whose innermost dimension is contiguous (column ranges of a projection's output).  Calls run on the
 # current stream of the tensors' device.  `work` is a uint8 CUDA tensor of at least the *_work bytes; without one the call takes its
 # workspace from torch's allocator.
+#
+# Tensors are checked and handed over by binding/clear.cpp (_clear.so): from Python that takes longer than a token's step.
 
-_TYPES = None              # torch dtype -> FESC_BF16, FESC_F16, FESC_F32
+_ext = None
 
 
-def _clear_type(t):
-    global _TYPES
-    if _TYPES is None:
+def _binding():
+    global _ext
+    if _ext is None:
+        L = lib()
+        path = os.path.join(_HERE, "_clear.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is missing: run `python -m paper_2608_17442_b200.build`")
         import torch
 
-        _TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
-    if t.dtype not in _TYPES:
-        raise FescError(EINVAL, f"type {t.dtype}: bfloat16, float16 and float32 are supported")
-    return _TYPES[t.dtype]
+        from importlib import import_module
 
-
-class _Clear:
-    """Checks the tensors of one call and hands out their pointers; the device of the first one is where the call runs."""
-
-    def __init__(self, call: str, t):
-        self.call, self.device, self.dtype = call, t.device, t.dtype
-        if not t.is_cuda:
-            raise FescError(EINVAL, f"{call}: a tensor is not on a CUDA device")
-
-    def refuse(self, what: str):
-        raise FescError(EINVAL, f"{self.call}: {what}")
-
-    def ptr(self, name: str, t, shape, dtype=None, dense=False):
-        """Data pointer of t (None passes through), which must have this shape and type, and contiguous rows (or be dense)."""
-        if t is None:
-            return None
-        if t.shape != shape:
-            self.refuse(f"{name} has the shape {tuple(t.shape)}, not {tuple(shape)}")
-        if t.dtype != (dtype or self.dtype):
-            self.refuse(f"{name} has the type {t.dtype}, not {dtype or self.dtype}")
-        if t.device != self.device:
-            self.refuse(f"{name} is on {t.device}, the others on {self.device}")
-        if dense:
-            if not t.is_contiguous():
-                self.refuse(f"{name} is not contiguous")
-        elif dtype is None and t.stride(-1) != 1 and shape[-1] > 1:
-            self.refuse(f"{name}: the innermost dimension is not contiguous")
-        if (_debug_bounds or (_debug_bounds is None and debug_bounds())) and t.numel():
-            span = 1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))
-            lib().fesc_debug_bounds_register(t.data_ptr(), span * t.element_size())
-        return t.data_ptr()
-
-    def work(self, t, need: int):
-        """(pointer, bytes, the tensor that has to live until the launch) of a workspace of `need` bytes."""
-        if t is None:
-            if not need:
-                return None, 0, None
-            import torch
-
-            t = torch.empty(need, dtype=torch.uint8, device=self.device)
-        elif t.device != self.device or not t.is_contiguous():
-            self.refuse("the workspace is not contiguous, or on another device")
-        if _debug_bounds:
-            lib().fesc_debug_bounds_register(t.data_ptr(), t.numel() * t.element_size())
-        return t.data_ptr(), t.numel() * t.element_size(), t
-
-    def go(self, f, *args):
-        """The call on the current stream of the tensors' device."""
-        import torch
-
-        if self.device.index == torch.cuda.current_device():
-            rc = f(*args, _stream())
-        else:
-            with torch.cuda.device(self.device):
-                rc = f(*args, _stream())
-        if rc != OK:
-            raise FescError(rc, lib().fesc_clear_last_error().decode())
-
-
-def _three(t, n=3):
-    """Strides of batch, token and head of a [batch, L, H, ...] tensor (0 where there is one of them)."""
-    s, z = t.stride(), t.shape
-    return tuple(s[i] if z[i] > 1 else 0 for i in range(3))
-
-
-def _scan_desc(c, x, g, B, C):
-    if x.dim() != 4 or B.dim() != 4:
-        c.refuse("x is [batch, L, H, P], B and C are [batch, L, G, N]")
-    batch, L, H, P = x.shape
-    G, N = B.shape[2:]
-    d = ClearScanDesc(batch, L, H, P, G, N, _clear_type(x))
-    d.x[:], d.g[:], d.B[:], d.C[:] = _three(x), _three(g) if g.dim() == 3 else (0, 0, 0), _three(B), _three(C) if C.dim() == 4 else (0, 0, 0)
-    return d
-
-
-def _scan_inputs(c, d, x, g, B, C, skip, h0, lengths):
-    import torch
-
-    f32 = torch.float32
-    return (c.ptr("x", x, x.shape), c.ptr("g", g, (d.batch, d.L, d.H), f32), c.ptr("B", B, B.shape), c.ptr("C", C, B.shape) if B.shape[:2] == x.shape[:2]
-            else c.refuse("B and C have other batches or lengths than x"), c.ptr("skip", skip, (d.H,), f32, True),
-            c.ptr("h0", h0, (d.batch, d.H, d.P, d.N), f32, True), c.ptr("lengths", lengths, (d.batch,), torch.int32, True))
-
-
-def clear_scan(x, g, B, C, y, skip=None, h0=None, h_out=None, lengths=None, work=None):
-    """Gated linear recurrence h_t = exp(g_t) h_{t-1} + x_t B_t^T, y_t = h_t C_t + skip x_t into y (and the last states into h_out).
-    x, y [batch, L, H, P]; g [batch, L, H] float32; B, C [batch, L, G, N]; skip [H], h0, h_out [batch, H, P, N] float32; lengths [batch] int32."""
-    import torch
-
-    c = _Clear("clear_scan", x)
-    d = _scan_desc(c, x, g, B, C)
-    a = _scan_inputs(c, d, x, g, B, C, skip, h0, lengths)
-    out = c.ptr("y", y, x.shape)
-    d.y[:] = _three(y)
-    last = c.ptr("h_out", h_out, (d.batch, d.H, d.P, d.N), torch.float32, True)
-    w, n, keep = c.work(work, lib().fesc_clear_scan_work(d))
-    c.go(lib().fesc_clear_scan, d, *a, out, last, w, n)
+        m = import_module("._clear", __name__)
+        debug = torch.cuda.is_available() and debug_bounds()
+        names = ["clear_scan", "clear_scan_backward", "clear_scan_step", "clear_norm", "clear_norm_backward", "clear_scan_work", "clear_scan_backward_work",
+                 "clear_norm_backward_work", "clear_last_error"]
+        address = lambda name: ctypes.cast(getattr(L, "fesc_" + name), ctypes.c_void_p).value
+        m.init(FescError, *map(address, names), address("debug_bounds_register") if debug else 0)
+        _ext = m
+    return _ext
 
 
 def clear_sync():
@@ -501,72 +415,30 @@ def clear_sync():
         raise FescError(rc, lib().fesc_clear_last_error().decode())
 
 
+def clear_scan(x, g, B, C, y, skip=None, h0=None, h_out=None, lengths=None, work=None):
+    """Gated linear recurrence h_t = exp(g_t) h_{t-1} + x_t B_t^T, y_t = h_t C_t + skip x_t into y (and the last states into h_out).
+    x, y [batch, L, H, P]; g [batch, L, H] float32; B, C [batch, L, G, N]; skip [H], h0, h_out [batch, H, P, N] float32; lengths [batch] int32."""
+    (_ext or _binding()).clear_scan(x, g, B, C, y, skip, h0, h_out, lengths, work)
+
+
 def clear_scan_backward(x, g, B, C, dy, dx, dg, dB, dC, skip=None, dskip=None, h0=None, dh_out=None, dh0=None, lengths=None, work=None):
     """Gradients of clear_scan from dy (and dh_out, the gradient of its h_out) into dx, dg, dB, dC, dskip and dh0."""
-    import torch
-
-    f32 = torch.float32
-    c = _Clear("clear_scan_backward", x)
-    d = _scan_desc(c, x, g, B, C)
-    a = _scan_inputs(c, d, x, g, B, C, skip, h0, lengths)
-    states = (d.batch, d.H, d.P, d.N)
-    b = (c.ptr("dy", dy, x.shape), c.ptr("dh_out", dh_out, states, f32, True), c.ptr("dx", dx, x.shape), c.ptr("dg", dg, (d.batch, d.L, d.H), f32),
-         c.ptr("dB", dB, B.shape), c.ptr("dC", dC, B.shape), c.ptr("dskip", dskip, (d.H,), f32, True), c.ptr("dh0", dh0, states, f32, True))
-    d.y[:], d.dx[:], d.dg[:], d.dB[:], d.dC[:] = _three(dy), _three(dx), _three(dg), _three(dB), _three(dC)
-    w, n, keep = c.work(work, lib().fesc_clear_scan_backward_work(d))
-    c.go(lib().fesc_clear_scan_backward, d, *a, *b, w, n)
+    (_ext or _binding()).clear_scan_backward(x, g, B, C, dy, dx, dg, dB, dC, skip, dskip, h0, dh_out, dh0, lengths, work)
 
 
 def clear_scan_step(x, g, B, C, state, y, skip=None, state_out=None):
     """One token of clear_scan: x, y [batch, H, P], g [batch, H], B, C [batch, G, N]; state [batch, H, P, N] is updated in place, or left alone
     when state_out is given."""
-    import torch
-
-    f32 = torch.float32
-    c = _Clear("clear_scan_step", x)
-    if x.dim() != 3 or B.dim() != 3 or g.dim() != 2 or C.dim() != 3:
-        c.refuse("x is [batch, H, P], g [batch, H], B and C are [batch, G, N]")
-    (batch, H, P), (G, N) = x.shape, B.shape[1:]
-    d = ClearScanDesc(batch, 1, H, P, G, N, _clear_type(x))
-    for t, s in ((x, d.x), (g, d.g), (B, d.B), (C, d.C), (y, d.y)):
-        s[0], s[2] = t.stride(0) if batch > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0
-    to = state if state_out is None else state_out
-    c.go(lib().fesc_clear_scan_step, d, c.ptr("x", x, x.shape), c.ptr("g", g, (batch, H), f32), c.ptr("B", B, (batch, G, N)), c.ptr("C", C, (batch, G, N)),
-         c.ptr("skip", skip, (H,), f32, True), c.ptr("state", state, (batch, H, P, N), f32, True), c.ptr("state_out", to, (batch, H, P, N), f32, True),
-         c.ptr("y", y, x.shape))
-
-
-def _norm_desc(c, y, groups, eps, /, **rows):
-    if y.dim() != 2:
-        c.refuse("y is [rows, d]")
-    d = ClearNormDesc(y.shape[0], y.shape[1], groups, _clear_type(y), eps)
-    many = y.shape[0] > 1
-    for name, t in rows.items():
-        if t is not None:
-            setattr(d, name + "_stride", t.stride(0) if many else 0)
-    return d, [c.ptr(name, t, y.shape) for name, t in rows.items()]
+    (_ext or _binding()).clear_scan_step(x, g, B, C, state, y, skip, state_out)
 
 
 def clear_norm(y, gamma, n, eps, gate=None, residual=None, scale=None, h=None, groups=1):
     """h = residual + scale * (y * silu(gate)), n = gamma * h / sqrt(mean over a group of h^2 + eps), into n (and h).
     y, n, gate, residual, h [rows, d]; gamma, scale [d] float32."""
-    import torch
-
-    f32 = torch.float32
-    c = _Clear("clear_norm", y)
-    d, (py, pg, pr, pn, ph) = _norm_desc(c, y, groups, eps, y=y, gate=gate, residual=residual, n=n, h=h)
-    c.go(lib().fesc_clear_norm, d, py, c.ptr("gamma", gamma, (d.d,), f32, True), pg, pr, c.ptr("scale", scale, (d.d,), f32, True), pn, ph)
+    (_ext or _binding()).clear_norm(y, gamma, n, eps, gate, residual, scale, h, groups)
 
 
 def clear_norm_backward(y, gamma, dn, dy, dgamma, eps, gate=None, dgate=None, residual=None, dresidual=None, scale=None, dscale=None, dh=None, groups=1,
                         work=None):
     """Gradients of clear_norm from dn (and dh, the gradient of its h) into dy, dgamma, dgate, dresidual and dscale."""
-    import torch
-
-    f32 = torch.float32
-    c = _Clear("clear_norm_backward", y)
-    d, (py, pg, pr, pdn, pdh, pdy, pdg, pdr) = _norm_desc(c, y, groups, eps, y=y, gate=gate, residual=residual, dn=dn, dh=dh, dy=dy, dgate=dgate,
-                                                         dresidual=dresidual)
-    w, nbytes, keep = c.work(work, lib().fesc_clear_norm_backward_work(d))
-    c.go(lib().fesc_clear_norm_backward, d, py, c.ptr("gamma", gamma, (d.d,), f32, True), pg, pr, c.ptr("scale", scale, (d.d,), f32, True), pdn, pdh, pdy,
-         c.ptr("dgamma", dgamma, (d.d,), f32, True), pdg, pdr, c.ptr("dscale", dscale, (d.d,), f32, True), w, nbytes)
+    (_ext or _binding()).clear_norm_backward(y, gamma, dn, dy, dgamma, eps, gate, dgate, residual, dresidual, scale, dscale, dh, groups, work)

@@ -1,4 +1,5 @@
-"""Build the CUDA library in-tree: csrc/*.cu -> libfesc_b200.so (sm_100a only)."""
+"""Build the CUDA library in-tree: csrc/*.cu -> libfesc_b200.so (sm_100a only), and the binding of the cleartext operators,
+binding/clear.cpp -> _clear.so (host code against the headers of the installed torch)."""
 from __future__ import annotations
 
 import glob
@@ -21,6 +22,10 @@ FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std
          "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
 
 
+BINDING = os.path.join(HERE, "binding", "clear.cpp")
+BINDING_LIB = os.path.join(HERE, "_clear.so")
+
+
 def _stale(target: str, deps) -> bool:
     if not os.path.exists(target):
         return True
@@ -29,6 +34,7 @@ def _stale(target: str, deps) -> bool:
 
 
 def build(force: bool = False, verbose: bool = False, debug_bounds: bool = False) -> str:
+    build_binding(force)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.cu")))
     hdrs = glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(INCLUDE, "*.h"))
     obj_dir, lib = (OBJ_DBG, LIB_DBG) if debug_bounds else (OBJ, LIB)
@@ -53,6 +59,28 @@ def build(force: bool = False, verbose: bool = False, debug_bounds: bool = False
                               ["-o", tmp] + objs)
         os.replace(tmp, lib)
     return lib
+
+
+def build_binding(force: bool = False) -> str:
+    if not (force or _stale(BINDING_LIB, [BINDING, os.path.join(INCLUDE, "fesc.h")])):
+        return BINDING_LIB
+    import sysconfig
+
+    import torch
+
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(NVCC))
+    tmp = BINDING_LIB + f".tmp{os.getpid()}"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I", INCLUDE,
+           "-isystem", os.path.join(root, "include"), "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
+           "-isystem", os.path.join(cuda, "include"), "-isystem", sysconfig.get_paths()["include"], BINDING, "-o", tmp, "-L", os.path.join(root, "lib"),
+           "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode:
+        sys.stderr.write(r.stdout + r.stderr)
+        raise RuntimeError("g++ failed: " + " ".join(cmd))
+    os.replace(tmp, BINDING_LIB)
+    return BINDING_LIB
 
 
 if __name__ == "__main__":
