@@ -40,7 +40,14 @@ __device__ __forceinline__ void team_sum(float& a, float& b, float2* words, uint
     }
 }
 
-__device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
+// By the approximate exponential and reciprocal (2 units each; the exponent's rounding adds 2^-24 |z|): with the exact ones the backward pass of the
+// gate issues for as long as it moves bytes.
+__device__ __forceinline__ float sigmoid(float z) {
+    float e, s;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.f + e));
+    return s;
+}
 
 // Eight neighbours of a row as they are in memory: what a thread keeps between its two looks at them (half the registers of float32 for 16-bit types)
 template <class T>
@@ -71,53 +78,60 @@ struct Eight {
     }
 };
 
-template <class T, bool GATE, bool RESIDUAL>
-__global__ void __launch_bounds__(1024) k_clear_norm(const NormArgs a) {
-    __shared__ float2 words[32];
+template <class T, bool GATE, bool RESIDUAL, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : 4) k_clear_norm(const NormArgs a) {
+    __shared__ float2 words[2][32];
     pdl_begin();
     const uint32_t teams = (blockDim.x >> 5) / a.team_warps, team = (threadIdx.x >> 5) / a.team_warps, first = blockIdx.y * a.width;
-    const uint32_t row = blockIdx.x * teams + team;
-    const int c = (int)(threadIdx.x - team * a.team_warps * 32) * 8, count = row < a.rows ? (int)a.width - c : 0;
-    const T* y = (const T*)a.y + (long long)row * a.sy + first + c;
-    const T* z = GATE ? (const T*)a.gate + (long long)row * a.sgate + first + c : nullptr;
-    const T* r = RESIDUAL ? (const T*)a.residual + (long long)row * a.sresidual + first + c : nullptr;
-    T* n = (T*)a.n + (long long)row * a.sn + first + c;
-    T* ho = a.h ? (T*)a.h + (long long)row * a.sh + first + c : nullptr;
-    const size_t bytes = (size_t)min(max(count, 0), 8) * sizeof(T);
-    bool live = count > 0;
-    if (live) live = DBG_REGION(y, bytes) && (!GATE || DBG_REGION(z, bytes)) && (!RESIDUAL || DBG_REGION(r, bytes)) && DBG_REGION(n, bytes) &&
-                     (!ho || DBG_REGION(ho, bytes)) && DBG_REGION(a.gamma, a.d * sizeof(float)) && (!a.scale || DBG_REGION(a.scale, a.d * sizeof(float)));
-    const int some = live ? count : 0;
-    float h[8], g[8], sum = 0.f, unused = 0.f;
-    clear_load8(y, some, a.wide, h);
-    if (GATE) {
-        float v[8];
-        clear_load8(z, some, a.wide, v);
+    const int c = (int)(threadIdx.x - team * a.team_warps * 32) * 8, width = (int)a.width - c;
+    const T *py = (const T*)a.y + first + c, *pz = (const T*)a.gate + first + c, *pr = (const T*)a.residual + first + c;
+    float g[8], s[8];
+    const bool ok = DBG_REGION(a.gamma, a.d * sizeof(float)) && (!a.scale || DBG_REGION(a.scale, a.d * sizeof(float)));
+    Eight<T> y, z, r, ny, nz, nr;
+    auto fetch = [&](uint32_t row) {
+        int count = row < a.rows && width > 0 ? width : 0;
+        const size_t bytes = (size_t)min(count, 8) * sizeof(T);
+        if (count && !(DBG_REGION(py + row * a.sy, bytes) && (!GATE || DBG_REGION(pz + row * a.sgate, bytes)) && (!RESIDUAL || DBG_REGION(pr + row * a.sresidual, bytes))))
+            count = 0;
+        ny.load(py + row * a.sy, count, a.wide);
+        if (GATE) nz.load(pz + row * a.sgate, count, a.wide);
+        if (RESIDUAL) nr.load(pr + row * a.sresidual, count, a.wide);
+    };
+    fetch(blockIdx.x * teams + team);
+    clear_load8(a.gamma + first + c, ok ? width : 0, a.wide, g);
+    if (RESIDUAL && a.scale) clear_load8(a.scale + first + c, ok ? width : 0, a.wide, s);
+    uint32_t turn = 0;
+    // the same number of turns for every team: barriers inside
+    for (uint32_t base = blockIdx.x * teams; base < a.rows; base += gridDim.x * teams, turn ^= 1) {
+        const uint32_t row = base + team;
+        y = ny, z = nz, r = nr;
+        fetch(row + gridDim.x * teams);
+        float h[8], sum = 0.f, unused = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; e++) h[e] *= v[e] * sigmoid(v[e]);
+        for (int e = 0; e < 8; e++) {
+            float v = y[e];
+            if (GATE) v *= z[e] * sigmoid(z[e]);
+            if (RESIDUAL) v = r[e] + (a.scale ? s[e] * v : v);
+            h[e] = v, sum += v * v;      // zeros behind the row's end
+        }
+        T* n = (T*)a.n + (long long)row * a.sn + first + c;
+        T* ho = a.h ? (T*)a.h + (long long)row * a.sh + first + c : nullptr;
+        int count = row < a.rows ? width : 0;
+        const size_t bytes = (size_t)min(max(count, 0), 8) * sizeof(T);
+        if (count > 0 && !(DBG_REGION(n, bytes) && (!ho || DBG_REGION(ho, bytes)))) count = 0;
+        if (ho) clear_store8(ho, count, a.wide, h);
+        team_sum(sum, unused, words[turn], a.team_warps);
+        const float rho = rsqrtf(sum / (float)a.width + a.eps);
+#pragma unroll
+        for (int e = 0; e < 8; e++) h[e] *= g[e] * rho;
+        clear_store8(n, count, a.wide, h);
     }
-    if (RESIDUAL) {
-        float v[8], s[8];
-        clear_load8(r, some, a.wide, v);
-        if (a.scale) clear_load8(a.scale + first + c, some, a.wide, s);
-#pragma unroll
-        for (int e = 0; e < 8; e++) h[e] = v[e] + (a.scale ? s[e] * h[e] : h[e]);
-    }
-    clear_load8(a.gamma + first + c, some, a.wide, g);
-    if (ho) clear_store8(ho, some, a.wide, h);
-#pragma unroll
-    for (int e = 0; e < 8; e++) sum += h[e] * h[e];      // zeros behind the row's end
-    team_sum(sum, unused, words, a.team_warps);
-    const float rho = rsqrtf(sum / (float)a.width + a.eps);
-#pragma unroll
-    for (int e = 0; e < 8; e++) g[e] *= h[e] * rho;
-    clear_store8(n, some, a.wide, g);
 }
 
 // dh_tot = dh + rho w - h rho^3 mean(w h),  w = gamma dn;  dr = dh_tot;  ds = sum_rows dh_tot v;  dv = s dh_tot;
 // dy = dv silu(z);  dz = dv y sigma (1 + z (1 - sigma));  dgamma = sum_rows dn h rho
 template <class T, bool GATE, bool RESIDUAL, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : 2) k_clear_norm_backward(const NormArgs a) {
+__global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : RESIDUAL ? 2 : 3) k_clear_norm_backward(const NormArgs a) {
     __shared__ float2 words[2][32];
     __shared__ float cols[NORM_WARPS * 256];
     pdl_begin();
@@ -271,9 +285,10 @@ static bool norm_wide(const fesc_clear_norm_desc* desc, const void* p, int64_t s
     return !p || (((size_t)p & 15) == 0 && (stride * bytes) % 16 == 0);
 }
 
-template <class T>
+template <class T, int THREADS>
 static void (*norm_kernel(bool gate, bool residual))(NormArgs) {
-    return gate ? residual ? k_clear_norm<T, true, true> : k_clear_norm<T, true, false> : residual ? k_clear_norm<T, false, true> : k_clear_norm<T, false, false>;
+    return gate ? residual ? k_clear_norm<T, true, true, THREADS> : k_clear_norm<T, true, false, THREADS>
+                : residual ? k_clear_norm<T, false, true, THREADS> : k_clear_norm<T, false, false, THREADS>;
 }
 // CTAs of more than 256 threads (rows of more than 2048 channels) have 64 registers a thread and keep some of a row's words in local memory
 template <class T, int THREADS>
@@ -286,11 +301,13 @@ static auto by_type(uint32_t type, F f) {
     return type == FESC_BF16 ? f(__nv_bfloat16()) : type == FESC_F16 ? f(__half()) : f(float());
 }
 
-// CTAs of the backward pass per group of channels: rows are dealt out to at most this many, whose column sums are added up afterwards
-static uint32_t norm_ctas(const fesc_clear_norm_desc* desc, const NormShape& s) {
+// CTAs per group of channels, to which rows are dealt out: as many as are resident (a thread has up to 64 registers forwards, 80 backwards, 128
+// backwards with a residual).
+// Backwards their column sums are added up afterwards.
+static uint32_t norm_ctas(const fesc_clear_norm_desc* desc, const NormShape& s, bool backward, bool residual) {
     const uint64_t all = (desc->rows + s.teams - 1) / s.teams;
-    const uint32_t most = 4 * 148;
-    return all < most ? (uint32_t)all : most;
+    const uint32_t threads = s.warps * s.teams * 32, resident = threads > 256 ? (threads > 512 ? 1 : 2) : 65536 / (threads * (!backward ? 64 : residual ? 128 : 80));
+    return all < 148 * resident ? (uint32_t)all : 148 * resident;
 }
 
 extern "C" int fesc_clear_norm(const fesc_clear_norm_desc* desc, const void* d_y, const float* d_gamma, const void* d_gate, const void* d_residual,
@@ -317,15 +334,17 @@ extern "C" int fesc_clear_norm(const fesc_clear_norm_desc* desc, const void* d_y
              norm_wide(desc, d_gamma, 0, 4) && norm_wide(desc, d_scale, 0, 4);
     const NormShape s = norm_shape(desc);
     a.team_warps = s.warps;
-    auto kernel = by_type(desc->type, [&](auto t) { return norm_kernel<decltype(t)>(d_gate, d_residual); });
-    CLEAR_CUDA(launch(kernel, dim3((a.rows + s.teams - 1) / s.teams, desc->groups), dim3(s.teams * s.warps * 32), 0, (cudaStream_t)stream, a));
+    auto kernel = by_type(desc->type, [&](auto t) { 
+        return s.warps > NORM_WARPS ? norm_kernel<decltype(t), 1024>(d_gate, d_residual) : norm_kernel<decltype(t), 256>(d_gate, d_residual);
+    });
+    CLEAR_CUDA(launch(kernel, dim3(norm_ctas(desc, s, false, d_residual), desc->groups), dim3(s.teams * s.warps * 32), 0, (cudaStream_t)stream, a));
     return FESC_OK;
 }
 
 extern "C" size_t fesc_clear_norm_backward_work(const fesc_clear_norm_desc* desc) {
     const char* what;
     if (!desc || norm_check(desc, &what) != FESC_OK) return 0;
-    return (size_t)norm_ctas(desc, norm_shape(desc)) * 2 * desc->d * sizeof(float);
+    return (size_t)norm_ctas(desc, norm_shape(desc), true, false) * 2 * desc->d * sizeof(float);
 }
 
 extern "C" int fesc_clear_norm_backward(const fesc_clear_norm_desc* desc, const void* d_y, const float* d_gamma, const void* d_gate,
@@ -372,7 +391,7 @@ extern "C" int fesc_clear_norm_backward(const fesc_clear_norm_desc* desc, const 
              norm_wide(desc, d_gamma, 0, 4) && norm_wide(desc, d_scale, 0, 4);
     const NormShape s = norm_shape(desc);
     a.team_warps = s.warps;
-    const uint32_t ctas = norm_ctas(desc, s);
+    const uint32_t ctas = norm_ctas(desc, s, true, d_residual);
     auto kernel = by_type(desc->type, [&](auto t) { 
         return s.warps > NORM_WARPS ? norm_backward_kernel<decltype(t), 1024>(d_gate, d_residual) : norm_backward_kernel<decltype(t), 256>(d_gate, d_residual);
     });
