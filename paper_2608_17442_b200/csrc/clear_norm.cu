@@ -2,10 +2,12 @@
 //   v = y * silu(z),  h = r + s * v,  n = gamma * h / sqrt(mean h^2 + eps)      (mean over a group of channels)
 // the products that the encrypted path forms in fesc_norm_square and fesc_norm_scale, with the gate and residual of the block.
 //
-// One pass: a thread holds eight neighbours of a row, as many warps as a group of channels needs form a team (3 for 768 channels, 6 for
-// 1536), sums go through shuffles and one exchange in shared memory, and what depends on them is written from the registers.  Bound by memory.
+// One pass: a thread holds eight channels of a row (neighbours where 16-byte accesses are possible, every 32nd otherwise), as many warps as a
+// group of channels needs form a team (3 for 768 channels, 6 for 1536), sums go through shuffles and one exchange in shared memory, and what
+// depends on them is written from the registers.  Rows are dealt out to the CTAs that are resident, and the next row's loads are under way while a
+// row is computed.  Bound by memory; the gate's backward pass issues for half of that time.
 // The gradients of gamma and s are sums over rows: a CTA adds up its own rows in a fixed order, a second kernel adds up the CTAs, so the
-// results do not depend on the order in which CTAs run.  There the next row's loads are under way while a row is computed.
+// results do not depend on the order in which CTAs run.
 #define FESC_DBG_FILE 16   // file id in the sites a debug build reports
 #include "clear.cuh"
 
@@ -49,180 +51,199 @@ __device__ __forceinline__ float sigmoid(float z) {
     return s;
 }
 
-// Eight neighbours of a row as they are in memory: what a thread keeps between its two looks at them (half the registers of float32 for 16-bit types)
+// Eight channels of a row as they are in memory: what a thread keeps between its two looks at them (half the registers of float32 for 16-bit types).
+// `left`: channels from the thread's first one to the group's end.
 template <class T>
 struct Eight {
     uint4 w[sizeof(T) / 2];
-    __device__ __forceinline__ void load(const T* p, int count, bool wide) {
-        if (wide && count >= 8) {
+    __device__ __forceinline__ void load(const T* p, int left, bool wide) {
+        if (wide) {
 #pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; i++) w[i] = reinterpret_cast<const uint4*>(p)[i];
+            for (int i = 0; i < (int)sizeof(T) / 2; i++) w[i] = left > 0 ? reinterpret_cast<const uint4*>(p)[i] : make_uint4(0, 0, 0, 0);
         } else {
             T v[8];
 #pragma unroll
-            for (int i = 0; i < 8; i++) v[i] = i < count ? p[i] : ClearType<T>::from(0.f);
+            for (int i = 0; i < 8; i++) v[i] = 32 * i < left ? p[32 * i] : ClearType<T>::from(0.f);
             memcpy(w, v, sizeof(v));
         }
     }
-    __device__ __forceinline__ float operator[](int i) const {      // i known when compiled
-        const uint32_t u[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
+    __device__ __forceinline__ f2 operator[](int i) const {      // two of them, i known when compiled
+        const uint4& v = w[sizeof(T) == 4 ? i >> 1 : 0];
+        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
         if constexpr (sizeof(T) == 4) {
-            const uint32_t x[4] = {w[sizeof(T) / 2 - 1].x, w[sizeof(T) / 2 - 1].y, w[sizeof(T) / 2 - 1].z, w[sizeof(T) / 2 - 1].w};
-            return __uint_as_float(i < 4 ? u[i & 3] : x[i & 3]);
+            return {__uint_as_float(u[2 * (i & 1)]), __uint_as_float(u[2 * (i & 1) + 1])};
         } else if constexpr (std::is_same_v<T, __nv_bfloat16>) {
-            return __uint_as_float(i & 1 ? u[i >> 1] & 0xFFFF0000u : u[i >> 1] << 16);
+            return both(u[i]);
         } else {
-            const __half2 h = *reinterpret_cast<const __half2*>(&u[i >> 1]);
-            return i & 1 ? __high2float(h) : __low2float(h);
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
+            return {f.x, f.y};
         }
     }
 };
+template <class T>
+__device__ __forceinline__ void store8(T* p, int left, bool wide, const f2 (&v)[4]) {
+    if (wide) {
+        const float x[8] = {v[0].x, v[0].y, v[1].x, v[1].y, v[2].x, v[2].y, v[3].x, v[3].y};
+        if (left > 0) clear_store8(p, 8, true, x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            if (32 * i < left) p[32 * i] = ClearType<T>::from(i & 1 ? v[i / 2].y : v[i / 2].x);
+    }
+}
+__device__ __forceinline__ f2 twice(float v) { return {v, v}; }
+
+// the channels of a thread: the first one, and how many there are from there to the group's end
+__device__ __forceinline__ int first_channel(uint32_t thread, bool wide) { return wide ? thread * 8 : thread / 32 * 256 + thread % 32; }
+// its bytes of a row, for the debug build
+template <class T>
+__device__ __forceinline__ size_t span8(int left, bool wide) {
+    return left <= 0 ? 0 : wide ? 8 * sizeof(T) : (size_t)(min((left - 1) / 32, 7) * 32 + 1) * sizeof(T);
+}
 
 template <class T, bool GATE, bool RESIDUAL, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : 4) k_clear_norm(const NormArgs a) {
     __shared__ float2 words[2][32];
     pdl_begin();
     const uint32_t teams = (blockDim.x >> 5) / a.team_warps, team = (threadIdx.x >> 5) / a.team_warps, first = blockIdx.y * a.width;
-    const int c = (int)(threadIdx.x - team * a.team_warps * 32) * 8, width = (int)a.width - c;
+    const int c = first_channel(threadIdx.x - team * a.team_warps * 32, a.wide), width = (int)a.width - c;
     const T *py = (const T*)a.y + first + c, *pz = (const T*)a.gate + first + c, *pr = (const T*)a.residual + first + c;
-    float g[8], s[8];
     const bool ok = DBG_REGION(a.gamma, a.d * sizeof(float)) && (!a.scale || DBG_REGION(a.scale, a.d * sizeof(float)));
     Eight<T> y, z, r, ny, nz, nr;
+    Eight<float> g, s;
     auto fetch = [&](uint32_t row) {
-        int count = row < a.rows && width > 0 ? width : 0;
-        const size_t bytes = (size_t)min(count, 8) * sizeof(T);
-        if (count && !(DBG_REGION(py + row * a.sy, bytes) && (!GATE || DBG_REGION(pz + row * a.sgate, bytes)) && (!RESIDUAL || DBG_REGION(pr + row * a.sresidual, bytes))))
-            count = 0;
-        ny.load(py + row * a.sy, count, a.wide);
-        if (GATE) nz.load(pz + row * a.sgate, count, a.wide);
-        if (RESIDUAL) nr.load(pr + row * a.sresidual, count, a.wide);
+        int left = row < a.rows ? width : 0;
+        const size_t bytes = span8<T>(left, a.wide);
+        if (left > 0 && !(DBG_REGION(py + row * a.sy, bytes) && (!GATE || DBG_REGION(pz + row * a.sgate, bytes)) && (!RESIDUAL || DBG_REGION(pr + row * a.sresidual, bytes))))
+            left = 0;
+        ny.load(py + row * a.sy, left, a.wide);
+        if (GATE) nz.load(pz + row * a.sgate, left, a.wide);
+        if (RESIDUAL) nr.load(pr + row * a.sresidual, left, a.wide);
     };
     fetch(blockIdx.x * teams + team);
-    clear_load8(a.gamma + first + c, ok ? width : 0, a.wide, g);
-    if (RESIDUAL && a.scale) clear_load8(a.scale + first + c, ok ? width : 0, a.wide, s);
+    g.load(a.gamma + first + c, ok ? width : 0, a.wide);
+    if (RESIDUAL && a.scale) s.load(a.scale + first + c, ok ? width : 0, a.wide);
     uint32_t turn = 0;
     // the same number of turns for every team: barriers inside
     for (uint32_t base = blockIdx.x * teams; base < a.rows; base += gridDim.x * teams, turn ^= 1) {
         const uint32_t row = base + team;
         y = ny, z = nz, r = nr;
         fetch(row + gridDim.x * teams);
-        float h[8], sum = 0.f, unused = 0.f;
+        f2 h[4], sums = {0.f, 0.f};
+        float unused = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-            float v = y[e];
-            if (GATE) v *= z[e] * sigmoid(z[e]);
-            if (RESIDUAL) v = r[e] + (a.scale ? s[e] * v : v);
-            h[e] = v, sum += v * v;      // zeros behind the row's end
+        for (int e = 0; e < 4; e++) {
+            f2 v = y[e];
+            if (GATE) v = mul2(v, mul2(z[e], {sigmoid(z[e].x), sigmoid(z[e].y)}));
+            if (RESIDUAL) v = a.scale ? fma2(s[e], v, r[e]) : add2(v, r[e]);
+            h[e] = v, sums = fma2(v, v, sums);      // zeros behind the row's end
         }
         T* n = (T*)a.n + (long long)row * a.sn + first + c;
         T* ho = a.h ? (T*)a.h + (long long)row * a.sh + first + c : nullptr;
-        int count = row < a.rows ? width : 0;
-        const size_t bytes = (size_t)min(max(count, 0), 8) * sizeof(T);
-        if (count > 0 && !(DBG_REGION(n, bytes) && (!ho || DBG_REGION(ho, bytes)))) count = 0;
-        if (ho) clear_store8(ho, count, a.wide, h);
+        int left = row < a.rows ? width : 0;
+        const size_t bytes = span8<T>(left, a.wide);
+        if (left > 0 && !(DBG_REGION(n, bytes) && (!ho || DBG_REGION(ho, bytes)))) left = 0;
+        if (ho) store8(ho, left, a.wide, h);
+        float sum = sums.x + sums.y;
         team_sum(sum, unused, words[turn], a.team_warps);
         const float rho = rsqrtf(sum / (float)a.width + a.eps);
 #pragma unroll
-        for (int e = 0; e < 8; e++) h[e] *= g[e] * rho;
-        clear_store8(n, count, a.wide, h);
+        for (int e = 0; e < 4; e++) h[e] = mul2(h[e], mul2(g[e], twice(rho)));
+        store8(n, left, a.wide, h);
     }
 }
 
 // dh_tot = dh + rho w - h rho^3 mean(w h),  w = gamma dn;  dr = dh_tot;  ds = sum_rows dh_tot v;  dv = s dh_tot;
-// dy = dv silu(z);  dz = dv y sigma (1 + z (1 - sigma));  dgamma = sum_rows dn h rho
+// dy = dv silu(z);  dz = dv y sigma (1 + z (1 - sigma)) = dv y (sigma + silu(z) (1 - sigma));  dgamma = sum_rows dn h rho
 template <class T, bool GATE, bool RESIDUAL, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : RESIDUAL ? 2 : 3) k_clear_norm_backward(const NormArgs a) {
     __shared__ float2 words[2][32];
     __shared__ float cols[NORM_WARPS * 256];
     pdl_begin();
     const uint32_t teams = (blockDim.x >> 5) / a.team_warps, team = (threadIdx.x >> 5) / a.team_warps, first = blockIdx.y * a.width;
-    const int c = (int)(threadIdx.x - team * a.team_warps * 32) * 8, width = (int)a.width - c;
+    const int c = first_channel(threadIdx.x - team * a.team_warps * 32, a.wide), width = (int)a.width - c;
     const T *py = (const T*)a.y + first + c, *pz = (const T*)a.gate + first + c, *pr = (const T*)a.residual + first + c, *pn = (const T*)a.dn + first + c,
             *ph = (const T*)a.dh + first + c;
     const bool dh = RESIDUAL && a.dh;
-    float g[8], s[8], dgamma[8] = {}, dscale[8] = {};
+    f2 dgamma[4] = {}, dscale[4] = {};
     const bool ok = DBG_REGION(a.gamma, a.d * sizeof(float)) && (!a.scale || DBG_REGION(a.scale, a.d * sizeof(float)));
-    clear_load8(a.gamma + first + c, ok ? width : 0, a.wide, g);
-    if (RESIDUAL && a.scale) clear_load8(a.scale + first + c, ok ? width : 0, a.wide, s);
     Eight<T> y, z, r, w, hh, ny, nz, nr, nw, nh;
-    auto fetch = [&](uint32_t row, Eight<T>& vy, Eight<T>& vz, Eight<T>& vr, Eight<T>& vw, Eight<T>& vh) {
-        int count = row < a.rows && width > 0 ? width : 0;
-        const size_t bytes = (size_t)min(count, 8) * sizeof(T);
-        if (count && !(DBG_REGION(py + row * a.sy, bytes) && DBG_REGION(pn + row * a.sdn, bytes) && (!GATE || DBG_REGION(pz + row * a.sgate, bytes)) &&
-                       (!RESIDUAL || DBG_REGION(pr + row * a.sresidual, bytes)) && (!dh || DBG_REGION(ph + row * a.sdh, bytes))))
-            count = 0;
-        vy.load(py + row * a.sy, count, a.wide), vw.load(pn + row * a.sdn, count, a.wide);
-        if (GATE) vz.load(pz + row * a.sgate, count, a.wide);
-        if (RESIDUAL) vr.load(pr + row * a.sresidual, count, a.wide);
-        if (dh) vh.load(ph + row * a.sdh, count, a.wide);
+    Eight<float> g, s;
+    auto fetch = [&](uint32_t row) {
+        int left = row < a.rows ? width : 0;
+        const size_t bytes = span8<T>(left, a.wide);
+        if (left > 0 && !(DBG_REGION(py + row * a.sy, bytes) && DBG_REGION(pn + row * a.sdn, bytes) && (!GATE || DBG_REGION(pz + row * a.sgate, bytes)) &&
+                          (!RESIDUAL || DBG_REGION(pr + row * a.sresidual, bytes)) && (!dh || DBG_REGION(ph + row * a.sdh, bytes))))
+            left = 0;
+        ny.load(py + row * a.sy, left, a.wide), nw.load(pn + row * a.sdn, left, a.wide);
+        if (GATE) nz.load(pz + row * a.sgate, left, a.wide);
+        if (RESIDUAL) nr.load(pr + row * a.sresidual, left, a.wide);
+        if (dh) nh.load(ph + row * a.sdh, left, a.wide);
     };
-    fetch(blockIdx.x * teams + team, ny, nz, nr, nw, nh);
+    fetch(blockIdx.x * teams + team);
+    g.load(a.gamma + first + c, ok ? width : 0, a.wide);
+    if (RESIDUAL && a.scale) s.load(a.scale + first + c, ok ? width : 0, a.wide);
     uint32_t turn = 0;
     // the same number of turns for every team: barriers inside
     for (uint32_t base = blockIdx.x * teams; base < a.rows; base += gridDim.x * teams, turn ^= 1) {
         const uint32_t row = base + team;
         y = ny, z = nz, r = nr, w = nw, hh = nh;
-        fetch(row + gridDim.x * teams, ny, nz, nr, nw, nh);
-        float h[8], sig[8], sum = 0.f, dot = 0.f;
+        fetch(row + gridDim.x * teams);
+        f2 h[4], sig[4], sums = {0.f, 0.f}, dots = {0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-            sig[e] = GATE ? sigmoid(z[e]) : 1.f;
-            float v = y[e];
-            if (GATE) v *= z[e] * sig[e];
-            if (RESIDUAL) v = r[e] + (a.scale ? s[e] * v : v);
+        for (int e = 0; e < 4; e++) {
+            f2 v = y[e];
+            if (GATE) sig[e] = {sigmoid(z[e].x), sigmoid(z[e].y)}, v = mul2(v, mul2(z[e], sig[e]));
+            if (RESIDUAL) v = a.scale ? fma2(s[e], v, r[e]) : add2(v, r[e]);
             h[e] = v;
-            sum += v * v, dot += g[e] * w[e] * v;
+            sums = fma2(v, v, sums), dots = fma2(mul2(g[e], w[e]), v, dots);
         }
+        float sum = sums.x + sums.y, dot = dots.x + dots.y;
         team_sum(sum, dot, words[turn], a.team_warps);
         const float rho = rsqrtf(sum / (float)a.width + a.eps), k = rho * rho * rho * (dot / (float)a.width);
-        int count = row < a.rows ? width : 0;
+        int left = row < a.rows ? width : 0;
         T* dy = (T*)a.dy + (long long)row * a.sdy + first + c;
         T* dz = GATE ? (T*)a.dgate + (long long)row * a.sdgate + first + c : nullptr;
         T* dr = RESIDUAL ? (T*)a.dresidual + (long long)row * a.sdresidual + first + c : nullptr;
-        const size_t bytes = (size_t)min(max(count, 0), 8) * sizeof(T);
-        if (count > 0 && !(DBG_REGION(dy, bytes) && (!GATE || DBG_REGION(dz, bytes)) && (!RESIDUAL || DBG_REGION(dr, bytes)))) count = 0;
-        float d[8];
+        const size_t bytes = span8<T>(left, a.wide);
+        if (left > 0 && !(DBG_REGION(dy, bytes) && (!GATE || DBG_REGION(dz, bytes)) && (!RESIDUAL || DBG_REGION(dr, bytes)))) left = 0;
+        f2 d[4];
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-            d[e] = rho * g[e] * w[e] - k * h[e];
-            if (dh) d[e] += hh[e];
-            dgamma[e] += w[e] * h[e] * rho;
+        for (int e = 0; e < 4; e++) {
+            const f2 wr = mul2(w[e], twice(rho));
+            d[e] = fma2(h[e], twice(-k), mul2(g[e], wr));
+            if (dh) d[e] = add2(d[e], hh[e]);
+            dgamma[e] = fma2(wr, h[e], dgamma[e]);
         }
-        if (RESIDUAL) {
-            clear_store8(dr, count, a.wide, d);
-            if (a.scale) {
+        if (RESIDUAL) store8(dr, left, a.wide, d);
+        f2 o[4];
 #pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    dscale[e] += d[e] * (GATE ? y[e] * z[e] * sig[e] : y[e]);
-                    d[e] *= s[e];
-                }
+        for (int e = 0; e < 4; e++) {
+            const f2 silu = GATE ? mul2(z[e], sig[e]) : f2{1.f, 1.f};
+            if (RESIDUAL && a.scale) {
+                dscale[e] = fma2(d[e], GATE ? mul2(y[e], silu) : y[e], dscale[e]);
+                d[e] = mul2(d[e], s[e]);
             }
+            if (GATE) o[e] = mul2(mul2(d[e], y[e]), fma2(silu, fma2(sig[e], twice(-1.f), twice(1.f)), sig[e])), d[e] = mul2(d[e], silu);
         }
-        if (GATE) {
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 8; e++) {
-                v[e] = d[e] * y[e] * sig[e] * (1.f + z[e] * (1.f - sig[e]));
-                d[e] *= z[e] * sig[e];
-            }
-            clear_store8(dz, count, a.wide, v);
-        }
-        clear_store8(dy, count, a.wide, d);
+        if (GATE) store8(dz, left, a.wide, o);
+        store8(dy, left, a.wide, d);
     }
     // the teams' sums, team by team
     float* part = a.part + (size_t)blockIdx.x * 2 * a.d + first;
     if (!DBG_REGION(part, (a.d + a.width) * sizeof(float))) return;
-    auto leave = [&](const float(&v)[8], float* out) {
+    auto leave = [&](const f2 (&v)[4], float* out) {
+        const int step = a.wide ? 1 : 32;
         if (teams == 1) {
 #pragma unroll
             for (int e = 0; e < 8; e++)
-                if (e < width) out[c + e] = v[e];
+                if (e * step < width) out[c + e * step] = e & 1 ? v[e / 2].y : v[e / 2].x;
             return;
         }
         const uint32_t span = a.team_warps * 256;       // a CTA of several teams has at most NORM_WARPS warps
         __syncthreads();
 #pragma unroll
-        for (int e = 0; e < 8; e++) cols[team * span + c + e] = v[e];
+        for (int e = 0; e < 8; e++) cols[team * span + c + e * step] = e & 1 ? v[e / 2].y : v[e / 2].x;
         __syncthreads();
         for (uint32_t j = threadIdx.x; j < a.width; j += blockDim.x) {
             float t = 0.f;
@@ -234,23 +255,25 @@ __global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : RESIDUAL ? 2 : 3)
     if (RESIDUAL && a.scale) leave(dscale, part + a.d);
 }
 
-// out[c] = the CTAs' sums of channel c: 8 threads take every eighth CTA each, then add up
-__global__ void __launch_bounds__(256) k_clear_norm_columns(const float* part, float* dgamma, float* dscale, uint32_t ctas, uint32_t d) {
-    __shared__ float words[8][33];
+// out[c] = the CTAs' sums of channel c: 32 threads take every 32nd CTA each, then add up in a tree (8 threads with 74 loads each took longer than
+// the pass over the rows)
+__global__ void __launch_bounds__(1024) k_clear_norm_columns(const float* part, float* dgamma, float* dscale, uint32_t ctas, uint32_t d) {
+    __shared__ double words[32][33];
     pdl_begin();
     const uint32_t x = threadIdx.x & 31, s = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
     float* out = blockIdx.y ? dscale : dgamma;
     if (!DBG_REGION(part, (size_t)ctas * 2 * d * sizeof(float)) || !DBG_REGION(out, d * sizeof(float))) return;
     double t = 0.0;
-    if (c < d)
-        for (uint32_t i = s; i < ctas; i += 8) t += part[((size_t)i * 2 + blockIdx.y) * d + c];
-    words[s][x] = (float)t;
-    __syncthreads();
-    if (s == 0 && c < d) {
-        double v = 0.0;
-        for (int i = 0; i < 8; i++) v += words[i][x];
-        out[c] = (float)v;
+    if (c < d) {
+#pragma unroll 4
+        for (uint32_t i = s; i < ctas; i += 32) t += part[((size_t)i * 2 + blockIdx.y) * d + c];
     }
+    words[s][x] = t;
+    __syncthreads();
+    double v = words[x][s];      // warp s adds up column s
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+    if (x == 0 && blockIdx.x * 32 + s < d) out[blockIdx.x * 32 + s] = (float)v;
 }
 
 // ---------------------------------------------------------------------------------------
@@ -329,7 +352,7 @@ extern "C" int fesc_clear_norm(const fesc_clear_norm_desc* desc, const void* d_y
     a.y = d_y, a.gate = d_gate, a.residual = d_residual, a.n = d_n, a.h = d_h, a.gamma = d_gamma, a.scale = d_scale;
     a.sy = desc->y_stride, a.sgate = desc->gate_stride, a.sresidual = desc->residual_stride, a.sn = desc->n_stride, a.sh = desc->h_stride;
     a.rows = (uint32_t)desc->rows, a.d = desc->d, a.width = width, a.eps = desc->eps;
-    a.wide = width * bytes % 16 == 0 && width % 4 == 0 && norm_wide(desc, d_y, a.sy, bytes) && norm_wide(desc, d_gate, a.sgate, bytes) &&
+    a.wide = width % 8 == 0 && norm_wide(desc, d_y, a.sy, bytes) && norm_wide(desc, d_gate, a.sgate, bytes) &&
              norm_wide(desc, d_residual, a.sresidual, bytes) && norm_wide(desc, d_n, a.sn, bytes) && norm_wide(desc, d_h, a.sh, bytes) &&
              norm_wide(desc, d_gamma, 0, 4) && norm_wide(desc, d_scale, 0, 4);
     const NormShape s = norm_shape(desc);
@@ -385,7 +408,7 @@ extern "C" int fesc_clear_norm_backward(const fesc_clear_norm_desc* desc, const 
     a.sy = desc->y_stride, a.sgate = desc->gate_stride, a.sresidual = desc->residual_stride, a.sdn = desc->dn_stride, a.sdh = desc->dh_stride;
     a.sdy = desc->dy_stride, a.sdgate = desc->dgate_stride, a.sdresidual = desc->dresidual_stride;
     a.rows = (uint32_t)desc->rows, a.d = desc->d, a.width = width, a.eps = desc->eps;
-    a.wide = width * bytes % 16 == 0 && width % 4 == 0 && norm_wide(desc, d_y, a.sy, bytes) && norm_wide(desc, d_gate, a.sgate, bytes) &&
+    a.wide = width % 8 == 0 && norm_wide(desc, d_y, a.sy, bytes) && norm_wide(desc, d_gate, a.sgate, bytes) &&
              norm_wide(desc, d_residual, a.sresidual, bytes) && norm_wide(desc, d_dn, a.sdn, bytes) && norm_wide(desc, d_dh, a.sdh, bytes) &&
              norm_wide(desc, d_dy, a.sdy, bytes) && norm_wide(desc, d_dgate, a.sdgate, bytes) && norm_wide(desc, d_dresidual, a.sdresidual, bytes) &&
              norm_wide(desc, d_gamma, 0, 4) && norm_wide(desc, d_scale, 0, 4);
@@ -396,6 +419,6 @@ extern "C" int fesc_clear_norm_backward(const fesc_clear_norm_desc* desc, const 
         return s.warps > NORM_WARPS ? norm_backward_kernel<decltype(t), 1024>(d_gate, d_residual) : norm_backward_kernel<decltype(t), 256>(d_gate, d_residual);
     });
     CLEAR_CUDA(launch(kernel, dim3(ctas, desc->groups), dim3(s.teams * s.warps * 32), 0, st, a));
-    CLEAR_CUDA(launch(k_clear_norm_columns, dim3((desc->d + 31) / 32, d_dscale ? 2 : 1), dim3(256), 0, st, (const float*)a.part, d_dgamma, d_dscale, ctas, desc->d));
+    CLEAR_CUDA(launch(k_clear_norm_columns, dim3((desc->d + 31) / 32, d_dscale ? 2 : 1), dim3(1024), 0, st, (const float*)a.part, d_dgamma, d_dscale, ctas, desc->d));
     return FESC_OK;
 }

@@ -49,8 +49,12 @@ CASES = [(1, 1, 1, "fp32", 1, 1, 1), (8, 1536, 1, "bf16", 1, 0, 0), (37, 768, 1,
 @pytest.mark.parametrize("rows, d, groups, t, gate, residual, scale", CASES)
 def test_norm_and_gradients_against_the_definition(rows, d, groups, t, gate, residual, scale):
     s = inputs(rows, d, t, gate, residual, scale, rows + d)
-    T = TYPES[t]
-    n, h = forward(s, groups)
+    check(s, groups, *forward(s, groups), backward(s, groups))
+
+
+def check(s, groups, n, h, o):
+    (rows, d), T = s["y"].shape, s["y"].dtype
+    gate, residual, scale = (s[k] is not None for k in ("gate", "residual", "scale"))
     wn, wh, grads = reference(s, groups)
     # magnitudes of what is summed; a sum of a row is a tree over its threads behind at most 16 terms of a thread: below 32 roundings of 2^-24, the
     # functions 2 units each
@@ -66,7 +70,6 @@ def test_norm_and_gradients_against_the_definition(rows, d, groups, t, gate, res
     # relative error of the mean square: twice that of h, of which a sum of two terms may keep little
     part = spread(rho ** 2 * (hm * wh.abs()).reshape(rows, groups, -1).mean(2, keepdim=True))
     assert off(n, wn, u * gamma * spread(rho) * (hm + wh.abs() * (1 + part)), T) <= 0
-    o = backward(s, groups)
     w = gamma * wide(s["dn"]).abs()
     inner = spread(rho ** 3 * (w * hm).reshape(rows, groups, -1).mean(2, keepdim=True))
     dt = (spread(rho) * w + hm * inner) * (2 + part) + (wide(s["dh"]).abs() if residual else 0)
@@ -91,15 +94,20 @@ def test_views_unaligned_rows_and_shared_rows():
     s = inputs(50, 96, "bf16", 1, 1, 1, 3)
     n, h = forward(s, 2)
     o = backward(s, 2)
-    for shift in (0, 1, 8):
-        pad = {k: v for k, v in s.items()}
-        for k in ("y", "gate", "residual", "dn", "dh"):
-            room = torch.zeros((50, 96 + 17), dtype=torch.bfloat16, device="cuda")[:, shift:shift + 96]
-            room.copy_(s[k])
-            pad[k] = room
-        n2, h2 = forward(pad, 2)
-        o2 = backward(pad, 2)
-        assert torch.equal(n, n2) and torch.equal(h, h2) and all(torch.equal(o[k], o2[k]) for k in o)
+    check(s, 2, n, h, o)
+    for extra, shifts in ((16, (0, 8, 16)), (17, (0, 1, 8))):        # rows that allow 16-byte accesses, and rows that do not
+        first = None
+        for shift in shifts:
+            pad = {k: v for k, v in s.items()}
+            for k in ("y", "gate", "residual", "dn", "dh"):
+                room = torch.zeros((50, 96 + extra), dtype=torch.bfloat16, device="cuda")[:, shift:shift + 96]
+                room.copy_(s[k])
+                pad[k] = room
+            n2, h2 = forward(pad, 2)
+            o2 = backward(pad, 2)
+            check(s, 2, n2, h2, o2)
+            first = first or ((n, h, o) if extra == 16 else (n2, h2, o2))      # a row is added up in one order per kind of access
+            assert torch.equal(first[0], n2) and torch.equal(first[1], h2) and all(torch.equal(first[2][k], o2[k]) for k in o)
     one = dict(s, residual=s["residual"][:1].expand(50, 96))
     n2, _ = forward(one)
     n3, _ = forward(dict(s, residual=one["residual"].contiguous()))
