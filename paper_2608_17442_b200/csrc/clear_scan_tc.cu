@@ -10,7 +10,9 @@
 // out = decay since the chunk's start * O1 + O2.  A tile of 128 tokens x 64 columns in shared memory (a panel, 16 KB, 128-byte swizzle) is the
 // K-major operand of one product and the MN-major operand of another, so nothing is stored twice or transposed.
 //
-// Sixteen warps compute (a thread owns a row and a quarter of the columns), one issues the products, one sums up the log decays of the next chunks.
+// Sixteen warps compute (a thread owns a row and a quarter of the columns), one issues the products, one sums up the log decays of the next chunks,
+// two copy the next chunk's operands.  Shared memory leaves the L1 so little that a spilled register is read back from L2: with the copies
+// in the computing warps, whose 96 registers their addresses overflowed, a chunk took 10 500 cycles.
 // The products of a chunk run while the threads are at something else: O1 while the faded values are formed, H while the scores are decayed,
 // O2 while the state is updated; the next chunk's S while the outputs are written.  Reading operands from shared memory (128 bytes a cycle) is
 // what a product of these widths takes, so the planes of one right operand are multiplied side by side where tensor memory has room
@@ -23,8 +25,8 @@
 
 #define TC_Q 128
 #define PANEL 16384u
-#define TC_WARPS 16             // that compute; one more issues, one more sums decays
-#define TC_THREADS (32 * (TC_WARPS + 2))
+#define TC_WARPS 16             // that compute; one more issues, one more sums decays, two copy
+#define TC_THREADS (32 * (TC_WARPS + 4))
 
 template <int MODE>
 struct TcLayout {
@@ -33,9 +35,10 @@ struct TcLayout {
     // panels in shared memory; k and v have two sets
     static constexpr int q = 0, QP = OUT ? 2 : GRAD ? 1 : 0;
     static constexpr int broad = QP, narrow = broad + 4, w = narrow + 2, st = w + 3, panels = st + (MODE ? NO : 0);
-    // columns of tensor memory, all 512 with outputs: the planes of the scores lie over the scores themselves
+    // Columns of tensor memory, all 512 with outputs.  The first two planes of 16 decayed scores lie over the 16 scores, so a warp overwrites what it
+    // has read itself; a third plane has columns of its own.
     static constexpr uint32_t DV = GRAD ? 128 : 64, O1_PARTS = OUT ? 2 : 1, H_PARTS = GRAD ? 1 : 3;      // accumulators side by side, one per plane
-    static constexpr uint32_t P = 0, S = GRAD ? 64 : 0, O1 = GRAD ? 192 : 128, O2 = O1 + O1_PARTS * DV, H = MODE ? O2 + DV : 0, columns = MODE ? 512 : 256;
+    static constexpr uint32_t S = 0, P3 = 128, O1 = GRAD ? 192 : 128, O2 = O1 + O1_PARTS * DV, H = MODE ? O2 + DV : 0, columns = MODE ? 512 : 256;
     static_assert(H + 64 * H_PARTS <= columns, "accumulators fit");
     static constexpr size_t bytes = (size_t)panels * PANEL + 1024;  // panels start on 1024 bytes
 };
@@ -130,7 +133,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
     constexpr int NO = Lay::NO, NS = 3;
     extern __shared__ __align__(1024) uint8_t tc_smem[];
     __shared__ TcDecays decays[2];
-    __shared__ __align__(8) u64 bars[12];
+    __shared__ __align__(8) u64 bars[12];        // see below
     __shared__ uint32_t tmem_base;
     __shared__ volatile uint32_t dead;          // a wait gave up: the rest of the chunks goes through without waiting, with nothing of worth in it
     __shared__ float words[2][TC_WARPS];
@@ -173,8 +176,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
 #endif
     const uint32_t base = ((uint32_t)__cvta_generic_to_shared(tc_smem) + 1023) & ~1023u, bar = (uint32_t)__cvta_generic_to_shared(bars);
     uint8_t* const panels = tc_smem + (base - (uint32_t)__cvta_generic_to_shared(tc_smem));
-    const uint32_t b_load = bar, b_wv = bar + 8, b_p = bar + 16, b_epi = bar + 24, b_s = bar + 32, b_h = bar + 40, b_o = bar + 48, drained = bar + 56;
-    // of the two sets of decays: filled, and used; a set has barriers of its own because the warp that fills them runs up to two chunks ahead
+    // per chunk: operands copied; faded values, state, decayed scores written; products S and O1, H, O2 done
+    const uint32_t b_load = bar, b_wv = bar + 8, b_st = bar + 16, b_p = bar + 24, b_s = bar + 32, b_h = bar + 40, b_o = bar + 48, drained = bar + 56;
+    // of the two sets of decays and operands: decays filled, all used (and O1 and O2 read); a set has barriers of its own because those who fill
+    // them run up to two chunks ahead
     const uint32_t b_g = bar + 64, b_used = bar + 80;
     if (warp == TC_WARPS) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"((uint32_t)__cvta_generic_to_shared(&tmem_base)), "n"(Lay::columns)
@@ -182,7 +187,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     if (tid == 0) {
-        mbar_init(b_load, TC_WARPS), mbar_init(b_wv, TC_WARPS), mbar_init(b_p, TC_WARPS), mbar_init(b_epi, TC_WARPS);
+        mbar_init(b_load, 2), mbar_init(b_wv, TC_WARPS), mbar_init(b_p, TC_WARPS), mbar_init(b_st, TC_WARPS);
         for (uint32_t i = 0; i < 2; i++) mbar_init(b_g + 8 * i, 1), mbar_init(b_used + 8 * i, TC_WARPS);
         mbar_init(b_s, 1), mbar_init(b_h, 1), mbar_init(b_o, 1), mbar_init(drained, 1);
         dead = 0;
@@ -192,7 +197,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
     __syncthreads();
     tc_after();
     const uint32_t tmem = tmem_base;
+    auto left = [&](int c) { return min(TC_Q, t_hi - t_lo - c * TC_Q); };      // tokens of a chunk
     const int chunks = t_hi > t_lo ? (t_hi - t_lo + TC_Q - 1) / TC_Q : 0, dir = a.backwards ? -1 : 1;
+    const int t_first = a.backwards ? t_hi - 1 : t_lo;
     auto wait = [&](uint32_t which, uint32_t parity) {
         if (mbar_try_wait(which, parity & 1)) return;
         if (!dead && mbar_wait_bounded(which, parity & 1)) dead = 1, g_clear_status = 1;
@@ -220,7 +227,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
                             tc_mma_ss(tmem + Lay::S, pq + at, (Lay::OUT ? pb : pn) + at, I_S, k);
                         }
                     }
-                    if (c) wait(b_epi, c - 1);
+                    wait(b_st, c);
+                    if (c) wait(b_used + 8 * (set ^ 1), (c - 1) >> 1);
                     tc_after();
                     if (!dead) {
 #pragma unroll
@@ -248,7 +256,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
                         for (uint32_t p = 0; p < NO; p++)
 #pragma unroll
                             for (uint32_t k = 0; k < 8; k++)
-                                tc_mma_ts(tmem + Lay::O2, tmem + Lay::P + 64 * p + 8 * k, (Lay::GRAD ? pb : pn) + k * 128, I_O2, p || k);
+                                tc_mma_ts(tmem + Lay::O2, tmem + (p < 2 ? Lay::S + 16 * k + 8 * p : Lay::P3 + 8 * k), (Lay::GRAD ? pb : pn) + k * 128, I_O2, p || k);
                         tc_commit(b_o);
                     }
                 }
@@ -299,6 +307,45 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
             if (lane == 0) mbar_arrive(b_g + 8 * (c & 1));
         }
         if (MODE == MODE_STATE && lane == 0 && tile == 0) a.decay[slot * a.H + head] = (float)exp2(through);
+    } else if (warp > TC_WARPS + 1) {
+        // Copies.  A thread has one 16-byte chunk of every eighth row: its place in a panel moves by 1024 bytes from row to row.
+        const uint32_t me = tid - 32 * (TC_WARPS + 2), r0 = me >> 3, col = (me & 7) * 8, to = base + panel_at(r0, me & 7);
+        const T *pb = nullptr, *pn = nullptr, *pq = nullptr;
+        if (chunks) {
+            pb = scan_row<T>(ob, b, t_first + dir * (int)r0, head, group, tile) + col, pn = scan_row<T>(on, b, t_first + dir * (int)r0, head, group, tile) + col;
+            if (MODE) pq = scan_row<T>(a.q, b, t_first + dir * (int)r0, head, group, tile) + col;
+        }
+        // one panel of a chunk; what does not exist is not read: zero bytes of an address that does
+        auto copy = [&](uint32_t panel, const T* p, long long step, int width, int valid) {
+            const int bytes = min(max(width - (int)col, 0), 8) * 2;
+            const uint32_t dst = to + panel * PANEL;
+            if (valid == TC_Q && bytes == 16) {
+#pragma unroll 8
+                for (uint32_t i = 0; i < TC_Q / 8; i++, p += step) cp_async16(dst + 1024 * i, p);
+            } else {
+                for (uint32_t i = 0; i < TC_Q / 8; i++, p += step) {
+                    const int n = (int)(r0 + 8 * i) < valid ? bytes : 0;
+                    cp_async16_part(dst + 1024 * i, n ? p : (const T*)a.g, n);
+                }
+            }
+        };
+        for (int c = 0; c < chunks; c++) {
+            const uint32_t set = c & 1;
+            if (c >= 2) wait(b_used + 8 * set, (c >> 1) - 1);
+            const long long sb = 8 * dir * ob.st, sn = 8 * dir * on.st, sq = 8 * dir * a.q.st, done = (long long)c * (TC_Q / 8);
+            copy(Lay::broad + 2 * set, pb + done * sb, sb, (int)a.N, left(c));
+            copy(Lay::broad + 2 * set + 1, pb + done * sb + 64, sb, (int)a.N - 64, left(c));
+            copy(Lay::narrow + set, pn + done * sn, sn, pw, left(c));
+            if (MODE) {
+                if (c) wait(b_s, c - 1);
+                copy(Lay::q, pq + done * sq, sq, qw, left(c));
+                if (Lay::QP == 2) copy(Lay::q + 1, pq + done * sq + 64, sq, qw - 64, left(c));
+            }
+            cp_async_wait();
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(b_load);
+        }
     } else {
         const uint32_t quarter = warp & 3, part = warp >> 2, row = 32 * quarter + lane;     // row: token of the chunk, or column of the state
         const uint32_t lanes = tmem + (quarter << 21), at0 = panel_at(row, 2 * part), at1 = panel_at(row, 2 * part + 1);   // this thread's 16 of 64 columns
@@ -329,59 +376,21 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
             }
             put(Lay::st, pl, NO);
         };
-        // Panels of an operand's rows for a chunk: a thread copies two chunks of 16 bytes a panel, eight threads a row of 128 bytes.  What does not
-        // change from chunk to chunk: the place in the panel, the bytes that exist, the row to start from.
-        const int r0 = (int)(tid >> 3), col = (int)(tid & 7) * 8;
-        const uint32_t to = base + panel_at(r0, tid & 7);
-        const int t_first = a.backwards ? t_hi - 1 : t_lo;
-        struct Rows {
-            const T* p;
-            long long step;      // 64 rows on
-            int width;
-        };
-        auto rows = [&](const ScanOperand& o, int width) {
-            return Rows{chunks ? scan_row<T>(o, b, t_first + dir * r0, head, group, tile) + col : nullptr, (long long)dir * 64 * o.st, width - col};
-        };
-        auto fetch = [&](Rows& r, uint32_t panel, int n, int valid) {
-#pragma unroll
-            for (int j = 0; j < n; j++) {
-                const int bytes = min(max(r.width - 64 * j, 0), 8) * 2;
-                const uint32_t dst = to + (panel + j) * PANEL;
-                if (valid == TC_Q && bytes == 16) {
-                    cp_async16(dst, r.p + 64 * j), cp_async16(dst + 8192, r.p + r.step + 64 * j);
-                } else {
-                    // a row that does not exist is not read: zero bytes of an address that does
-                    const int n0 = r0 < valid ? bytes : 0, n1 = r0 + 64 < valid ? bytes : 0;
-                    cp_async16_part(dst, n0 ? r.p + 64 * j : (const T*)a.g, n0), cp_async16_part(dst + 8192, n1 ? r.p + r.step + 64 * j : (const T*)a.g, n1);
-                }
-            }
-            r.p += 2 * r.step;
-        };
-        auto left = [&](int c) { return min(TC_Q, t_hi - t_lo - c * TC_Q); };
-        Rows fb = rows(ob, (int)a.N), fn = rows(on, pw), fq = MODE ? rows(a.q, qw) : Rows{nullptr, 0, 0};
         auto arrive = [&](uint32_t which) {
             __syncwarp();
             if (lane == 0) mbar_arrive(which);
         };
         float diag = 0.f;
         const float skip = Lay::OUT && a.skip ? a.skip[head] : 0.f;
-        if (chunks) {
-            if (MODE) fetch(fq, Lay::q, Lay::QP, left(0));
-            fetch(fb, Lay::broad, 2, left(0));
-            fetch(fn, Lay::narrow, 1, left(0));
-            if (MODE) put_state();
-            cp_async_wait();
+        if (MODE && chunks) {
+            put_state();
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            arrive(b_load);
+            arrive(b_st);
         }
         for (int c = 0; c < chunks; c++) {
             const int valid = left(c), set = c & 1;
             const TcDecays& d = decays[set];
-            wait(b_load, c);                     // everyone's copies have landed, no one needs the other set any more
-            if (c + 1 < chunks) {
-                fetch(fb, Lay::broad + 2 * (set ^ 1), 2, left(c + 1));
-                fetch(fn, Lay::narrow + (set ^ 1), 1, left(c + 1));
-            }
+            wait(b_load, c);
             wait(b_g + 8 * set, c >> 1);
             {
                 const float f = d.fade[row];
@@ -400,60 +409,60 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
                 // decayed scores of this row and the columns 32 part .. 32 part + 31
                 wait(b_s, c);                       // S and O1
                 tc_after();
-                uint32_t x[32];
-                if (part <= quarter) {
-                    tc_ld32(x, lanes + Lay::S + 32 * part);
-                    tc_wait_ld();
-                }
-                tc_before();
-                bar_sync(2 + quarter, 128);         // the other warps of these rows have their scores too
-                tc_after();
-                if (c + 1 < chunks) fetch(fq, Lay::q, Lay::QP, left(c + 1));     // O1 is done, too
                 const float2 ci = d.cum[row];
                 // whole loops per case: a branch inside would keep the columns from overlapping
-                auto store = [&](const uint32_t (&pl)[8][NO], int h) {
+                auto read = [&](f2 (&x)[8], int h) {
+                    uint32_t u[16];
+                    tc_ld16(u, lanes + Lay::S + 32 * part + 16 * h);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 8; e++) x[e] = {__uint_as_float(u[2 * e]), __uint_as_float(u[2 * e + 1])};
+                };
+                auto write = [&](const uint32_t (&pl)[8][NO], int h) {
 #pragma unroll
                     for (int p = 0; p < NO; p++) {
                         uint32_t q[8];
 #pragma unroll
                         for (int e = 0; e < 8; e++) q[e] = pl[e][p];
-                        tc_st8(lanes + Lay::P + 64 * p + 16 * part + 8 * h, q);
+                        tc_st8(lanes + (p < 2 ? Lay::S + 32 * part + 16 * h + 8 * p : Lay::P3 + 16 * part + 8 * h), q);
                     }
                 };
                 if (part < quarter) {
                     const float r = ex2((ci.x - d.ref[part].x) + (ci.y - d.ref[part].y));
 #pragma unroll
                     for (int h = 0; h < 2; h++) {
+                        f2 x[8];
                         uint32_t pl[8][NO];
+                        read(x, h);
 #pragma unroll
                         for (int e = 0; e < 8; e += 2) {
-                            const int j = 16 * h + 2 * e;
-                            const float4 tl = *reinterpret_cast<const float4*>(&d.tail[32 * part + j]);
-                            split2<NO>(mul2({__uint_as_float(x[j]), __uint_as_float(x[j + 1])}, mul2({r, r}, {tl.x, tl.y})), pl[e]);
-                            split2<NO>(mul2({__uint_as_float(x[j + 2]), __uint_as_float(x[j + 3])}, mul2({r, r}, {tl.z, tl.w})), pl[e + 1]);
+                            const float4 tl = *reinterpret_cast<const float4*>(&d.tail[32 * part + 16 * h + 2 * e]);
+                            split2<NO>(mul2(x[e], mul2({r, r}, {tl.x, tl.y})), pl[e]);
+                            split2<NO>(mul2(x[e + 1], mul2({r, r}, {tl.z, tl.w})), pl[e + 1]);
                         }
-                        store(pl, h);
+                        write(pl, h);
                     }
                 } else if (part == quarter) {
 #pragma unroll
                     for (int h = 0; h < 2; h++) {
+                        f2 x[8];
                         uint32_t pl[8][NO];
+                        read(x, h);
 #pragma unroll
                         for (int e = 0; e < 8; e++) {
                             const int j = 16 * h + 2 * e;
                             const float4 cj = *reinterpret_cast<const float4*>(&d.cum[32 * part + j]);
                             const f2 d0 = fma2({cj.x, cj.y}, {-1.f, -1.f}, {ci.x, ci.y}), d1 = fma2({cj.z, cj.w}, {-1.f, -1.f}, {ci.x, ci.y});
-                            f2 v = {__uint_as_float(x[j]), __uint_as_float(x[j + 1])};
-                            if (Lay::GRAD) diag += (lane == j ? v.x : 0.f) + (lane == j + 1 ? v.y : 0.f);
-                            v = mul2(v, {ex2(d0.x + d0.y), ex2(d1.x + d1.y)});
+                            if (Lay::GRAD) diag += (lane == j ? x[e].x : 0.f) + (lane == j + 1 ? x[e].y : 0.f);
+                            f2 v = mul2(x[e], {ex2(d0.x + d0.y), ex2(d1.x + d1.y)});
                             v.x = j <= lane ? v.x : 0.f, v.y = j + 1 <= lane ? v.y : 0.f;
                             split2<NO>(v, pl[e]);
                         }
-                        store(pl, h);
+                        write(pl, h);
                     }
                 } else {
                     const uint32_t pl[8][NO] = {};
-                    store(pl, 0), store(pl, 1);
+                    write(pl, 0), write(pl, 1);
                 }
                 tc_wait_st();
                 tc_before();
@@ -475,24 +484,26 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
                     st[e] = fma2(st[e], {keep, keep}, v);
                 }
             }
-            if (MODE && c + 1 < chunks) put_state();
-            uint32_t skipped[8] = {};
-            if (Lay::OUT && a.skip) {
-                const uint8_t* src = panels + (Lay::narrow + set) * PANEL;
-                const uint4 v0 = *reinterpret_cast<const uint4*>(src + at0), v1 = *reinterpret_cast<const uint4*>(src + at1);
-                skipped[0] = v0.x, skipped[1] = v0.y, skipped[2] = v0.z, skipped[3] = v0.w, skipped[4] = v1.x, skipped[5] = v1.y, skipped[6] = v1.z, skipped[7] = v1.w;
-            }
-            cp_async_wait();
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             tc_before();
-            if (c + 1 < chunks) arrive(b_load);
+            if (!MODE) {
+                arrive(b_used + 8 * set);
+                continue;
+            }
+            if (c + 1 < chunks) {
+                put_state();
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                arrive(b_st);
+            }
             const float grow = d.grow[row];
-            arrive(b_used + 8 * set);
-            if (!MODE) continue;
-
             const bool live = (int)row < valid;
             const long long t = t_first + (long long)dir * (c * TC_Q + (int)row);
             if (Lay::OUT) {
+                uint32_t skipped[8] = {};
+                if (a.skip) {
+                    const uint8_t* src = panels + (Lay::narrow + set) * PANEL;
+                    const uint4 v0 = *reinterpret_cast<const uint4*>(src + at0), v1 = *reinterpret_cast<const uint4*>(src + at1);
+                    skipped[0] = v0.x, skipped[1] = v0.y, skipped[2] = v0.z, skipped[3] = v0.w, skipped[4] = v1.x, skipped[5] = v1.y, skipped[6] = v1.z, skipped[7] = v1.w;
+                }
                 wait(b_o, c);
                 tc_after();
                 uint32_t x[16], x1[16], y[16];
@@ -501,7 +512,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
                 tc_ld16(y, lanes + Lay::O2 + 16 * part);
                 tc_wait_ld();
                 tc_before();
-                arrive(b_epi);
+                arrive(b_used + 8 * set);
                 T* out = (T*)a.out + b * a.ob + t * a.ot + head * a.oh + tile * SCAN_TILE + 16 * part;
                 const int count = live ? vw - 16 * (int)part : 0;
                 uint32_t o[8];
@@ -552,7 +563,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
                     tc_wait_ld();
                     if (k == 1) {
                         tc_before();
-                        arrive(b_epi);
+                        arrive(b_used + 8 * set);
                     }
 #pragma unroll
                     for (int e = 0; e < 8; e++) {
