@@ -213,7 +213,7 @@ struct ScanShape {
 // values, and a state written and read) or one on tcgen05 (chunks of 128).
 static ScanShape scan_shape(const fesc_clear_scan_desc* d) {
     ScanShape s;
-    s.tc = d->type == FESC_BF16 && d->N > 64;
+    s.tc = d->type == FESC_BF16 && d->N > 64 && d->N % 8 == 0 && d->P % 8 == 0;
     s.tiles = (d->P + SCAN_TILE - 1) / SCAN_TILE, s.vheads = d->H * s.tiles, s.np = d->N > 64 ? 128 : 64;
     // in pieces of 128 tokens
     const uint64_t pieces = ((uint64_t)d->L + 127) / 128, ctas = (uint64_t)d->batch * s.vheads;
@@ -321,7 +321,7 @@ extern "C" int fesc_clear_scan(const fesc_clear_scan_desc* desc, const void* d_x
     const uint32_t bytes = clear_type_bytes(d.type);
     ScanArgs a = scan_args(desc, s, d_g, d_lengths);
     a.q = operand(d_C, d.C, false, bytes), a.k = operand(d_B, d.B, false, bytes), a.v = operand(d_x, d.x, true, bytes);
-    const bool tc = s.tc && a.q.wide && a.k.wide && a.v.wide;
+    const bool tc = s.tc && a.q.wide && a.k.wide && a.v.wide && out_width(d_y, d.y, bytes);
     a.init = d_h0;
     if (s.segments > 1) {
         float* states = (float*)d_work;
@@ -375,7 +375,7 @@ extern "C" int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const 
     const uint32_t bytes = clear_type_bytes(d.type);
     const ScanOperand x = operand(d_x, d.x, true, bytes), B = operand(d_B, d.B, false, bytes), C = operand(d_C, d.C, false, bytes),
                       dy = operand(d_dy, d.y, true, bytes);
-    const bool tc = s.tc && x.wide && B.wide && C.wide && dy.wide;
+    const bool tc = s.tc && x.wide && B.wide && C.wide && dy.wide && out_width(d_dx, d.dx, bytes);
     const ScanArgs base = scan_args(desc, s, d_g, d_lengths);
     const float *h = d_h0, *dh = d_dh_out;
     if (s.segments > 1) {

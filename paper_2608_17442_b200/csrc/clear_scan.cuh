@@ -495,6 +495,6 @@ cudaError_t scan_launch(const ScanArgs& a, int mode, cudaStream_t st) {
 extern template cudaError_t scan_launch<__nv_bfloat16>(const ScanArgs&, int, cudaStream_t);
 extern template cudaError_t scan_launch<__half>(const ScanArgs&, int, cudaStream_t);
 extern template cudaError_t scan_launch<float>(const ScanArgs&, int, cudaStream_t);
-// the same on tcgen05: bfloat16, states of 65 to 128 columns, operands with 16-byte rows (clear_scan_tc.cu); dots then has SCAN_DOTS parts a head tile
+// the same on tcgen05: bfloat16, states of 65 to 128 columns, N and P multiples of 8, operands and outputs with 16-byte rows (clear_scan_tc.cu); dots then has SCAN_DOTS parts a head tile
 #define SCAN_DOTS 4
 cudaError_t scan_tc_launch(const ScanArgs& a, int mode, cudaStream_t st);

@@ -60,6 +60,10 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// The longer part of a wait, out of line: the kernel has some thirty of them, and its instructions have to stay in the cache of one SM.
+static __device__ __noinline__ void wait_on(uint32_t bar, uint32_t parity, volatile uint32_t* dead) {
+    if (!*dead && mbar_wait_bounded(bar, parity)) *dead = 1, g_clear_status = 1;
+}
 // bytes of (row, 16-byte chunk c of eight) in a panel
 __device__ __forceinline__ uint32_t panel_at(uint32_t row, uint32_t c) { return row * 128 + ((c ^ (row & 7)) << 4); }
 
@@ -201,8 +205,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
     const int chunks = t_hi > t_lo ? (t_hi - t_lo + TC_Q - 1) / TC_Q : 0, dir = a.backwards ? -1 : 1;
     const int t_first = a.backwards ? t_hi - 1 : t_lo;
     auto wait = [&](uint32_t which, uint32_t parity) {
-        if (mbar_try_wait(which, parity & 1)) return;
-        if (!dead && mbar_wait_bounded(which, parity & 1)) dead = 1, g_clear_status = 1;
+        if (!mbar_try_wait(which, parity & 1)) wait_on(which, parity & 1, &dead);
     };
 
     if (warp == TC_WARPS) {
@@ -315,32 +318,36 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
             pb = scan_row<T>(ob, b, t_first + dir * (int)r0, head, group, tile) + col, pn = scan_row<T>(on, b, t_first + dir * (int)r0, head, group, tile) + col;
             if (MODE) pq = scan_row<T>(a.q, b, t_first + dir * (int)r0, head, group, tile) + col;
         }
-        // one panel of a chunk; what does not exist is not read: zero bytes of an address that does
-        auto copy = [&](uint32_t panel, const T* p, long long step, int width, int valid) {
-            const int bytes = min(max(width - (int)col, 0), 8) * 2;
-            const uint32_t dst = to + panel * PANEL;
-            if (valid == TC_Q && bytes == 16) {
+        // panels first .. first + n - 1 of a chunk; what does not exist is not read: zero bytes of an address that does
+        auto copy = [&](uint32_t first, int n, const T* src, long long step, int width, int valid) {
+#pragma unroll 1
+            for (int j = 0; j < n; j++, src += 64, width -= 64) {
+                const int bytes = min(max(width - (int)col, 0), 8) * 2;
+                const uint32_t dst = to + (first + j) * PANEL;
+                const T* p = src;
+                if (valid == TC_Q && bytes == 16) {
 #pragma unroll 8
-                for (uint32_t i = 0; i < TC_Q / 8; i++, p += step) cp_async16(dst + 1024 * i, p);
-            } else {
-                for (uint32_t i = 0; i < TC_Q / 8; i++, p += step) {
-                    const int n = (int)(r0 + 8 * i) < valid ? bytes : 0;
-                    cp_async16_part(dst + 1024 * i, n ? p : (const T*)a.g, n);
+                    for (uint32_t i = 0; i < TC_Q / 8; i++, p += step) cp_async16(dst + 1024 * i, p);
+                } else {
+#pragma unroll 1
+                    for (uint32_t i = 0; i < TC_Q / 8; i++, p += step) {
+                        const int some = (int)(r0 + 8 * i) < valid ? bytes : 0;
+                        cp_async16_part(dst + 1024 * i, some ? p : (const T*)a.g, some);
+                    }
                 }
             }
         };
+        const long long sb = 8 * dir * ob.st, sn = 8 * dir * on.st, sq = 8 * dir * a.q.st;
         for (int c = 0; c < chunks; c++) {
             const uint32_t set = c & 1;
             if (c >= 2) wait(b_used + 8 * set, (c >> 1) - 1);
-            const long long sb = 8 * dir * ob.st, sn = 8 * dir * on.st, sq = 8 * dir * a.q.st, done = (long long)c * (TC_Q / 8);
-            copy(Lay::broad + 2 * set, pb + done * sb, sb, (int)a.N, left(c));
-            copy(Lay::broad + 2 * set + 1, pb + done * sb + 64, sb, (int)a.N - 64, left(c));
-            copy(Lay::narrow + set, pn + done * sn, sn, pw, left(c));
+            copy(Lay::broad + 2 * set, 2, pb, sb, (int)a.N, left(c));
+            copy(Lay::narrow + set, 1, pn, sn, pw, left(c));
             if (MODE) {
                 if (c) wait(b_s, c - 1);
-                copy(Lay::q, pq + done * sq, sq, qw, left(c));
-                if (Lay::QP == 2) copy(Lay::q + 1, pq + done * sq + 64, sq, qw - 64, left(c));
+                copy(Lay::q, Lay::QP, pq, sq, qw, left(c));
             }
+            pb += sb * (TC_Q / 8), pn += sn * (TC_Q / 8), pq += sq * (TC_Q / 8);
             cp_async_wait();
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
@@ -524,13 +531,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
                 }
                 if (a.out_wide > 1 && count >= 16) {
                     st32(out, o);
-                } else if (a.out_wide && count % 8 == 0) {
+                } else {
                     if (count >= 8) *reinterpret_cast<uint4*>(out) = make_uint4(o[0], o[1], o[2], o[3]);
                     if (count >= 16) *reinterpret_cast<uint4*>(out + 8) = make_uint4(o[4], o[5], o[6], o[7]);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 16; e++)
-                        if (e < count) reinterpret_cast<uint16_t*>(out)[e] = (uint16_t)(o[e / 2] >> (e & 1 ? 16 : 0));
                 }
             } else {
                 // u's part of the row is on its way while the products finish
@@ -538,17 +541,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
                 const T* pu = scan_row<T>(a.u, b, t_first + (long long)dir * (c * TC_Q + min((int)row, valid - 1)), head, group, tile) + 32 * part;
 #pragma unroll
                 for (int k = 0; k < 4; k++) {
-                    const int count = (int)a.N - 32 * (int)part - 8 * k;
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (a.u.wide && count >= 8) v = *reinterpret_cast<const uint4*>(pu + 8 * k);
-                    else {
-                        uint32_t h[4];
-#pragma unroll
-                        for (int e = 0; e < 4; e++)
-                            h[e] = (2 * e < count ? (uint32_t)reinterpret_cast<const uint16_t*>(pu)[8 * k + 2 * e] : 0u) |
-                                   (2 * e + 1 < count ? (uint32_t)reinterpret_cast<const uint16_t*>(pu)[8 * k + 2 * e + 1] << 16 : 0u);
-                        v = make_uint4(h[0], h[1], h[2], h[3]);
-                    }
+                    const uint4 v = 32 * part + 8 * k < a.N ? *reinterpret_cast<const uint4*>(pu + 8 * k) : make_uint4(0, 0, 0, 0);
                     u[4 * k] = v.x, u[4 * k + 1] = v.y, u[4 * k + 2] = v.z, u[4 * k + 3] = v.w;
                 }
                 wait(b_o, c);
