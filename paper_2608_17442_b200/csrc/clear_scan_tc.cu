@@ -38,7 +38,7 @@ struct TcLayout {
     // Columns of tensor memory, all 512 with outputs.  The first two planes of 16 decayed scores lie over the 16 scores, so a warp overwrites what it
     // has read itself; a third plane has columns of its own.
     static constexpr uint32_t DV = GRAD ? 128 : 64, O1_PARTS = OUT ? 2 : 1, H_PARTS = GRAD ? 1 : 3;      // accumulators side by side, one per plane
-    static constexpr uint32_t S = 0, P3 = 128, O1 = GRAD ? 192 : 128, O2 = O1 + O1_PARTS * DV, H = MODE ? O2 + DV : 0, columns = MODE ? 512 : 256;
+    static constexpr uint32_t S = 0, P3 = 128, O1 = GRAD ? 192 : 128, O2 = O1 + O1_PARTS * DV, H = MODE ? O2 + DV : 0, columns = 512;
     static_assert(H + 64 * H_PARTS <= columns, "accumulators fit");
     static constexpr size_t bytes = (size_t)panels * PANEL + 1024;  // panels start on 1024 bytes
 };
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
     tc_before();
     __syncthreads();
     tc_after();
-    const uint32_t tmem = tmem_base;
+    constexpr uint32_t tmem = 0;            // all 512 columns: they begin at 0
     auto left = [&](int c) { return min(TC_Q, t_hi - t_lo - c * TC_Q); };      // tokens of a chunk
     const int chunks = t_hi > t_lo ? (t_hi - t_lo + TC_Q - 1) / TC_Q : 0, dir = a.backwards ? -1 : 1;
     const int t_first = a.backwards ? t_hi - 1 : t_lo;
@@ -214,55 +214,53 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
         constexpr uint32_t I_S = IDESC | (16u << 17), I_H = IDESC | (1u << 15) | (1u << 16) | ((8u * Lay::H_PARTS) << 17);
         constexpr uint32_t I_O1 = IDESC | (16u << 17) | (Lay::GRAD ? 0 : 1u << 16), I_O2 = IDESC | (1u << 16) | ((Lay::DV / 8) << 17);
         constexpr uint32_t STEP = PANEL >> 4, QK = Lay::OUT ? 8 : 4;                        // steps of 16 along q's columns
-        if (lane == 0) {
-            const uint32_t pq = tc_desc(base + Lay::q * PANEL), pw_ = tc_desc(base + Lay::w * PANEL), ps = tc_desc(base + Lay::st * PANEL);
-            for (int c = 0; c < chunks; c++) {
-                const uint32_t set = c & 1;
-                const uint32_t pb = tc_desc(base + (Lay::broad + 2 * set) * PANEL), pn = tc_desc(base + (Lay::narrow + set) * PANEL);
-                if (MODE) {
-                    wait(b_load, c);
-                    if (c) wait(b_o, c - 1);                             // the scores' planes lie over the scores
-                    tc_after();
-                    if (!dead) {
-#pragma unroll
-                        for (uint32_t k = 0; k < QK; k++) {
-                            const uint32_t at = (k >> 2) * STEP + (k & 3) * 2;
-                            tc_mma_ss(tmem + Lay::S, pq + at, (Lay::OUT ? pb : pn) + at, I_S, k);
-                        }
-                    }
-                    wait(b_st, c);
-                    if (c) wait(b_used + 8 * (set ^ 1), (c - 1) >> 1);
-                    tc_after();
-                    if (!dead) {
-#pragma unroll
-                        for (uint32_t p = 0; p < (Lay::OUT ? 1 : NO); p++)
-#pragma unroll
-                            for (uint32_t k = 0; k < QK; k++)
-                                tc_mma_ss(tmem + Lay::O1, pq + (k >> 2) * STEP + (k & 3) * 2, ps + p * STEP + (Lay::OUT ? k * 128 : k * 2), I_O1, p || k);
-                        tc_commit(b_s);
-                    }
-                }
-                wait(b_wv, c);
+        // One thread issues, and what it computes per product counts: the set of operands is known when compiled, so addresses are sums with constants.
+        const uint32_t d0 = tc_desc(base);
+        auto chunk = [&](int c, auto which) {
+            constexpr uint32_t set = decltype(which)::value;
+            const uint32_t pq = d0 + Lay::q * STEP, pw_ = d0 + Lay::w * STEP, ps = d0 + Lay::st * STEP, pb = d0 + (Lay::broad + 2 * set) * STEP,
+                           pn = d0 + (Lay::narrow + set) * STEP;
+            if (MODE) {
+                wait(b_load, c);
+                if (c) wait(b_o, c - 1);                             // the scores' planes lie over the scores
                 tc_after();
-                if (!dead) {
 #pragma unroll
-                    for (uint32_t p = 0; p < (Lay::H_PARTS == 1 ? NS : 1); p++)
-#pragma unroll
-                        for (uint32_t k = 0; k < 8; k++) tc_mma_ss(tmem + Lay::H, pb + k * 128, pw_ + p * STEP + k * 128, I_H, p || k);
-                    tc_commit(b_h);
+                for (uint32_t k = 0; k < QK; k++) {
+                    const uint32_t at = (k >> 2) * STEP + (k & 3) * 2;
+                    tc_mma_ss(tmem + Lay::S, pq + at, (Lay::OUT ? pb : pn) + at, I_S, k);
                 }
-                if (MODE) {
-                    wait(b_p, c);
-                    tc_after();
-                    if (!dead) {
+                wait(b_st, c);
+                if (c) wait(b_used + 8 * (set ^ 1), (c - 1) >> 1);
+                tc_after();
 #pragma unroll
-                        for (uint32_t p = 0; p < NO; p++)
+                for (uint32_t p = 0; p < (Lay::OUT ? 1 : NO); p++)
 #pragma unroll
-                            for (uint32_t k = 0; k < 8; k++)
-                                tc_mma_ts(tmem + Lay::O2, tmem + (p < 2 ? Lay::S + 16 * k + 8 * p : Lay::P3 + 8 * k), (Lay::GRAD ? pb : pn) + k * 128, I_O2, p || k);
-                        tc_commit(b_o);
-                    }
-                }
+                    for (uint32_t k = 0; k < QK; k++)
+                        tc_mma_ss(tmem + Lay::O1, pq + (k >> 2) * STEP + (k & 3) * 2, ps + p * STEP + (Lay::OUT ? k * 128 : k * 2), I_O1, p || k);
+                tc_commit(b_s);
+            }
+            wait(b_wv, c);
+            tc_after();
+#pragma unroll
+            for (uint32_t p = 0; p < (Lay::H_PARTS == 1 ? NS : 1); p++)
+#pragma unroll
+                for (uint32_t k = 0; k < 8; k++) tc_mma_ss(tmem + Lay::H, pb + k * 128, pw_ + p * STEP + k * 128, I_H, p || k);
+            tc_commit(b_h);
+            if (MODE) {
+                wait(b_p, c);
+                tc_after();
+#pragma unroll
+                for (uint32_t p = 0; p < NO; p++)
+#pragma unroll
+                    for (uint32_t k = 0; k < 8; k++)
+                        tc_mma_ts(tmem + Lay::O2, tmem + (p < 2 ? Lay::S + 16 * k + 8 * p : Lay::P3 + 8 * k), (Lay::GRAD ? pb : pn) + k * 128, I_O2, p || k);
+                tc_commit(b_o);
+            }
+        };
+        if (lane == 0) {
+            for (int c = 0; c < chunks; c += 2) {
+                chunk(c, std::integral_constant<uint32_t, 0>());
+                if (c + 1 < chunks) chunk(c + 1, std::integral_constant<uint32_t, 1>());
             }
             tc_commit(drained);
             mbar_wait_bounded(drained, 0);
@@ -355,7 +353,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
         }
     } else {
         const uint32_t quarter = warp & 3, part = warp >> 2, row = 32 * quarter + lane;     // row: token of the chunk, or column of the state
-        const uint32_t lanes = tmem + (quarter << 21), at0 = panel_at(row, 2 * part), at1 = panel_at(row, 2 * part + 1);   // this thread's 16 of 64 columns
+        const uint32_t lanes = quarter << 21, at0 = panel_at(row, 2 * part), at1 = panel_at(row, 2 * part + 1);   // this thread's 16 of 64 columns
         f2 st[8];                                                                            // state[channel 16 part + i][column row]
         const float* init = MODE && a.init ? a.init + (a.segments > 1 ? slot : b) * states + state_at : nullptr;
 #pragma unroll
@@ -603,7 +601,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const ScanArgs 
     tc_before();
     __syncthreads();
     tc_after();
-    if (warp == TC_WARPS) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(Lay::columns));
+    if (warp == TC_WARPS) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "n"(Lay::columns));
 }
 
 cudaError_t scan_tc_launch(const ScanArgs& a, int mode, cudaStream_t st) {
