@@ -18,12 +18,19 @@ int clear_fail(int code, const char* what) {
 }
 extern "C" const char* fesc_clear_last_error(void) { return clear_error.c_str(); }
 
-// Chains the segments: slot s gets the state before segment s (in the sweep's direction) and what the segment adds goes into the chain.
-__global__ void __launch_bounds__(256) k_clear_combine(float* states, const float* decay, const float* init, uint32_t segments, uint32_t per_head,
-                                                       size_t per_b, uint32_t backwards) {
+// Chains the segments: slot s gets the state before segment s (in the sweep's direction) and what the segment adds goes into the chain.  blockIdx.z:
+// forwards, backwards.
+struct Chain {
+    float* states;
+    const float *decay, *init;
+};
+__global__ void __launch_bounds__(256) k_clear_combine(const Chain forwards, const Chain back, uint32_t segments, uint32_t per_head, size_t per_b) {
     pdl_begin();
     const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
     const uint32_t b = blockIdx.y;
+    const bool backwards = blockIdx.z;
+    float* const states = backwards ? back.states : forwards.states;
+    const float *const decay = backwards ? back.decay : forwards.decay, *const init = backwards ? back.init : forwards.init;
     if (i >= per_b) return;
     float* s = states + (size_t)b * segments * per_b + i;
     const uint32_t H = (uint32_t)(per_b / per_head), n = (uint32_t)(per_b - i < 4 ? per_b - i : 4);
@@ -239,7 +246,7 @@ static const char* scan_check(const fesc_clear_scan_desc* d) {
     if (d->N > SCAN_MAX_STATE) return "clear_scan: states of more than 128 columns";
     if (d->P > 4096 || d->L >= (1u << 30)) return "clear_scan: more than 4096 channels of a head or 2^30 tokens";
     const ScanShape s = scan_shape(d);
-    if ((uint64_t)d->batch * s.segments * s.vheads >= (1ull << 31) || d->batch > 65535 || (uint64_t)d->batch * d->L * d->G * 32 >= (1ull << 38))
+    if (3 * (uint64_t)d->batch * s.segments * s.vheads >= (1ull << 31) || d->batch > 65535 || (uint64_t)d->batch * d->L * d->G * 32 >= (1ull << 38))
         return "clear_scan: too many sequences, heads or tokens for one call";
     return nullptr;
 }
@@ -279,15 +286,15 @@ static ScanArgs scan_args(const fesc_clear_scan_desc* d, const ScanShape& s, con
     a.tiles = s.tiles, a.segments = s.segments, a.seg_chunks = s.seg_chunks;
     return a;
 }
-static cudaError_t scan_go(const fesc_clear_scan_desc* d, bool tc, const ScanArgs& a, int mode, cudaStream_t st) {
+static cudaError_t scan_go(const fesc_clear_scan_desc* d, bool tc, const ScanSet& a, int mode, cudaStream_t st) {
     return tc                    ? scan_tc_launch(a, mode, st)
          : d->type == FESC_BF16 ? scan_launch<__nv_bfloat16>(a, mode, st)
          : d->type == FESC_F16  ? scan_launch<__half>(a, mode, st)
                                 : scan_launch<float>(a, mode, st);
 }
-static cudaError_t combine(const fesc_clear_scan_desc* d, const ScanShape& s, float* states, const float* decay, const float* init, bool backwards, cudaStream_t st) {
-    return launch(k_clear_combine, dim3((uint32_t)((s.states + 1023) / 1024), d->batch), dim3(256), 0, st, states, decay, init, s.segments, d->P * d->N, s.states,
-                  (uint32_t)backwards);
+static cudaError_t combine(const fesc_clear_scan_desc* d, const ScanShape& s, const Chain& forwards, const Chain& back, cudaStream_t st) {
+    return launch(k_clear_combine, dim3((uint32_t)((s.states + 1023) / 1024), d->batch, back.states ? 2 : 1), dim3(256), 0, st, forwards, back, s.segments, d->P * d->N,
+                  s.states);
 }
 
 extern "C" size_t fesc_clear_scan_work(const fesc_clear_scan_desc* desc) {
@@ -327,13 +334,13 @@ extern "C" int fesc_clear_scan(const fesc_clear_scan_desc* desc, const void* d_x
         float* states = (float*)d_work;
         float* decay = states + s.state_floats;
         a.last = states, a.decay = decay;
-        CLEAR_CUDA(scan_go(desc, tc, a, MODE_STATE, st));
-        CLEAR_CUDA(combine(desc, s, states, decay, d_h0, false, st));
+        CLEAR_CUDA(scan_go(desc, tc, {{a}, 1}, MODE_STATE, st));
+        CLEAR_CUDA(combine(desc, s, {states, decay, d_h0}, {}, st));
         a.init = states;
     }
     a.last = d_h_out, a.skip = d_skip, a.out = d_y, a.ob = d.y[0], a.ot = d.y[1], a.oh = d.y[2];
     a.out_wide = out_width(d_y, d.y, bytes);
-    CLEAR_CUDA(scan_go(desc, tc, a, MODE_OUT, st));
+    CLEAR_CUDA(scan_go(desc, tc, {{a}, 1}, MODE_OUT, st));
     return FESC_OK;
 }
 
@@ -379,25 +386,21 @@ extern "C" int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const 
     const ScanArgs base = scan_args(desc, s, d_g, d_lengths);
     const float *h = d_h0, *dh = d_dh_out;
     if (s.segments > 1) {
-        ScanArgs a = base;
-        a.k = B, a.v = x, a.last = before, a.decay = decay;
-        CLEAR_CUDA(scan_go(desc, tc, a, MODE_STATE, st));
-        a.k = C, a.v = dy, a.last = behind, a.decay = decay_back, a.backwards = 1;
-        CLEAR_CUDA(scan_go(desc, tc, a, MODE_STATE, st));
-        CLEAR_CUDA(combine(desc, s, before, decay, d_h0, false, st));
-        CLEAR_CUDA(combine(desc, s, behind, decay_back, d_dh_out, true, st));
+        ScanSet states = {{base, base}, 2};
+        states.a[0].k = B, states.a[0].v = x, states.a[0].last = before, states.a[0].decay = decay;
+        states.a[1].k = C, states.a[1].v = dy, states.a[1].last = behind, states.a[1].decay = decay_back, states.a[1].backwards = 1;
+        CLEAR_CUDA(scan_go(desc, tc, states, MODE_STATE, st));
+        CLEAR_CUDA(combine(desc, s, {before, decay, d_h0}, {behind, decay_back, d_dh_out}, st));
         h = before, dh = behind;
     }
-    ScanArgs a = base;                  // dC
-    a.q = dy, a.k = x, a.v = B, a.u = C, a.init = h, a.meet = dh, a.part = part_c, a.dots = row, a.ends = ends, a.diag = diag;
-    CLEAR_CUDA(scan_go(desc, tc, a, MODE_GRAD, st));
-    a = base;                           // dB
-    a.q = x, a.k = dy, a.v = C, a.u = B, a.init = dh, a.part = part_b, a.dots = col, a.backwards = 1;
-    CLEAR_CUDA(scan_go(desc, tc, a, MODE_GRAD, st));
-    a = base;                           // dx, and the gradient of the state before the first token
-    a.q = B, a.k = C, a.v = dy, a.init = dh, a.last = d_dh0, a.skip = d_skip, a.out = d_dx, a.ob = d.dx[0], a.ot = d.dx[1], a.oh = d.dx[2];
-    a.out_wide = out_width(d_dx, d.dx, bytes), a.backwards = 1;
-    CLEAR_CUDA(scan_go(desc, tc, a, MODE_OUT, st));
+    ScanSet set = {{base, base, base}, 3};
+    ScanArgs &c = set.a[0], &b = set.a[1], &o = set.a[2];
+    c.q = dy, c.k = x, c.v = B, c.u = C, c.init = h, c.meet = dh, c.part = part_c, c.dots = row, c.ends = ends, c.diag = diag;      // dC
+    b.q = x, b.k = dy, b.v = C, b.u = B, b.init = dh, b.part = part_b, b.dots = col, b.backwards = 1;                               // dB
+    // dx, and the gradient of the state before the first token
+    o.q = B, o.k = C, o.v = dy, o.init = dh, o.last = d_dh0, o.skip = d_skip, o.out = d_dx, o.ob = d.dx[0], o.ot = d.dx[1], o.oh = d.dx[2];
+    o.out_wide = out_width(d_dx, d.dx, bytes), o.backwards = 1;
+    CLEAR_CUDA(scan_go(desc, tc, set, MODE_GRAD, st));
     FinishArgs f = {};
     f.part_b = part_b, f.part_c = part_c, f.row = row, f.col = col, f.ends = ends, f.diag = diag;
     f.dB = d_dB, f.dC = d_dC, f.dg = d_dg, f.dskip = d_dskip, f.lengths = d_lengths, f.g = d_g, f.ib = d.g[0], f.it = d.g[1], f.ih = d.g[2];

@@ -54,7 +54,13 @@ struct ScanArgs {
     uint32_t b, L, H, P, G, N, tiles, segments, seg_chunks, backwards;
 };
 
-// the text of an operand's row: token t of sequence b for head h, tile s
+// The sweeps of a launch: MODE_STATE one or two, MODE_OUT one, MODE_GRAD three (dC, dB, and dx as MODE_OUT).  Heads, tokens and segments are the same.
+struct ScanSet {
+    ScanArgs a[3];
+    uint32_t count;
+};
+
+// an operand's row: token t of sequence b for head h, tile s
 template <class T>
 __device__ __forceinline__ const T* scan_row(const ScanOperand& o, uint32_t b, long long t, uint32_t head, uint32_t group, uint32_t tile) {
     return (const T*)o.p + b * o.sb + t * o.st + (o.tiled ? head * o.sh + tile * SCAN_TILE : group * o.sh);
@@ -125,17 +131,16 @@ struct ScanShared {
 };
 
 template <class T, int DK, int DV, int MODE>
-__global__ void __launch_bounds__(128) k_clear_scan(const ScanArgs a) {
+__device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
     using S = ScanShared<T, DK, DV, MODE>;
     constexpr int NI = S::NI, NO = S::NO, NS = 3, MT = DV / 64, KT = DK / 8;
     extern __shared__ __align__(128) __nv_bfloat16 sm[];
     __shared__ __align__(16) float2 cum[SCAN_Q];               // log2 of the decay up to a token of the chunk, as a sum of two floats
     __shared__ __align__(16) float grow[SCAN_Q], fade[SCAN_Q]; // decay from the chunk's start to a token; from a token to the chunk's end
     __shared__ float words[4];
-    pdl_begin();
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, q4 = lane & 3;
     // heads vary fastest: neighbours in the grid share the rows of their group
-    const uint32_t vheads = a.H * a.tiles, vh = blockIdx.x % vheads, seg = blockIdx.x / vheads % a.segments, b = blockIdx.x / vheads / a.segments;
+    const uint32_t vheads = a.H * a.tiles, vh = block % vheads, seg = block / vheads % a.segments, b = block / vheads / a.segments;
     const uint32_t head = vh / a.tiles, tile = vh % a.tiles, group = head / (a.H / a.G);
     const int length = a.lengths ? min(max(a.lengths[b], 0), (int)a.L) : (int)a.L;
     const int seg_tokens = (int)a.seg_chunks * SCAN_Q, t_lo = (int)seg * seg_tokens, t_hi = min(length, t_lo + seg_tokens);
@@ -475,26 +480,45 @@ __global__ void __launch_bounds__(128) k_clear_scan(const ScanArgs a) {
     }
 }
 
+// one grid for the sweeps of a call: those of the backward pass are independent
+template <class T, int NP>
+__global__ void __launch_bounds__(128) k_clear_scan_state(const __grid_constant__ ScanSet s) {
+    pdl_begin();
+    sweep<T, NP, 64, MODE_STATE>(s.a[blockIdx.x % s.count], blockIdx.x / s.count);
+}
+template <class T, int NP>
+__global__ void __launch_bounds__(128) k_clear_scan(const __grid_constant__ ScanSet s) {
+    pdl_begin();
+    sweep<T, NP, 64, MODE_OUT>(s.a[0], blockIdx.x);
+}
+template <class T, int NP>
+__global__ void __launch_bounds__(128) k_clear_scan_backward(const __grid_constant__ ScanSet s) {
+    pdl_begin();
+    const uint32_t which = blockIdx.x % 3, block = blockIdx.x / 3;
+    if (which < 2) sweep<T, 64, NP, MODE_GRAD>(s.a[which], block);
+    else sweep<T, NP, 64, MODE_OUT>(s.a[2], block);
+}
+
 // one type's kernels, by mode and by whether states have more than 64 columns
 template <class T>
-cudaError_t scan_launch(const ScanArgs& a, int mode, cudaStream_t st) {
+cudaError_t scan_launch(const ScanSet& s, int mode, cudaStream_t st) {
     auto go = [&](auto kernel, size_t smem) {
         cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        return e != cudaSuccess ? e : launch(kernel, dim3(a.b * a.segments * a.H * a.tiles), dim3(128), smem, st, a);
+        const ScanArgs& a = s.a[0];
+        return e != cudaSuccess ? e : launch(kernel, dim3(s.count * a.b * a.segments * a.H * a.tiles), dim3(128), smem, st, s);
     };
-    const bool big = a.N > 64;
-    switch (mode) {
-        case MODE_STATE: return big ? go(k_clear_scan<T, 128, 64, MODE_STATE>, ScanShared<T, 128, 64, MODE_STATE>::bytes)
-                                    : go(k_clear_scan<T, 64, 64, MODE_STATE>, ScanShared<T, 64, 64, MODE_STATE>::bytes);
-        case MODE_OUT: return big ? go(k_clear_scan<T, 128, 64, MODE_OUT>, ScanShared<T, 128, 64, MODE_OUT>::bytes)
-                                  : go(k_clear_scan<T, 64, 64, MODE_OUT>, ScanShared<T, 64, 64, MODE_OUT>::bytes);
-        default: return big ? go(k_clear_scan<T, 64, 128, MODE_GRAD>, ScanShared<T, 64, 128, MODE_GRAD>::bytes)
-                            : go(k_clear_scan<T, 64, 64, MODE_GRAD>, ScanShared<T, 64, 64, MODE_GRAD>::bytes);
-    }
+    auto pick = [&](auto np) {
+        constexpr int NP = decltype(np)::value;
+        constexpr size_t out = ScanShared<T, NP, 64, MODE_OUT>::bytes, grad = ScanShared<T, 64, NP, MODE_GRAD>::bytes;
+        return mode == MODE_STATE ? go(k_clear_scan_state<T, NP>, ScanShared<T, NP, 64, MODE_STATE>::bytes)
+             : mode == MODE_OUT   ? go(k_clear_scan<T, NP>, out)
+                                  : go(k_clear_scan_backward<T, NP>, out > grad ? out : grad);
+    };
+    return s.a[0].N > 64 ? pick(std::integral_constant<int, 128>()) : pick(std::integral_constant<int, 64>());
 }
-extern template cudaError_t scan_launch<__nv_bfloat16>(const ScanArgs&, int, cudaStream_t);
-extern template cudaError_t scan_launch<__half>(const ScanArgs&, int, cudaStream_t);
-extern template cudaError_t scan_launch<float>(const ScanArgs&, int, cudaStream_t);
+extern template cudaError_t scan_launch<__nv_bfloat16>(const ScanSet&, int, cudaStream_t);
+extern template cudaError_t scan_launch<__half>(const ScanSet&, int, cudaStream_t);
+extern template cudaError_t scan_launch<float>(const ScanSet&, int, cudaStream_t);
 // the same on tcgen05: bfloat16, states of 65 to 128 columns, N and P multiples of 8, operands and outputs with 16-byte rows (clear_scan_tc.cu); dots then has SCAN_DOTS parts a head tile
 #define SCAN_DOTS 4
-cudaError_t scan_tc_launch(const ScanArgs& a, int mode, cudaStream_t st);
+cudaError_t scan_tc_launch(const ScanSet& s, int mode, cudaStream_t st);
