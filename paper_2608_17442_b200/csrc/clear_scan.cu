@@ -38,23 +38,37 @@ __global__ void __launch_bounds__(256) k_clear_combine(const Chain forwards, con
         !DBG_REGION(s, ((segments - 1) * per_b + n) * sizeof(float)) || (init && !DBG_REGION(init + b * per_b + i, n * sizeof(float))))
         return;
     const bool wide = per_b % 4 == 0 && per_head % 4 == 0 && ((size_t)init & 15) == 0;
+    const uint32_t h0 = (uint32_t)i / per_head;      // H * P * N is below 2^32 (checked)
     float run[4] = {};
     for (uint32_t e = 0; e < n && init; e++) run[e] = init[b * per_b + i + e];
+    if (wide) {
+        // the loads of eight segments before the first of their stores: one trip to memory for all
+        for (uint32_t c = 0; c < segments; c += 8) {
+            float4 add[8];
+            float f[8];
+#pragma unroll
+            for (uint32_t k = 0; k < 8; k++)
+                if (c + k < segments) {
+                    const uint32_t at = backwards ? segments - 1 - c - k : c + k;
+                    add[k] = *reinterpret_cast<const float4*>(s + (size_t)at * per_b), f[k] = decay[((size_t)b * segments + at) * H + h0];
+                }
+#pragma unroll
+            for (uint32_t k = 0; k < 8; k++)
+                if (c + k < segments) {
+                    const uint32_t at = backwards ? segments - 1 - c - k : c + k;
+                    *reinterpret_cast<float4*>(s + (size_t)at * per_b) = make_float4(run[0], run[1], run[2], run[3]);
+                    run[0] = f[k] * run[0] + add[k].x, run[1] = f[k] * run[1] + add[k].y, run[2] = f[k] * run[2] + add[k].z, run[3] = f[k] * run[3] + add[k].w;
+                }
+        }
+        return;
+    }
     for (uint32_t c = 0; c < segments; c++) {
         const uint32_t at = backwards ? segments - 1 - c : c;
         float* p = s + (size_t)at * per_b;
-        const float* d = decay + ((size_t)b * segments + at) * H;
-        if (wide) {
-            const float4 add = *reinterpret_cast<const float4*>(p);
-            *reinterpret_cast<float4*>(p) = make_float4(run[0], run[1], run[2], run[3]);
-            const float f = d[i / per_head];
-            run[0] = f * run[0] + add.x, run[1] = f * run[1] + add.y, run[2] = f * run[2] + add.z, run[3] = f * run[3] + add.w;
-        } else {
-            for (uint32_t e = 0; e < n; e++) {
-                const float add = p[e];
-                p[e] = run[e];
-                run[e] = d[(i + e) / per_head] * run[e] + add;
-            }
+        for (uint32_t e = 0; e < n; e++) {
+            const float add = p[e];
+            p[e] = run[e];
+            run[e] = decay[((size_t)b * segments + at) * H + ((uint32_t)i + e) / per_head] * run[e] + add;
         }
     }
 }
@@ -65,28 +79,30 @@ struct FinishArgs {
     float *dg, *dskip;
     const int* lengths;
     long long Bb, Bt, Bg, Cb, Ct, Cg, gb, gt, gh, ib, it, ih;
-    uint32_t b, L, H, G, N, NP, tiles, segments, seg_chunks, sum_blocks, dg_blocks;
-    uint32_t dots;                 // parts of row and col per head
+    uint32_t b, L, H, G, N, tiles, segments, seg_chunks;
+    uint32_t dots;                                       // parts of row and col per head
+    uint32_t log_quads;                                  // columns of part_b and part_c: 4 << log_quads
+    uint32_t sum_each, sum_blocks, dg_blocks;            // blocks: of a sequence's group in one sum, of both sums, of dg
 };
-// What is left of the backward pass, by block: sums of dB and dC over the heads of a group; the gradient of the log decays; that of the skip.
+// What is left of the backward pass, by block: sums of dB and dC over the heads of a group; the gradient of the log decays, a block per
+// sequence, head and segment; that of the skip.
 template <class T>
 __global__ void __launch_bounds__(256) k_clear_scan_finish(const FinishArgs a) {
+    __shared__ double words[2][8];
     pdl_begin();
-    const uint32_t vheads = a.H * a.tiles, tid = threadIdx.x;
+    const uint32_t vheads = a.H * a.tiles, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    auto tokens = [&](uint32_t b) { return a.lengths ? min(max(a.lengths[b], 0), (int)a.L) : (int)a.L; };
     if (blockIdx.x < a.sum_blocks) {
-        const uint32_t quads = a.NP / 4;
-        const size_t i = (size_t)blockIdx.x * 256 + tid, all = (size_t)a.b * a.L * a.G * quads;
-        if (i >= all) return;
-        const uint32_t n = (uint32_t)(i % quads) * 4, grp = (uint32_t)(i / quads % a.G), t = (uint32_t)(i / quads / a.G % a.L), b = (uint32_t)(i / quads / a.G / a.L);
-        const int length = a.lengths ? min(max(a.lengths[b], 0), (int)a.L) : (int)a.L;
-        if ((int)t >= length || n >= a.N) return;
-        const uint32_t per = vheads / a.G;
-        const size_t step = (size_t)a.L * a.NP;
-        const float* src = (blockIdx.y ? a.part_c : a.part_b) + (((size_t)b * vheads + grp * per) * a.L + t) * a.NP + n;
-        T* dst = blockIdx.y ? (T*)a.dC + b * a.Cb + t * a.Ct + grp * a.Cg + n : (T*)a.dB + b * a.Bb + t * a.Bt + grp * a.Bg + n;
+        const uint32_t piece = blockIdx.x / a.sum_each, c_sum = piece & 1, grp = (piece >> 1) % a.G, b = (piece >> 1) / a.G;
+        const size_t i = (size_t)(blockIdx.x % a.sum_each) * 256 + tid, t = i >> a.log_quads;
+        const uint32_t n = 4 * ((uint32_t)i & ((1u << a.log_quads) - 1)), per = vheads / a.G, NP = 4u << a.log_quads;
+        if (t >= (size_t)tokens(b) || n >= a.N) return;
+        const size_t step = (size_t)a.L * NP;
+        const float* src = (c_sum ? a.part_c : a.part_b) + (((size_t)b * vheads + grp * per) * a.L + t) * NP + n;
+        T* dst = c_sum ? (T*)a.dC + b * a.Cb + (long long)t * a.Ct + grp * a.Cg + n : (T*)a.dB + b * a.Bb + (long long)t * a.Bt + grp * a.Bg + n;
         if (!DBG_REGION(src, ((per - 1) * step + 4) * sizeof(float)) || !DBG_REGION(dst, min(4u, a.N - n) * sizeof(T))) return;
         float s[4] = {};
-#pragma unroll 4
+#pragma unroll 8
         for (uint32_t h = 0; h < per; h++) {
             const float4 v = *reinterpret_cast<const float4*>(src + h * step);
             s[0] += v.x, s[1] += v.y, s[2] += v.z, s[3] += v.w;
@@ -96,14 +112,11 @@ __global__ void __launch_bounds__(256) k_clear_scan_finish(const FinishArgs a) {
             if (n + e < a.N) dst[e] = ClearType<T>::from(s[e]);
         return;
     }
-    if (blockIdx.y) return;
-    const uint32_t lane = tid & 31, blk = blockIdx.x - a.sum_blocks;
-    if (blk < a.dg_blocks) {                       // a warp per sequence, head and segment
-        const size_t w = (size_t)blk * 8 + (tid >> 5);
-        if (w >= (size_t)a.b * a.H * a.segments) return;
-        const uint32_t head = (uint32_t)(w % a.H), seg = (uint32_t)(w / a.H % a.segments), b = (uint32_t)(w / a.H / a.segments);
-        const int length = a.lengths ? min(max(a.lengths[b], 0), (int)a.L) : (int)a.L;
-        const int lo = (int)(seg * a.seg_chunks) * SCAN_Q, hi = min(length, lo + (int)a.seg_chunks * SCAN_Q);
+    const uint32_t blk = blockIdx.x - a.sum_blocks;
+    if (blk < a.dg_blocks) {
+        // R_t = R_{t+1} + row_t - col_t from the segment's end, 256 tokens at a time; the next ones' words are read while these are summed
+        const uint32_t head = blk % a.H, seg = blk / a.H % a.segments, b = blk / a.H / a.segments;
+        const int length = tokens(b), lo = (int)(seg * a.seg_chunks) * SCAN_Q, hi = min(length, lo + (int)a.seg_chunks * SCAN_Q);
         if (lo >= hi) return;
         const float* row = a.row + ((size_t)b * a.H + head) * a.dots * a.L;
         const float* col = a.col + ((size_t)b * a.H + head) * a.dots * a.L;
@@ -112,27 +125,60 @@ __global__ void __launch_bounds__(256) k_clear_scan_finish(const FinishArgs a) {
         if (!DBG_REGION(dg + lo * a.gt, ((long long)(hi - 1 - lo) * a.gt + 1) * sizeof(float))) return;
         double run = 0.0;
         for (uint32_t s = 0; s < a.tiles; s++) run += a.ends[((size_t)b * a.segments + seg) * vheads + head * a.tiles + s];
-        for (int top = hi - 1; top >= lo; top -= 32) {
-            const int t = top - (int)lane;
-            double v = 0.0;
-            if (t >= lo)
-                for (uint32_t s = 0; s < a.dots; s++) v += (double)row[(size_t)s * a.L + t] - (double)col[(size_t)s * a.L + t];
+        double next = 0.0;
+        bool next_drop = false;
+        auto read = [&](int t) {
+            next = 0.0, next_drop = false;
+            if (t < lo) return;
+            for (uint32_t s = 0; s < a.dots; s++) next += (double)row[(size_t)s * a.L + t] - (double)col[(size_t)s * a.L + t];
+            next_drop = g[t * a.it] < SCAN_DROP;
+        };
+        read(hi - 1 - (int)tid);
+        uint32_t turn = 0;
+        for (int top = hi - 1; top >= lo; top -= 256, turn ^= 1) {
+            const int t = top - (int)tid;
+            double v = next;
+            const bool drop = next_drop;
+            read(t - 256);
+            // a dropped state has the gradient zero, from which the sum goes on: what a token adds up goes back to the nearest drop at or behind it
+            if (__syncthreads_or(drop)) {
+                // seldom: token by token
+                __shared__ double all[256];
+                __shared__ bool drops[256];
+                all[tid] = v, drops[tid] = drop;
+                __syncthreads();
+                if (tid == 0)
+                    for (int k = 0; k < 256 && top - k >= lo; k++) {
+                        run = drops[k] ? 0.0 : run + all[k];
+                        dg[(long long)(top - k) * a.gt] = (float)run;
+                    }
+                if (tid == 0) words[0][0] = run;
+                __syncthreads();
+                run = words[0][0];
+                __syncthreads();
+                continue;
+            }
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const double u = __shfl_up_sync(~0u, v, o);
                 if ((int)lane >= o) v += u;
             }
-            // a dropped state has the gradient zero, from which the sum goes on
-            const uint32_t drops = __ballot_sync(~0u, t >= lo && g[t * a.it] < SCAN_DROP) & (~0u >> (31 - lane));
-            const double from = __shfl_sync(~0u, v, drops ? 31 - __clz(drops) : 0);
-            v = drops ? v - from : run + v;
-            if (t >= lo) dg[t * a.gt] = (float)v;
-            run = __shfl_sync(~0u, v, 31);
+            if (lane == 31) words[turn][warp] = v;
+            __syncthreads();
+            double total = 0.0, before = 0.0;
+#pragma unroll
+            for (uint32_t w = 0; w < 8; w++) {
+                const double x = words[turn][w];
+                if (w < warp) before += x;
+                total += x;
+            }
+            if (t >= lo) dg[t * a.gt] = (float)(run + before + v);
+            run += total;
         }
         return;
     }
     // the skip: a warp per head
-    const uint32_t head = (blk - a.dg_blocks) * 8 + (tid >> 5);
+    const uint32_t head = (blk - a.dg_blocks) * 8 + warp;
     if (!a.dskip || head >= a.H) return;
     double s = 0.0;
     const size_t all = (size_t)a.b * a.segments * a.tiles;
@@ -246,7 +292,8 @@ static const char* scan_check(const fesc_clear_scan_desc* d) {
     if (d->N > SCAN_MAX_STATE) return "clear_scan: states of more than 128 columns";
     if (d->P > 4096 || d->L >= (1u << 30)) return "clear_scan: more than 4096 channels of a head or 2^30 tokens";
     const ScanShape s = scan_shape(d);
-    if (3 * (uint64_t)d->batch * s.segments * s.vheads >= (1ull << 31) || d->batch > 65535 || (uint64_t)d->batch * d->L * d->G * 32 >= (1ull << 38))
+    if (3 * (uint64_t)d->batch * s.segments * s.vheads >= (1ull << 31) || d->batch > 65535 ||
+        (uint64_t)d->batch * d->G * ((uint64_t)d->L / 8 + 1) * 2 + (uint64_t)d->batch * d->H * s.segments >= (1ull << 31) - d->H || (uint64_t)d->H * d->P * d->N >= (1ull << 31))
         return "clear_scan: too many sequences, heads or tokens for one call";
     return nullptr;
 }
@@ -405,10 +452,10 @@ extern "C" int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const 
     f.part_b = part_b, f.part_c = part_c, f.row = row, f.col = col, f.ends = ends, f.diag = diag;
     f.dB = d_dB, f.dC = d_dC, f.dg = d_dg, f.dskip = d_dskip, f.lengths = d_lengths, f.g = d_g, f.ib = d.g[0], f.it = d.g[1], f.ih = d.g[2];
     f.Bb = d.dB[0], f.Bt = d.dB[1], f.Bg = d.dB[2], f.Cb = d.dC[0], f.Ct = d.dC[1], f.Cg = d.dC[2], f.gb = d.dg[0], f.gt = d.dg[1], f.gh = d.dg[2];
-    f.b = d.batch, f.L = d.L, f.H = d.H, f.G = d.G, f.N = d.N, f.NP = s.np, f.tiles = s.tiles, f.segments = s.segments, f.seg_chunks = s.seg_chunks, f.dots = s.tiles * (tc ? SCAN_DOTS : 1);
-    f.sum_blocks = (uint32_t)(((size_t)d.batch * d.L * d.G * (s.np / 4) + 255) / 256);
-    f.dg_blocks = (uint32_t)(((size_t)d.batch * d.H * s.segments + 7) / 8);
-    const dim3 grid(f.sum_blocks + f.dg_blocks + (d.H + 7) / 8, 2);
+    f.b = d.batch, f.L = d.L, f.H = d.H, f.G = d.G, f.N = d.N, f.tiles = s.tiles, f.segments = s.segments, f.seg_chunks = s.seg_chunks;
+    f.dots = s.tiles * (tc ? SCAN_DOTS : 1), f.log_quads = s.np == 128 ? 5 : 4;
+    f.sum_each = (uint32_t)(((size_t)d.L * (s.np / 4) + 255) / 256), f.sum_blocks = 2 * d.batch * d.G * f.sum_each, f.dg_blocks = d.batch * d.H * s.segments;
+    const dim3 grid(f.sum_blocks + f.dg_blocks + (d.H + 7) / 8);
     auto kernel = d.type == FESC_BF16 ? k_clear_scan_finish<__nv_bfloat16> : d.type == FESC_F16 ? k_clear_scan_finish<__half> : k_clear_scan_finish<float>;
     CLEAR_CUDA(launch(kernel, grid, dim3(256), 0, st, f));
     return FESC_OK;
