@@ -133,7 +133,7 @@ __device__ __forceinline__ void st32(void* p, const uint32_t* v) {
 
 struct TcShared {
     TcDecays decays[2];
-    alignas(8) u64 bars[12];        // see below
+    alignas(8) u64 bars[14];        // see below
     uint32_t tmem_base;
     volatile uint32_t dead;         // a wait gave up: the rest of the chunks goes through without waiting, with nothing of worth in it
     float words[2][TC_WARPS];
@@ -187,19 +187,20 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
 #endif
     const uint32_t base = ((uint32_t)__cvta_generic_to_shared(tc_smem) + 1023) & ~1023u, bar = (uint32_t)__cvta_generic_to_shared(bars);
     uint8_t* const panels = tc_smem + (base - (uint32_t)__cvta_generic_to_shared(tc_smem));
-    // per chunk: operands copied; faded values, state, decayed scores written; products S and O1, H, O2 done
-    const uint32_t b_load = bar, b_wv = bar + 8, b_st = bar + 16, b_p = bar + 24, b_s = bar + 32, b_h = bar + 40, b_o = bar + 48, drained = bar + 56;
-    // of the two sets of decays and operands: decays filled, all used (and O1 and O2 read); a set has barriers of its own because those who fill
-    // them run up to two chunks ahead
-    const uint32_t b_g = bar + 64, b_used = bar + 80;
+    // per chunk: q copied; faded values and state, decayed scores written; products S, O1, H, O2 done.  No one gets to what completes a barrier's
+    // next phase before everyone who waits for this one has.
+    const uint32_t b_q = bar, b_wv = bar + 8, b_o1 = bar + 16, b_p = bar + 24, b_s = bar + 32, b_h = bar + 40, b_o = bar + 48, drained = bar + 56;
+    // Of the two sets of decays and of k and v: filled, and all used (and O1 and O2 read).  A set has barriers of its own because those who fill them
+    // run up to two chunks ahead: two phases of one barrier would be over before some warp has waited for the first, which then looks like the third.
+    const uint32_t b_g = bar + 64, b_used = bar + 80, b_kv = bar + 96;
     if (warp == TC_WARPS) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"((uint32_t)__cvta_generic_to_shared(&tmem_base)), "n"(Lay::columns)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     if (tid == 0) {
-        mbar_init(b_load, 2), mbar_init(b_wv, TC_WARPS), mbar_init(b_p, TC_WARPS), mbar_init(b_st, TC_WARPS);
-        for (uint32_t i = 0; i < 2; i++) mbar_init(b_g + 8 * i, 1), mbar_init(b_used + 8 * i, TC_WARPS);
+        mbar_init(b_q, 2), mbar_init(b_wv, TC_WARPS), mbar_init(b_p, TC_WARPS), mbar_init(b_o1, 1);
+        for (uint32_t i = 0; i < 2; i++) mbar_init(b_g + 8 * i, 1), mbar_init(b_used + 8 * i, TC_WARPS), mbar_init(b_kv + 8 * i, 2);
         mbar_init(b_s, 1), mbar_init(b_h, 1), mbar_init(b_o, 1), mbar_init(drained, 1);
         dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -228,7 +229,8 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
             const uint32_t pq = d0 + Lay::q * STEP, pw_ = d0 + Lay::w * STEP, ps = d0 + Lay::st * STEP, pb = d0 + (Lay::broad + 2 * set) * STEP,
                            pn = d0 + (Lay::narrow + set) * STEP;
             if (MODE) {
-                wait(b_load, c);
+                wait(b_kv + 8 * set, c >> 1);
+                wait(b_q, c);
                 if (c) wait(b_o, c - 1);                             // the scores' planes lie over the scores
                 tc_after();
 #pragma unroll
@@ -236,14 +238,6 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                     const uint32_t at = (k >> 2) * STEP + (k & 3) * 2;
                     tc_mma_ss(tmem + Lay::S, pq + at, (Lay::OUT ? pb : pn) + at, I_S, k);
                 }
-                wait(b_st, c);
-                if (c) wait(b_used + 8 * (set ^ 1), (c - 1) >> 1);
-                tc_after();
-#pragma unroll
-                for (uint32_t p = 0; p < (Lay::OUT ? 1 : NO); p++)
-#pragma unroll
-                    for (uint32_t k = 0; k < QK; k++)
-                        tc_mma_ss(tmem + Lay::O1, pq + (k >> 2) * STEP + (k & 3) * 2, ps + p * STEP + (Lay::OUT ? k * 128 : k * 2), I_O1, p || k);
                 tc_commit(b_s);
             }
             wait(b_wv, c);
@@ -253,6 +247,16 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
 #pragma unroll
                 for (uint32_t k = 0; k < 8; k++) tc_mma_ss(tmem + Lay::H, pb + k * 128, pw_ + p * STEP + k * 128, I_H, p || k);
             tc_commit(b_h);
+            if (MODE) {
+                if (c) wait(b_used + 8 * (set ^ 1), (c - 1) >> 1);
+                tc_after();
+#pragma unroll
+                for (uint32_t p = 0; p < (Lay::OUT ? 1 : NO); p++)
+#pragma unroll
+                    for (uint32_t k = 0; k < QK; k++)
+                        tc_mma_ss(tmem + Lay::O1, pq + (k >> 2) * STEP + (k & 3) * 2, ps + p * STEP + (Lay::OUT ? k * 128 : k * 2), I_O1, p || k);
+                tc_commit(b_o1);
+            }
             if (MODE) {
                 wait(b_p, c);
                 tc_after();
@@ -342,21 +346,25 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                 }
             }
         };
+        auto landed = [&](uint32_t which) {
+            cp_async_wait();
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(which);
+        };
         const long long sb = 8 * dir * ob.st, sn = 8 * dir * on.st, sq = 8 * dir * a.q.st;
         for (int c = 0; c < chunks; c++) {
             const uint32_t set = c & 1;
             if (c >= 2) wait(b_used + 8 * set, (c >> 1) - 1);
             copy(Lay::broad + 2 * set, 2, pb, sb, (int)a.N, left(c));
             copy(Lay::narrow + set, 1, pn, sn, pw, left(c));
+            landed(b_kv + 8 * set);
             if (MODE) {
-                if (c) wait(b_s, c - 1);
+                if (c) wait(b_o1, c - 1);
                 copy(Lay::q, Lay::QP, pq, sq, qw, left(c));
+                landed(b_q);
             }
             pb += sb * (TC_Q / 8), pn += sn * (TC_Q / 8), pq += sq * (TC_Q / 8);
-            cp_async_wait();
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(b_load);
         }
     } else {
         const uint32_t quarter = warp & 3, part = warp >> 2, row = 32 * quarter + lane;     // row: token of the chunk, or column of the state
@@ -394,32 +402,30 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
         };
         float diag = 0.f;
         const float skip = Lay::OUT && a.skip ? a.skip[head] : 0.f;
-        if (MODE && chunks) {
-            put_state();
+        // what the products of chunk c need from here: the state before it, and its faded values
+        auto provide = [&](int c) {
+            if (MODE) put_state();
+            wait(b_kv + 8 * (c & 1), c >> 1);
+            wait(b_g + 8 * (c & 1), c >> 1);
+            const float f = decays[c & 1].fade[row];
+            const uint8_t* src = panels + (Lay::narrow + (c & 1)) * PANEL;
+            const uint4 v0 = *reinterpret_cast<const uint4*>(src + at0), v1 = *reinterpret_cast<const uint4*>(src + at1);
+            const uint32_t u[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+            uint32_t pl[8][3];
+#pragma unroll
+            for (int e = 0; e < 8; e++) split2<NS>(mul2(both(u[e]), {f, f}), pl[e]);
+            put(Lay::w, pl, NS);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            arrive(b_st);
-        }
+            tc_before();
+            arrive(b_wv);
+        };
+        if (chunks) provide(0);
         for (int c = 0; c < chunks; c++) {
             const int valid = left(c), set = c & 1;
             const TcDecays& d = decays[set];
-            wait(b_load, c);
-            wait(b_g + 8 * set, c >> 1);
-            {
-                const float f = d.fade[row];
-                const uint8_t* src = panels + (Lay::narrow + set) * PANEL;
-                const uint4 v0 = *reinterpret_cast<const uint4*>(src + at0), v1 = *reinterpret_cast<const uint4*>(src + at1);
-                const uint32_t u[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
-                uint32_t pl[8][3];
-#pragma unroll
-                for (int e = 0; e < 8; e++) split2<NS>(mul2(both(u[e]), {f, f}), pl[e]);
-                put(Lay::w, pl, NS);
-            }
-            const float keep = d.keep;
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            arrive(b_wv);
             if (MODE) {
                 // decayed scores of this row and the columns 32 part .. 32 part + 31
-                wait(b_s, c);                       // S and O1
+                wait(b_s, c);
                 tc_after();
                 const float2 ci = d.cum[row];
                 // whole loops per case: a branch inside would keep the columns from overlapping
@@ -483,6 +489,7 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
             wait(b_h, c);
             tc_after();
             {
+                const float keep = d.keep;
                 uint32_t x[Lay::H_PARTS][16];
 #pragma unroll
                 for (int p = 0; p < (int)Lay::H_PARTS; p++) tc_ld16(x[p], lanes + Lay::H + 64 * p + 16 * part);
@@ -490,23 +497,22 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
                     auto pair = [&](int p) { return f2{__uint_as_float(x[p][2 * e]), __uint_as_float(x[p][2 * e + 1])}; };
-                    f2 v = pair(Lay::H_PARTS - 1);
+                    f2 v = pair((int)Lay::H_PARTS - 1);
 #pragma unroll
-                    for (int p = Lay::H_PARTS - 2; p >= 0; p--) v = add2(v, pair(p));
+                    for (int p = (int)Lay::H_PARTS - 2; p >= 0; p--) v = add2(v, pair(p));
                     st[e] = fma2(st[e], {keep, keep}, v);
                 }
             }
-            tc_before();
+            const float grow = d.grow[row];
+            if (c + 1 < chunks) {
+                if (MODE) wait(b_o1, c);       // the state's panels are free
+                provide(c + 1);                // before the outputs: O2 is under way
+            }
             if (!MODE) {
                 arrive(b_used + 8 * set);
                 continue;
             }
-            if (c + 1 < chunks) {
-                put_state();
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                arrive(b_st);
-            }
-            const float grow = d.grow[row];
+
             const bool live = (int)row < valid;
             const long long t = t_first + (long long)dir * (c * TC_Q + (int)row);
             if (Lay::OUT) {
