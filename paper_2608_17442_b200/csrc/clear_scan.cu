@@ -80,7 +80,6 @@ struct FinishArgs {
     const int* lengths;
     long long Bb, Bt, Bg, Cb, Ct, Cg, gb, gt, gh, ib, it, ih;
     uint32_t b, L, H, G, N, tiles, segments, seg_chunks;
-    uint32_t dots;                                       // parts of row and col per head
     uint32_t log_quads;                                  // columns of part_b and part_c: 4 << log_quads
     uint32_t sum_each, sum_blocks, dg_blocks;            // blocks: of a sequence's group in one sum, of both sums, of dg
 };
@@ -118,8 +117,8 @@ __global__ void __launch_bounds__(256) k_clear_scan_finish(const FinishArgs a) {
         const uint32_t head = blk % a.H, seg = blk / a.H % a.segments, b = blk / a.H / a.segments;
         const int length = tokens(b), lo = (int)(seg * a.seg_chunks) * SCAN_Q, hi = min(length, lo + (int)a.seg_chunks * SCAN_Q);
         if (lo >= hi) return;
-        const float* row = a.row + ((size_t)b * a.H + head) * a.dots * a.L;
-        const float* col = a.col + ((size_t)b * a.H + head) * a.dots * a.L;
+        const float* row = a.row + ((size_t)b * a.H + head) * a.tiles * a.L;
+        const float* col = a.col + ((size_t)b * a.H + head) * a.tiles * a.L;
         float* dg = a.dg + b * a.gb + head * a.gh;
         const float* g = a.g + b * a.ib + head * a.ih;
         if (!DBG_REGION(dg + lo * a.gt, ((long long)(hi - 1 - lo) * a.gt + 1) * sizeof(float))) return;
@@ -130,7 +129,7 @@ __global__ void __launch_bounds__(256) k_clear_scan_finish(const FinishArgs a) {
         auto read = [&](int t) {
             next = 0.0, next_drop = false;
             if (t < lo) return;
-            for (uint32_t s = 0; s < a.dots; s++) next += (double)row[(size_t)s * a.L + t] - (double)col[(size_t)s * a.L + t];
+            for (uint32_t s = 0; s < a.tiles; s++) next += (double)row[(size_t)s * a.L + t] - (double)col[(size_t)s * a.L + t];
             next_drop = g[t * a.it] < SCAN_DROP;
         };
         read(hi - 1 - (int)tid);
@@ -280,8 +279,9 @@ static ScanShape scan_shape(const fesc_clear_scan_desc* d) {
     auto whole = [](size_t floats) { return (floats + 63) / 64 * 64; };      // parts of the workspace start on 256 bytes
     s.state_floats = s.segments > 1 ? whole((size_t)d->batch * s.segments * s.states) : 0;
     s.decay_floats = s.segments > 1 ? whole((size_t)d->batch * s.segments * d->H) : 0;
-    s.part_floats = whole((size_t)d->batch * s.vheads * d->L * s.np);
-    s.dot_floats = whole((size_t)d->batch * s.vheads * (s.tc ? SCAN_DOTS : 1) * d->L);
+    // rows of a sequence, or whole chunks
+    s.part_floats = whole((size_t)d->batch * s.vheads * s.np * (s.tc ? (size_t)s.segments * s.seg_chunks * SCAN_Q : d->L));
+    s.dot_floats = whole((size_t)d->batch * s.vheads * d->L);
     s.end_floats = whole((size_t)d->batch * s.segments * s.vheads);
     return s;
 }
@@ -290,6 +290,7 @@ static const char* scan_check(const fesc_clear_scan_desc* d) {
     if (d->type > FESC_F32) return "clear_scan: unknown type";
     if (!d->H || !d->P || !d->N || !d->G || d->H % d->G) return "clear_scan: an empty dimension, or groups that do not divide the heads";
     if (d->N > SCAN_MAX_STATE) return "clear_scan: states of more than 128 columns";
+    if (d->G > 65535) return "clear_scan: more than 65535 groups";
     if (d->P > 4096 || d->L >= (1u << 30)) return "clear_scan: more than 4096 channels of a head or 2^30 tokens";
     const ScanShape s = scan_shape(d);
     if (3 * (uint64_t)d->batch * s.segments * s.vheads >= (1ull << 31) || d->batch > 65535 ||
@@ -429,7 +430,7 @@ extern "C" int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const 
     const uint32_t bytes = clear_type_bytes(d.type);
     const ScanOperand x = operand(d_x, d.x, true, bytes), B = operand(d_B, d.B, false, bytes), C = operand(d_C, d.C, false, bytes),
                       dy = operand(d_dy, d.y, true, bytes);
-    const bool tc = s.tc && x.wide && B.wide && C.wide && dy.wide && out_width(d_dx, d.dx, bytes);
+    const bool tc = s.tc && x.wide && B.wide && C.wide && dy.wide && out_width(d_dx, d.dx, bytes) && out_width(d_dB, d.dB, bytes) && out_width(d_dC, d.dC, bytes);
     const ScanArgs base = scan_args(desc, s, d_g, d_lengths);
     const float *h = d_h0, *dh = d_dh_out;
     if (s.segments > 1) {
@@ -453,8 +454,14 @@ extern "C" int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const 
     f.dB = d_dB, f.dC = d_dC, f.dg = d_dg, f.dskip = d_dskip, f.lengths = d_lengths, f.g = d_g, f.ib = d.g[0], f.it = d.g[1], f.ih = d.g[2];
     f.Bb = d.dB[0], f.Bt = d.dB[1], f.Bg = d.dB[2], f.Cb = d.dC[0], f.Ct = d.dC[1], f.Cg = d.dC[2], f.gb = d.dg[0], f.gt = d.dg[1], f.gh = d.dg[2];
     f.b = d.batch, f.L = d.L, f.H = d.H, f.G = d.G, f.N = d.N, f.tiles = s.tiles, f.segments = s.segments, f.seg_chunks = s.seg_chunks;
-    f.dots = s.tiles * (tc ? SCAN_DOTS : 1), f.log_quads = s.np == 128 ? 5 : 4;
-    f.sum_each = (uint32_t)(((size_t)d.L * (s.np / 4) + 255) / 256), f.sum_blocks = 2 * d.batch * d.G * f.sum_each, f.dg_blocks = d.batch * d.H * s.segments;
+    f.log_quads = s.np == 128 ? 5 : 4, f.dg_blocks = d.batch * d.H * s.segments;
+    if (tc) {        // sums of their own; the decays after them
+        TcSums t = {part_b, part_c, B, C, (__nv_bfloat16*)d_dB, (__nv_bfloat16*)d_dC, row, col, d_lengths, f.Bb, f.Bt, f.Bg, f.Cb, f.Ct, f.Cg,
+                    d.L, d.H, d.G, d.N, s.tiles, s.segments, s.seg_chunks};
+        CLEAR_CUDA(scan_tc_sums(t, d.batch, st));
+    } else {
+        f.sum_each = (uint32_t)(((size_t)d.L * (s.np / 4) + 255) / 256), f.sum_blocks = 2 * d.batch * d.G * f.sum_each;
+    }
     const dim3 grid(f.sum_blocks + f.dg_blocks + (d.H + 7) / 8);
     auto kernel = d.type == FESC_BF16 ? k_clear_scan_finish<__nv_bfloat16> : d.type == FESC_F16 ? k_clear_scan_finish<__half> : k_clear_scan_finish<float>;
     CLEAR_CUDA(launch(kernel, grid, dim3(256), 0, st, f));

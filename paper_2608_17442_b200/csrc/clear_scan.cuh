@@ -519,6 +519,16 @@ cudaError_t scan_launch(const ScanSet& s, int mode, cudaStream_t st) {
 extern template cudaError_t scan_launch<__nv_bfloat16>(const ScanSet&, int, cudaStream_t);
 extern template cudaError_t scan_launch<__half>(const ScanSet&, int, cudaStream_t);
 extern template cudaError_t scan_launch<float>(const ScanSet&, int, cudaStream_t);
-// the same on tcgen05: bfloat16, states of 65 to 128 columns, N and P multiples of 8, operands and outputs with 16-byte rows (clear_scan_tc.cu); dots then has SCAN_DOTS parts a head tile
-#define SCAN_DOTS 4
+// The same on tcgen05: bfloat16, states of 65 to 128 columns, N and P multiples of 8, operands and outputs with 16-byte rows (clear_scan_tc.cu).
+// part is [b][head tile][segment][chunk of 128][16384] in an order of its own there, and dots is left to the kernel that sums it up over heads.
 cudaError_t scan_tc_launch(const ScanSet& s, int mode, cudaStream_t st);
+struct TcSums {
+    const float *part_b, *part_c;
+    ScanOperand uB, uC;
+    __nv_bfloat16 *dB, *dC;
+    float *row, *col;
+    const int* lengths;
+    long long Bb, Bt, Bg, Cb, Ct, Cg;
+    uint32_t L, H, G, N, tiles, segments, seg_chunks;
+};
+cudaError_t scan_tc_sums(const TcSums& a, uint32_t batch, cudaStream_t st);

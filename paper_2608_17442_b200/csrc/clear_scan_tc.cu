@@ -25,6 +25,9 @@
 
 #define TC_Q 128
 #define PANEL 16384u
+#ifndef TC_BACK_UNROLL
+#define TC_BACK_UNROLL 2
+#endif
 #define TC_WARPS 16             // that compute; one more issues, one more sums decays, two copy
 #define TC_THREADS (32 * (TC_WARPS + 4))
 
@@ -35,7 +38,7 @@ struct TcLayout {
     // panels in shared memory; k and v have two sets
     static constexpr int q = 0, QP = OUT ? 2 : GRAD ? 1 : 0;
     static constexpr int broad = QP, narrow = broad + 4, w = narrow + 2, st = w + 3, panels = st + (MODE ? NO : 0);
-    // Columns of tensor memory, all 512 with outputs.  The first two planes of 16 decayed scores lie over the 16 scores, so a warp overwrites what it
+    // Columns of tensor memory, of which a CTA takes all 512: they begin at 0.  The first two planes of 16 decayed scores lie over the 16 scores, so a warp overwrites what it
     // has read itself; a third plane has columns of its own.
     static constexpr uint32_t DV = GRAD ? 128 : 64, O1_PARTS = OUT ? 2 : 1, H_PARTS = GRAD ? 1 : 3;      // accumulators side by side, one per plane
     static constexpr uint32_t S = 0, P3 = 128, O1 = GRAD ? 192 : 128, O2 = O1 + O1_PARTS * DV, H = MODE ? O2 + DV : 0, columns = 512;
@@ -139,7 +142,8 @@ struct TcShared {
     float words[2][TC_WARPS];
 };
 
-template <int MODE>
+// UNROLL: products of a loop that are issued in a row (8: all)
+template <int MODE, int UNROLL>
 __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcShared& sh) {
     using Lay = TcLayout<MODE>;
     constexpr int NO = Lay::NO, NS = 3;
@@ -175,9 +179,8 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
         if (MODE) ok = ok && DBG_REGION(scan_row<T>(a.q, b, t_lo, head, group, tile), (n * a.q.st + qw) * sizeof(T));
         if (MODE == MODE_OUT) ok = ok && DBG_REGION((T*)a.out + b * a.ob + t_lo * a.ot + head * a.oh + tile * SCAN_TILE, (n * a.ot + vw) * sizeof(T));
         if (MODE == MODE_GRAD)
-            ok = ok && DBG_REGION(scan_row<T>(a.u, b, t_lo, head, group, tile), (n * a.u.st + a.N) * sizeof(T)) &&
-                 DBG_REGION(a.part + (((size_t)b * vheads + vh) * a.L + t_lo) * 128, (n + 1) * 128 * sizeof(float)) &&
-                 DBG_REGION(a.dots + ((size_t)b * vheads + vh) * SCAN_DOTS * a.L, SCAN_DOTS * (size_t)a.L * sizeof(float));
+            ok = ok && DBG_REGION(a.part + (((size_t)b * vheads + vh) * a.segments + seg) * (a.seg_chunks / 2) * (TC_Q * 128),
+                                  (size_t)((n + TC_Q) / TC_Q) * TC_Q * 128 * sizeof(float));
         if (!ok) return;
     }
     if ((MODE && a.init && !DBG_REGION(a.init + (a.segments > 1 ? slot : b) * states + state_at, (size_t)pw * a.N * 4)) ||
@@ -208,7 +211,6 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
     tc_before();
     __syncthreads();
     tc_after();
-    constexpr uint32_t tmem = 0;            // all 512 columns: they begin at 0
     auto left = [&](int c) { return min(TC_Q, t_hi - t_lo - c * TC_Q); };      // tokens of a chunk
     const int chunks = t_hi > t_lo ? (t_hi - t_lo + TC_Q - 1) / TC_Q : 0, dir = a.backwards ? -1 : 1;
     const int t_first = a.backwards ? t_hi - 1 : t_lo;
@@ -222,11 +224,20 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
         constexpr uint32_t I_S = IDESC | (16u << 17), I_H = IDESC | (1u << 15) | (1u << 16) | ((8u * Lay::H_PARTS) << 17);
         constexpr uint32_t I_O1 = IDESC | (16u << 17) | (Lay::GRAD ? 0 : 1u << 16), I_O2 = IDESC | (1u << 16) | ((Lay::DV / 8) << 17);
         constexpr uint32_t STEP = PANEL >> 4, QK = Lay::OUT ? 8 : 4;                        // steps of 16 along q's columns
-        // One thread issues, and what it computes per product counts: the set of operands is known when compiled, so addresses are sums with constants.
-        const uint32_t d0 = tc_desc(base);
-        auto chunk = [&](int c, auto which) {
-            constexpr uint32_t set = decltype(which)::value;
-            const uint32_t pq = d0 + Lay::q * STEP, pw_ = d0 + Lay::w * STEP, ps = d0 + Lay::st * STEP, pb = d0 + (Lay::broad + 2 * set) * STEP,
+        // One thread issues, and what it computes per product counts: with everything unrolled and the operands' set known when compiled the scan of
+        // 65536 tokens takes 300 us, in loops 343.  But a chunk's work has to stay in instruction caches that neighbouring SMs share: where they
+        // run different sweeps (the backward pass), unrolled code took turns of up to twice the time, and loops are used (529 -> 475 us).
+        auto product = [&](uint32_t d, uint32_t left, uint32_t left_step, uint32_t right, uint32_t right_step, uint32_t idesc, uint32_t n, bool add, auto from_tmem) {
+#pragma unroll UNROLL
+            for (uint32_t k = 0; k < n; k++, left += left_step, right += right_step, add = true) {
+                if constexpr (decltype(from_tmem)::value) tc_mma_ts(d, left, right, idesc, add);
+                else tc_mma_ss(d, left, right, idesc, add);
+            }
+        };
+        constexpr std::false_type SHARED{};
+        constexpr std::true_type TENSOR{};
+        auto chunk = [&](int c, uint32_t set) {
+            const uint32_t d0 = tc_desc(base), pq = d0 + Lay::q * STEP, pw_ = d0 + Lay::w * STEP, ps = d0 + Lay::st * STEP, pb = d0 + (Lay::broad + 2 * set) * STEP,
                            pn = d0 + (Lay::narrow + set) * STEP;
             if (MODE) {
                 wait(b_kv + 8 * set, c >> 1);
@@ -234,44 +245,41 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                 if (c) wait(b_o, c - 1);                             // the scores' planes lie over the scores
                 tc_after();
 #pragma unroll
-                for (uint32_t k = 0; k < QK; k++) {
-                    const uint32_t at = (k >> 2) * STEP + (k & 3) * 2;
-                    tc_mma_ss(tmem + Lay::S, pq + at, (Lay::OUT ? pb : pn) + at, I_S, k);
-                }
+                for (uint32_t j = 0; j < QK / 4; j++) product(Lay::S, pq + j * STEP, 2, (Lay::OUT ? pb : pn) + j * STEP, 2, I_S, 4, j, SHARED);
                 tc_commit(b_s);
             }
             wait(b_wv, c);
             tc_after();
 #pragma unroll
-            for (uint32_t p = 0; p < (Lay::H_PARTS == 1 ? NS : 1); p++)
-#pragma unroll
-                for (uint32_t k = 0; k < 8; k++) tc_mma_ss(tmem + Lay::H, pb + k * 128, pw_ + p * STEP + k * 128, I_H, p || k);
+            for (uint32_t p = 0; p < (Lay::H_PARTS == 1 ? NS : 1); p++) product(Lay::H, pb, 128, pw_ + p * STEP, 128, I_H, 8, p, SHARED);
             tc_commit(b_h);
             if (MODE) {
                 if (c) wait(b_used + 8 * (set ^ 1), (c - 1) >> 1);
                 tc_after();
+                if (Lay::OUT) {
 #pragma unroll
-                for (uint32_t p = 0; p < (Lay::OUT ? 1 : NO); p++)
+                    for (uint32_t j = 0; j < 2; j++) product(Lay::O1, pq + j * STEP, 2, ps + 512 * j, 128, I_O1, 4, j, SHARED);
+                } else {
 #pragma unroll
-                    for (uint32_t k = 0; k < QK; k++)
-                        tc_mma_ss(tmem + Lay::O1, pq + (k >> 2) * STEP + (k & 3) * 2, ps + p * STEP + (Lay::OUT ? k * 128 : k * 2), I_O1, p || k);
+                    for (uint32_t p = 0; p < NO; p++) product(Lay::O1, pq, 2, ps + p * STEP, 2, I_O1, 4, p, SHARED);
+                }
                 tc_commit(b_o1);
-            }
-            if (MODE) {
                 wait(b_p, c);
                 tc_after();
 #pragma unroll
                 for (uint32_t p = 0; p < NO; p++)
-#pragma unroll
-                    for (uint32_t k = 0; k < 8; k++)
-                        tc_mma_ts(tmem + Lay::O2, tmem + (p < 2 ? Lay::S + 16 * k + 8 * p : Lay::P3 + 8 * k), (Lay::GRAD ? pb : pn) + k * 128, I_O2, p || k);
+                    product(Lay::O2, p < 2 ? Lay::S + 8 * p : Lay::P3, p < 2 ? 16 : 8, Lay::GRAD ? pb : pn, 128, I_O2, 8, p, TENSOR);
                 tc_commit(b_o);
             }
         };
         if (lane == 0) {
-            for (int c = 0; c < chunks; c += 2) {
-                chunk(c, std::integral_constant<uint32_t, 0>());
-                if (c + 1 < chunks) chunk(c + 1, std::integral_constant<uint32_t, 1>());
+            if constexpr (UNROLL > 4) {
+                for (int c = 0; c < chunks; c += 2) {
+                    chunk(c, 0);
+                    if (c + 1 < chunks) chunk(c + 1, 1);
+                }
+            } else {
+                for (int c = 0; c < chunks; c++) chunk(c, c & 1);
             }
             tc_commit(drained);
             mbar_wait_bounded(drained, 0);
@@ -447,7 +455,7 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                 };
                 if (part < quarter) {
                     const float r = ex2((ci.x - d.ref[part].x) + (ci.y - d.ref[part].y));
-#pragma unroll
+#pragma unroll 1
                     for (int h = 0; h < 2; h++) {
                         f2 x[8];
                         uint32_t pl[8][NO];
@@ -461,7 +469,7 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                         write(pl, h);
                     }
                 } else if (part == quarter) {
-#pragma unroll
+#pragma unroll 1
                     for (int h = 0; h < 2; h++) {
                         f2 x[8];
                         uint32_t pl[8][NO];
@@ -480,7 +488,9 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                     }
                 } else {
                     const uint32_t pl[8][NO] = {};
-                    write(pl, 0), write(pl, 1);
+                    
+#pragma unroll 1
+                    for (int h = 0; h < 2; h++) write(pl, h);
                 }
                 tc_wait_st();
                 tc_before();
@@ -547,19 +557,12 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                     if (count >= 16) *reinterpret_cast<uint4*>(out + 8) = make_uint4(o[4], o[5], o[6], o[7]);
                 }
             } else {
-                // u's part of the row is on its way while the products finish
-                uint32_t u[16];
-                const T* pu = scan_row<T>(a.u, b, t_first + (long long)dir * (c * TC_Q + min((int)row, valid - 1)), head, group, tile) + 32 * part;
-#pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    const uint4 v = 32 * part + 8 * k < a.N ? *reinterpret_cast<const uint4*>(pu + 8 * k) : make_uint4(0, 0, 0, 0);
-                    u[4 * k] = v.x, u[4 * k + 1] = v.y, u[4 * k + 2] = v.z, u[4 * k + 3] = v.w;
-                }
+                // A warp's 32 rows x 32 columns lie together, a thread's eight columns after another's (the sums read them the same way): as rows of
+                // a matrix they would be 32 pieces of 32 bytes per store, and a chunk's stores took 4000 cycles.
+                float* to_part = a.part + ((((size_t)b * vheads + vh) * a.segments + seg) * (a.seg_chunks / 2) + c) * (TC_Q * 128) + (quarter * 4 + part) * 1024 + lane * 8;
                 wait(b_o, c);
                 tc_after();
-                f2 dot = {0.f, 0.f};
-                float* to_part = a.part + (((size_t)b * vheads + vh) * a.L + t) * 128 + 32 * part;
-#pragma unroll
+#pragma unroll 1
                 for (int k = 0; k < 2; k++) {
                     uint32_t x[16], y[16];
                     tc_ld16(x, lanes + Lay::O1 + 32 * part + 16 * k);
@@ -572,12 +575,10 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
 #pragma unroll
                     for (int e = 0; e < 8; e++) {
                         const f2 v = fma2({grow, grow}, {__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])}, {__uint_as_float(y[2 * e]), __uint_as_float(y[2 * e + 1])});
-                        dot = fma2(v, both(u[8 * k + e]), dot);
                         x[2 * e] = __float_as_uint(v.x), x[2 * e + 1] = __float_as_uint(v.y);
                     }
-                    if (live) st32(to_part + 16 * k, x), st32(to_part + 16 * k + 8, x + 8);
+                    if (live) st32(to_part + 512 * k, x), st32(to_part + 512 * k + 256, x + 8);
                 }
-                if (live) a.dots[(((size_t)b * vheads + vh) * SCAN_DOTS + part) * a.L + t] = dot.x + dot.y;
             }
         }
         if (a.last && (MODE == MODE_STATE || is_last)) {
@@ -622,19 +623,88 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
 __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc_state(const __grid_constant__ ScanSet s) {
     __shared__ TcShared sh;
     pdl_begin();
-    tc_sweep<MODE_STATE>(s.a[blockIdx.x % s.count], blockIdx.x / s.count, sh);
+    tc_sweep<MODE_STATE, 8>(s.a[blockIdx.x % s.count], blockIdx.x / s.count, sh);
 }
 __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const __grid_constant__ ScanSet s) {
     __shared__ TcShared sh;
     pdl_begin();
-    tc_sweep<MODE_OUT>(s.a[0], blockIdx.x, sh);
+    tc_sweep<MODE_OUT, 8>(s.a[0], blockIdx.x, sh);
 }
 __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc_backward(const __grid_constant__ ScanSet s) {
     __shared__ TcShared sh;
     pdl_begin();
     const uint32_t which = blockIdx.x % 3, block = blockIdx.x / 3;
-    if (which < 2) tc_sweep<MODE_GRAD>(s.a[which], block, sh);
-    else tc_sweep<MODE_OUT>(s.a[2], block, sh);
+    if (which < 2) tc_sweep<MODE_GRAD, TC_BACK_UNROLL>(s.a[which], block, sh);
+    else tc_sweep<MODE_OUT, TC_BACK_UNROLL>(s.a[2], block, sh);
+}
+
+// Sums of the tcgen05 sweeps' dB and dC over the heads of a group, and what each head's rows give with the rows of C and B (for the gradient of the
+// log decays).  A block has 32 positions of a chunk, a warp 16 columns of them, a thread one position; heads one after the other.
+#define SUM_HEADS 16
+__global__ void __launch_bounds__(256) k_clear_scan_tc_sums(const TcSums a) {
+    __shared__ float dots[SUM_HEADS][8][33];
+    pdl_begin();
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, which = blockIdx.x & 1, quarter = (blockIdx.x >> 1) & 3;
+    const uint32_t per_seg = a.seg_chunks / 2, chunk = (blockIdx.x >> 3) % per_seg, seg = (blockIdx.x >> 3) / per_seg, grp = blockIdx.y, b = blockIdx.z;
+    const int length = a.lengths ? min(max(a.lengths[b], 0), (int)a.L) : (int)a.L;
+    const int t_lo = (int)(seg * a.seg_chunks) * SCAN_Q, t_hi = min(length, t_lo + (int)a.seg_chunks * SCAN_Q), at = (int)(chunk * TC_Q + quarter * 32);
+    if (t_lo + at >= t_hi) return;                                  // none of these positions exists
+    const int pos = at + (int)lane, t = which ? t_hi - 1 - pos : t_lo + pos;          // 0: dC, forwards; 1: dB, backwards
+    const bool live = t_lo + pos < t_hi;
+    const uint32_t vheads = a.H * a.tiles, per = vheads / a.G, n = 16 * warp;
+    const size_t step = (size_t)a.segments * per_seg * (TC_Q * 128);
+    const float* src = (which ? a.part_b : a.part_c) + ((size_t)b * vheads + grp * per) * step + ((size_t)seg * per_seg + chunk) * (TC_Q * 128) +
+                       (quarter * 4 + (warp >> 1)) * 1024 + (warp & 1) * 512 + lane * 8;
+    const ScanOperand& o = which ? a.uB : a.uC;
+    __nv_bfloat16* dst = which ? a.dB + b * a.Bb + t * a.Bt + grp * a.Bg : a.dC + b * a.Cb + t * a.Ct + grp * a.Cg;
+    if (!DBG_REGION(src - lane * 8, ((per - 1) * step + 768) * sizeof(float)) || (live && !DBG_REGION(dst, a.N * sizeof(__nv_bfloat16)))) return;
+    f2 u[8], sum[8] = {};
+    {
+        const __nv_bfloat16* pu = (const __nv_bfloat16*)o.p + b * o.sb + t * o.st + grp * o.sh + n;
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const uint4 v = live && n + 8 * k < a.N ? *reinterpret_cast<const uint4*>(pu + 8 * k) : make_uint4(0, 0, 0, 0);
+            u[4 * k] = both(v.x), u[4 * k + 1] = both(v.y), u[4 * k + 2] = both(v.z), u[4 * k + 3] = both(v.w);
+        }
+    }
+    float* out = which ? a.col : a.row;
+    for (uint32_t h0 = 0; h0 < per; h0 += SUM_HEADS) {
+        const uint32_t heads = min(per - h0, (uint32_t)SUM_HEADS);
+        if (live) {
+#pragma unroll 4
+            for (uint32_t h = 0; h < heads; h++) {
+                const float4* p = reinterpret_cast<const float4*>(src + (h0 + h) * step);
+                const float4 v[4] = {p[0], p[1], p[64], p[65]};
+                f2 dot = {0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    const f2 x = {v[k].x, v[k].y}, y = {v[k].z, v[k].w};
+                    sum[2 * k] = add2(sum[2 * k], x), sum[2 * k + 1] = add2(sum[2 * k + 1], y);
+                    dot = fma2(u[2 * k + 1], y, fma2(u[2 * k], x, dot));
+                }
+                dots[h][warp][lane] = dot.x + dot.y;
+            }
+        }
+        __syncthreads();
+        for (uint32_t i = warp; i < heads; i += 8)
+            if (live) {
+                float s = 0.f;
+#pragma unroll
+                for (int w = 0; w < 8; w++) s += dots[i][w][lane];
+                out[((size_t)b * vheads + grp * per + h0 + i) * a.L + t] = s;
+            }
+        __syncthreads();
+    }
+    if (live) {
+#pragma unroll
+        for (int k = 0; k < 2; k++)
+            if (n + 8 * k < a.N)
+                *reinterpret_cast<uint4*>(dst + n + 8 * k) = make_uint4(pack_bf16(sum[4 * k].x, sum[4 * k].y), pack_bf16(sum[4 * k + 1].x, sum[4 * k + 1].y),
+                                                                       pack_bf16(sum[4 * k + 2].x, sum[4 * k + 2].y), pack_bf16(sum[4 * k + 3].x, sum[4 * k + 3].y));
+    }
+}
+cudaError_t scan_tc_sums(const TcSums& a, uint32_t batch, cudaStream_t st) {
+    return launch(k_clear_scan_tc_sums, dim3(8 * a.segments * (a.seg_chunks / 2), a.G, batch), dim3(256), 0, st, a);
 }
 
 cudaError_t scan_tc_launch(const ScanSet& s, int mode, cudaStream_t st) {
