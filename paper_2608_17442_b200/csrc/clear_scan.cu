@@ -85,9 +85,10 @@ struct FinishArgs {
 };
 // What is left of the backward pass, by block: sums of dB and dC over the heads of a group; the gradient of the log decays, a block per
 // sequence, head and segment; that of the skip.
-template <class T>
-__global__ void __launch_bounds__(256) k_clear_scan_finish(const FinishArgs a) {
-    __shared__ double words[2][8];
+template <class T, int THREADS>
+__global__ void __launch_bounds__(THREADS) k_clear_scan_finish(const FinishArgs a) {
+    constexpr uint32_t WARPS = THREADS / 32;
+    __shared__ double words[2][WARPS];
     pdl_begin();
     const uint32_t vheads = a.H * a.tiles, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     auto tokens = [&](uint32_t b) { return a.lengths ? min(max(a.lengths[b], 0), (int)a.L) : (int)a.L; };
@@ -113,7 +114,7 @@ __global__ void __launch_bounds__(256) k_clear_scan_finish(const FinishArgs a) {
     }
     const uint32_t blk = blockIdx.x - a.sum_blocks;
     if (blk < a.dg_blocks) {
-        // R_t = R_{t+1} + row_t - col_t from the segment's end, 256 tokens at a time; the next ones' words are read while these are summed
+        // R_t = R_{t+1} + row_t - col_t from the segment's end, a token a thread; the next ones' words are read while these are summed
         const uint32_t head = blk % a.H, seg = blk / a.H % a.segments, b = blk / a.H / a.segments;
         const int length = tokens(b), lo = (int)(seg * a.seg_chunks) * SCAN_Q, hi = min(length, lo + (int)a.seg_chunks * SCAN_Q);
         if (lo >= hi) return;
@@ -134,20 +135,20 @@ __global__ void __launch_bounds__(256) k_clear_scan_finish(const FinishArgs a) {
         };
         read(hi - 1 - (int)tid);
         uint32_t turn = 0;
-        for (int top = hi - 1; top >= lo; top -= 256, turn ^= 1) {
+        for (int top = hi - 1; top >= lo; top -= THREADS, turn ^= 1) {
             const int t = top - (int)tid;
             double v = next;
             const bool drop = next_drop;
-            read(t - 256);
+            read(t - THREADS);
             // a dropped state has the gradient zero, from which the sum goes on: what a token adds up goes back to the nearest drop at or behind it
             if (__syncthreads_or(drop)) {
                 // seldom: token by token
-                __shared__ double all[256];
-                __shared__ bool drops[256];
+                __shared__ double all[THREADS];
+                __shared__ bool drops[THREADS];
                 all[tid] = v, drops[tid] = drop;
                 __syncthreads();
                 if (tid == 0)
-                    for (int k = 0; k < 256 && top - k >= lo; k++) {
+                    for (int k = 0; k < THREADS && top - k >= lo; k++) {
                         run = drops[k] ? 0.0 : run + all[k];
                         dg[(long long)(top - k) * a.gt] = (float)run;
                     }
@@ -164,20 +165,20 @@ __global__ void __launch_bounds__(256) k_clear_scan_finish(const FinishArgs a) {
             }
             if (lane == 31) words[turn][warp] = v;
             __syncthreads();
-            double total = 0.0, before = 0.0;
+            double sums = lane < WARPS ? words[turn][lane] : 0.0;
 #pragma unroll
-            for (uint32_t w = 0; w < 8; w++) {
-                const double x = words[turn][w];
-                if (w < warp) before += x;
-                total += x;
+            for (int o = 1; o < (int)WARPS; o <<= 1) {
+                const double u = __shfl_up_sync(~0u, sums, o);
+                if ((int)lane >= o) sums += u;
             }
-            if (t >= lo) dg[t * a.gt] = (float)(run + before + v);
-            run += total;
+            const double before = __shfl_sync(~0u, sums, warp ? warp - 1 : 0);
+            if (t >= lo) dg[t * a.gt] = (float)(run + (warp ? before : 0.0) + v);
+            run += __shfl_sync(~0u, sums, WARPS - 1);
         }
         return;
     }
     // the skip: a warp per head
-    const uint32_t head = (blk - a.dg_blocks) * 8 + warp;
+    const uint32_t head = (blk - a.dg_blocks) * WARPS + warp;
     if (!a.dskip || head >= a.H) return;
     double s = 0.0;
     const size_t all = (size_t)a.b * a.segments * a.tiles;
@@ -261,18 +262,30 @@ struct ScanShape {
     size_t states, state_floats, decay_floats, part_floats, dot_floats, end_floats;
 };
 
-// Segments: as many as fill the SMs, with three CTAs each on mma.sync (none shorter than two chunks of 64: a segment adds a pass over its keys and
-// values, and a state written and read) or one on tcgen05 (chunks of 128).
-static ScanShape scan_shape(const fesc_clear_scan_desc* d) {
+// The shape of a call's sweeps, the backward pass's three at once.  Segments: what takes least time by a model in pieces of 128 tokens.  A CTA takes
+// as long as its pieces and START of them besides (pieces are slower on mma.sync); a grid as many rounds of that as its CTAs fill the places where they run; with more than
+// one segment a pass over the keys and values, at a third (mma.sync: half) of the time a piece, and the chaining come first.  (2048 tokens of 24 heads on tcgen05: forwards 6
+// segments, 30 us, with one 65; backwards 2, 95 us, with 6 128.)
+static ScanShape scan_shape(const fesc_clear_scan_desc* d, bool backward) {
     ScanShape s;
     s.tc = d->type == FESC_BF16 && d->N > 64 && d->N % 8 == 0 && d->P % 8 == 0;
     s.tiles = (d->P + SCAN_TILE - 1) / SCAN_TILE, s.vheads = d->H * s.tiles, s.np = d->N > 64 ? 128 : 64;
-    // in pieces of 128 tokens
-    const uint64_t pieces = ((uint64_t)d->L + 127) / 128, ctas = (uint64_t)d->batch * s.vheads;
-    uint64_t want = !ctas ? 1 : s.tc ? 148 / ctas : (3 * 148 + ctas - 1) / ctas;
-    if (want > pieces) want = pieces;
-    if (want < 1) want = 1;
-    const uint64_t each = pieces ? (pieces + want - 1) / want : 1;
+    const uint64_t pieces = ((uint64_t)d->L + 127) / 128, ctas = (uint64_t)d->batch * s.vheads, sweeps = backward ? 3 : 1;
+    const double START = s.tc ? 2.0 : 0.5, CHAIN = s.tc ? 1.5 : 0.5, STATE = s.tc ? 0.35 : 0.5;
+    // CTAs of a sweep on an SM, by shared memory
+    const uint64_t places = 148 * (s.tc ? 1 : d->type == FESC_BF16 ? 3 : d->type == FESC_F16 ? (d->N > 64 ? 2 : 3) : (d->N > 64 ? 1 : 2));
+    uint64_t each = pieces ? pieces : 1, last = 0;
+    double least = 1e300;
+    for (uint64_t want = 1; want <= pieces && want <= 1024; want++) {
+        const uint64_t of = (pieces + want - 1) / want, segments = (pieces + of - 1) / of;
+        if (segments == last) continue;
+        last = segments;
+        auto rounds = [&](uint64_t n) { return (double)((n * ctas * segments + places - 1) / places); };
+        double time = rounds(sweeps) * (START + of);
+        if (segments > 1) time += rounds(backward ? 2 : 1) * (START + STATE * of) + CHAIN;
+        if (time < least) each = of, least = time;
+        if (ctas * segments > 8 * places) break;          // more only adds rounds
+    }
     s.seg_chunks = (uint32_t)(each * (128 / SCAN_Q));
     s.segments = pieces ? (uint32_t)((pieces + each - 1) / each) : 1;
     s.states = (size_t)d->H * d->P * d->N;
@@ -292,9 +305,10 @@ static const char* scan_check(const fesc_clear_scan_desc* d) {
     if (d->N > SCAN_MAX_STATE) return "clear_scan: states of more than 128 columns";
     if (d->G > 65535) return "clear_scan: more than 65535 groups";
     if (d->P > 4096 || d->L >= (1u << 30)) return "clear_scan: more than 4096 channels of a head or 2^30 tokens";
-    const ScanShape s = scan_shape(d);
-    if (3 * (uint64_t)d->batch * s.segments * s.vheads >= (1ull << 31) || d->batch > 65535 ||
-        (uint64_t)d->batch * d->G * ((uint64_t)d->L / 8 + 1) * 2 + (uint64_t)d->batch * d->H * s.segments >= (1ull << 31) - d->H || (uint64_t)d->H * d->P * d->N >= (1ull << 31))
+    const ScanShape s = scan_shape(d, false), back = scan_shape(d, true);
+    const uint64_t segments = std::max(s.segments, back.segments);
+    if (3 * (uint64_t)d->batch * segments * s.vheads >= (1ull << 31) || d->batch > 65535 ||
+        (uint64_t)d->batch * d->G * ((uint64_t)d->L / 8 + 1) * 2 + (uint64_t)d->batch * d->H * segments >= (1ull << 31) - d->H || (uint64_t)d->H * d->P * d->N >= (1ull << 31))
         return "clear_scan: too many sequences, heads or tokens for one call";
     return nullptr;
 }
@@ -347,12 +361,12 @@ static cudaError_t combine(const fesc_clear_scan_desc* d, const ScanShape& s, co
 
 extern "C" size_t fesc_clear_scan_work(const fesc_clear_scan_desc* desc) {
     if (!desc || scan_check(desc)) return 0;
-    const ScanShape s = scan_shape(desc);
+    const ScanShape s = scan_shape(desc, false);
     return (s.state_floats + s.decay_floats) * sizeof(float);
 }
 extern "C" size_t fesc_clear_scan_backward_work(const fesc_clear_scan_desc* desc) {
     if (!desc || scan_check(desc)) return 0;
-    const ScanShape s = scan_shape(desc);
+    const ScanShape s = scan_shape(desc, true);
     return (2 * (s.state_floats + s.decay_floats + s.part_floats + s.dot_floats + s.end_floats)) * sizeof(float);
 }
 
@@ -368,7 +382,7 @@ extern "C" int fesc_clear_scan(const fesc_clear_scan_desc* desc, const void* d_x
     if (d.L && (!d_x || !d_g || !d_B || !d_C || !d_y)) return clear_fail(FESC_EINVAL, "clear_scan: x, g, B, C and y have to be given");
     if (same_buffer(d_y, d_x) || same_buffer(d_y, d_B) || same_buffer(d_y, d_C) || same_buffer(d_h_out, d_h0))
         return clear_fail(FESC_EINVAL, "clear_scan: an output is an input");
-    const ScanShape s = scan_shape(desc);
+    const ScanShape s = scan_shape(desc, false);
     const size_t need = fesc_clear_scan_work(desc);
     if (need && (!d_work || ((size_t)d_work & 255) || work_bytes < need))
         return clear_fail(FESC_EINVAL, "clear_scan: the workspace is too small or not aligned to 256 bytes");
@@ -418,7 +432,7 @@ extern "C" int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const 
         for (int j = 0; j < i; j++)
             if (same_buffer(outs[i], outs[j])) return clear_fail(FESC_EINVAL, "clear_scan_backward: two outputs are the same");
     }
-    const ScanShape s = scan_shape(desc);
+    const ScanShape s = scan_shape(desc, true);
     const size_t need = fesc_clear_scan_backward_work(desc);
     if (!d_work || ((size_t)d_work & 255) || work_bytes < need)
         return clear_fail(FESC_EINVAL, "clear_scan_backward: the workspace is too small or not aligned to 256 bytes");
@@ -462,9 +476,13 @@ extern "C" int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const 
     } else {
         f.sum_each = (uint32_t)(((size_t)d.L * (s.np / 4) + 255) / 256), f.sum_blocks = 2 * d.batch * d.G * f.sum_each;
     }
-    const dim3 grid(f.sum_blocks + f.dg_blocks + (d.H + 7) / 8);
-    auto kernel = d.type == FESC_BF16 ? k_clear_scan_finish<__nv_bfloat16> : d.type == FESC_F16 ? k_clear_scan_finish<__half> : k_clear_scan_finish<float>;
-    CLEAR_CUDA(launch(kernel, grid, dim3(256), 0, st, f));
+    auto finish = [&](auto kernel, uint32_t threads) {
+        return launch(kernel, dim3(f.sum_blocks + f.dg_blocks + (d.H + threads / 32 - 1) / (threads / 32)), dim3(threads), 0, st, f);
+    };
+    if (tc) CLEAR_CUDA(finish(k_clear_scan_finish<__nv_bfloat16, 1024>, 1024));
+    else if (d.type == FESC_BF16) CLEAR_CUDA(finish(k_clear_scan_finish<__nv_bfloat16, 256>, 256));
+    else if (d.type == FESC_F16) CLEAR_CUDA(finish(k_clear_scan_finish<__half, 256>, 256));
+    else CLEAR_CUDA(finish(k_clear_scan_finish<float, 256>, 256));
     return FESC_OK;
 }
 

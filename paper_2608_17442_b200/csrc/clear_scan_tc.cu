@@ -25,9 +25,7 @@
 
 #define TC_Q 128
 #define PANEL 16384u
-#ifndef TC_BACK_UNROLL
-#define TC_BACK_UNROLL 2
-#endif
+#define TC_BACK_UNROLL 2        // products in a row in the backward pass: 469 us (1: 470, 4: 482; all of them in the scan 299, 4 there 314)
 #define TC_WARPS 16             // that compute; one more issues, one more sums decays, two copy
 #define TC_THREADS (32 * (TC_WARPS + 4))
 
@@ -35,14 +33,15 @@ template <int MODE>
 struct TcLayout {
     static constexpr bool GRAD = MODE == MODE_GRAD, OUT = MODE == MODE_OUT;
     static constexpr int NO = GRAD ? 3 : 2;                        // planes of scores and states
-    // panels in shared memory; k and v have two sets
+    // panels in shared memory; k and v have two sets (without outputs the faded values, too: they are formed while the product before runs)
     static constexpr int q = 0, QP = OUT ? 2 : GRAD ? 1 : 0;
-    static constexpr int broad = QP, narrow = broad + 4, w = narrow + 2, st = w + 3, panels = st + (MODE ? NO : 0);
+    static constexpr int broad = QP, narrow = broad + 4, w = narrow + 2, W_SETS = MODE ? 1 : 2, st = w + 3 * W_SETS, panels = st + (MODE ? NO : 0);
     // Columns of tensor memory, of which a CTA takes all 512: they begin at 0.  The first two planes of 16 decayed scores lie over the 16 scores, so a warp overwrites what it
     // has read itself; a third plane has columns of its own.
     static constexpr uint32_t DV = GRAD ? 128 : 64, O1_PARTS = OUT ? 2 : 1, H_PARTS = GRAD ? 1 : 3;      // accumulators side by side, one per plane
     static constexpr uint32_t S = 0, P3 = 128, O1 = GRAD ? 192 : 128, O2 = O1 + O1_PARTS * DV, H = MODE ? O2 + DV : 0, columns = 512;
-    static_assert(H + 64 * H_PARTS <= columns, "accumulators fit");
+    static constexpr uint32_t H_SET = MODE ? 0 : 64 * H_PARTS;      // from one set's H to the other's
+    static_assert(H + H_SET + 64 * H_PARTS <= columns, "accumulators fit");
     static constexpr size_t bytes = (size_t)panels * PANEL + 1024;  // panels start on 1024 bytes
 };
 
@@ -136,7 +135,7 @@ __device__ __forceinline__ void st32(void* p, const uint32_t* v) {
 
 struct TcShared {
     TcDecays decays[2];
-    alignas(8) u64 bars[14];        // see below
+    alignas(8) u64 bars[16];        // see below
     uint32_t tmem_base;
     volatile uint32_t dead;         // a wait gave up: the rest of the chunks goes through without waiting, with nothing of worth in it
     float words[2][TC_WARPS];
@@ -190,21 +189,21 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
 #endif
     const uint32_t base = ((uint32_t)__cvta_generic_to_shared(tc_smem) + 1023) & ~1023u, bar = (uint32_t)__cvta_generic_to_shared(bars);
     uint8_t* const panels = tc_smem + (base - (uint32_t)__cvta_generic_to_shared(tc_smem));
-    // per chunk: q copied; faded values and state, decayed scores written; products S, O1, H, O2 done.  No one gets to what completes a barrier's
-    // next phase before everyone who waits for this one has.
-    const uint32_t b_q = bar, b_wv = bar + 8, b_o1 = bar + 16, b_p = bar + 24, b_s = bar + 32, b_h = bar + 40, b_o = bar + 48, drained = bar + 56;
-    // Of the two sets of decays and of k and v: filled, and all used (and O1 and O2 read).  A set has barriers of its own because those who fill them
-    // run up to two chunks ahead: two phases of one barrier would be over before some warp has waited for the first, which then looks like the third.
-    const uint32_t b_g = bar + 64, b_used = bar + 80, b_kv = bar + 96;
+    // Per chunk: q copied; decayed scores written; products S, O1, O2 done.  Of the two sets of chunks: faded values and state written, H done, decays
+    // filled, k and v copied, all used (and O1 and O2 read).  No one may get to what completes a barrier's next phase before everyone who waits for
+    // this one has: two phases on, a barrier looks as it did before.  Where those who complete it run up to two chunks ahead, each set has a
+    // barrier of its own.
+    const uint32_t b_q = bar, b_p = bar + 8, b_s = bar + 16, b_o1 = bar + 24, b_o = bar + 32, drained = bar + 40;
+    const uint32_t b_wv = bar + 48, b_h = bar + 64, b_g = bar + 80, b_kv = bar + 96, b_used = bar + 112;
     if (warp == TC_WARPS) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"((uint32_t)__cvta_generic_to_shared(&tmem_base)), "n"(Lay::columns)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     if (tid == 0) {
-        mbar_init(b_q, 2), mbar_init(b_wv, TC_WARPS), mbar_init(b_p, TC_WARPS), mbar_init(b_o1, 1);
-        for (uint32_t i = 0; i < 2; i++) mbar_init(b_g + 8 * i, 1), mbar_init(b_used + 8 * i, TC_WARPS), mbar_init(b_kv + 8 * i, 2);
-        mbar_init(b_s, 1), mbar_init(b_h, 1), mbar_init(b_o, 1), mbar_init(drained, 1);
+        mbar_init(b_q, 2), mbar_init(b_p, TC_WARPS), mbar_init(b_s, 1), mbar_init(b_o1, 1), mbar_init(b_o, 1), mbar_init(drained, 1);
+        for (uint32_t i = 0; i < 16; i += 8)
+            mbar_init(b_wv + i, TC_WARPS), mbar_init(b_h + i, 1), mbar_init(b_g + i, 1), mbar_init(b_kv + i, 2), mbar_init(b_used + i, TC_WARPS);
         dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -237,7 +236,7 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
         constexpr std::false_type SHARED{};
         constexpr std::true_type TENSOR{};
         auto chunk = [&](int c, uint32_t set) {
-            const uint32_t d0 = tc_desc(base), pq = d0 + Lay::q * STEP, pw_ = d0 + Lay::w * STEP, ps = d0 + Lay::st * STEP, pb = d0 + (Lay::broad + 2 * set) * STEP,
+            const uint32_t d0 = tc_desc(base), pq = d0 + Lay::q * STEP, pw_ = d0 + (Lay::w + (Lay::W_SETS == 2 ? 3 * set : 0)) * STEP, ps = d0 + Lay::st * STEP, pb = d0 + (Lay::broad + 2 * set) * STEP,
                            pn = d0 + (Lay::narrow + set) * STEP;
             if (MODE) {
                 wait(b_kv + 8 * set, c >> 1);
@@ -248,11 +247,12 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                 for (uint32_t j = 0; j < QK / 4; j++) product(Lay::S, pq + j * STEP, 2, (Lay::OUT ? pb : pn) + j * STEP, 2, I_S, 4, j, SHARED);
                 tc_commit(b_s);
             }
-            wait(b_wv, c);
+            wait(b_wv + 8 * set, c >> 1);
             tc_after();
 #pragma unroll
-            for (uint32_t p = 0; p < (Lay::H_PARTS == 1 ? NS : 1); p++) product(Lay::H, pb, 128, pw_ + p * STEP, 128, I_H, 8, p, SHARED);
-            tc_commit(b_h);
+            for (uint32_t p = 0; p < (Lay::H_PARTS == 1 ? NS : 1); p++)
+                product(Lay::H + Lay::H_SET * set, pb, 128, pw_ + p * STEP, 128, I_H, 8, p, SHARED);
+            tc_commit(b_h + 8 * set);
             if (MODE) {
                 if (c) wait(b_used + 8 * (set ^ 1), (c - 1) >> 1);
                 tc_after();
@@ -422,10 +422,10 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
             uint32_t pl[8][3];
 #pragma unroll
             for (int e = 0; e < 8; e++) split2<NS>(mul2(both(u[e]), {f, f}), pl[e]);
-            put(Lay::w, pl, NS);
+            put(Lay::w + (Lay::W_SETS == 2 ? 3 * (c & 1) : 0), pl, NS);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             tc_before();
-            arrive(b_wv);
+            arrive(b_wv + 8 * (c & 1));
         };
         if (chunks) provide(0);
         for (int c = 0; c < chunks; c++) {
@@ -496,13 +496,14 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                 tc_before();
                 arrive(b_p);
             }
-            wait(b_h, c);
+            if (!MODE && c + 1 < chunks) provide(c + 1);      // into the other set, while this chunk's product runs
+            wait(b_h + 8 * set, c >> 1);
             tc_after();
             {
                 const float keep = d.keep;
                 uint32_t x[Lay::H_PARTS][16];
 #pragma unroll
-                for (int p = 0; p < (int)Lay::H_PARTS; p++) tc_ld16(x[p], lanes + Lay::H + 64 * p + 16 * part);
+                for (int p = 0; p < (int)Lay::H_PARTS; p++) tc_ld16(x[p], lanes + Lay::H + Lay::H_SET * set + 64 * p + 16 * part);
                 tc_wait_ld();
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
@@ -514,8 +515,8 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                 }
             }
             const float grow = d.grow[row];
-            if (c + 1 < chunks) {
-                if (MODE) wait(b_o1, c);       // the state's panels are free
+            if (MODE && c + 1 < chunks) {
+                wait(b_o1, c);                 // the state's panels are free
                 provide(c + 1);                // before the outputs: O2 is under way
             }
             if (!MODE) {
@@ -639,10 +640,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc_backward(const 
 }
 
 // Sums of the tcgen05 sweeps' dB and dC over the heads of a group, and what each head's rows give with the rows of C and B (for the gradient of the
-// log decays).  A block has 32 positions of a chunk, a warp 16 columns of them, a thread one position; heads one after the other.
+// log decays).  A block has 32 positions of a chunk, a warp eight columns of them, a thread one position; heads one after the other, eight on their
+// way at a time.  Bound by memory: 403 MB of 16384 tokens and 24 heads in 70 us.
 #define SUM_HEADS 16
-__global__ void __launch_bounds__(256) k_clear_scan_tc_sums(const TcSums a) {
-    __shared__ float dots[SUM_HEADS][8][33];
+#define SUM_AHEAD 8
+__global__ void __launch_bounds__(512) k_clear_scan_tc_sums(const TcSums a) {
+    __shared__ float dots[SUM_HEADS][16][33];
     pdl_begin();
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, which = blockIdx.x & 1, quarter = (blockIdx.x >> 1) & 3;
     const uint32_t per_seg = a.seg_chunks / 2, chunk = (blockIdx.x >> 3) % per_seg, seg = (blockIdx.x >> 3) / per_seg, grp = blockIdx.y, b = blockIdx.z;
@@ -651,60 +654,58 @@ __global__ void __launch_bounds__(256) k_clear_scan_tc_sums(const TcSums a) {
     if (t_lo + at >= t_hi) return;                                  // none of these positions exists
     const int pos = at + (int)lane, t = which ? t_hi - 1 - pos : t_lo + pos;          // 0: dC, forwards; 1: dB, backwards
     const bool live = t_lo + pos < t_hi;
-    const uint32_t vheads = a.H * a.tiles, per = vheads / a.G, n = 16 * warp;
+    const uint32_t vheads = a.H * a.tiles, per = vheads / a.G, n = 8 * warp;
     const size_t step = (size_t)a.segments * per_seg * (TC_Q * 128);
     const float* src = (which ? a.part_b : a.part_c) + ((size_t)b * vheads + grp * per) * step + ((size_t)seg * per_seg + chunk) * (TC_Q * 128) +
-                       (quarter * 4 + (warp >> 1)) * 1024 + (warp & 1) * 512 + lane * 8;
+                       (quarter * 4 + (warp >> 2)) * 1024 + (warp & 3) * 256 + lane * 8;
     const ScanOperand& o = which ? a.uB : a.uC;
     __nv_bfloat16* dst = which ? a.dB + b * a.Bb + t * a.Bt + grp * a.Bg : a.dC + b * a.Cb + t * a.Ct + grp * a.Cg;
-    if (!DBG_REGION(src - lane * 8, ((per - 1) * step + 768) * sizeof(float)) || (live && !DBG_REGION(dst, a.N * sizeof(__nv_bfloat16)))) return;
-    f2 u[8], sum[8] = {};
-    {
-        const __nv_bfloat16* pu = (const __nv_bfloat16*)o.p + b * o.sb + t * o.st + grp * o.sh + n;
-#pragma unroll
-        for (int k = 0; k < 2; k++) {
-            const uint4 v = live && n + 8 * k < a.N ? *reinterpret_cast<const uint4*>(pu + 8 * k) : make_uint4(0, 0, 0, 0);
-            u[4 * k] = both(v.x), u[4 * k + 1] = both(v.y), u[4 * k + 2] = both(v.z), u[4 * k + 3] = both(v.w);
-        }
-    }
+    if (!DBG_REGION(src - lane * 8, ((per - 1) * step + 256) * sizeof(float)) || (live && !DBG_REGION(dst, a.N * sizeof(__nv_bfloat16)))) return;
+    const bool there = live && n < a.N;
+    const uint4 v = there ? *reinterpret_cast<const uint4*>((const __nv_bfloat16*)o.p + b * o.sb + t * o.st + grp * o.sh + n) : make_uint4(0, 0, 0, 0);
+    const f2 u[4] = {both(v.x), both(v.y), both(v.z), both(v.w)};
+    f2 sum[4] = {};
     float* out = which ? a.col : a.row;
     for (uint32_t h0 = 0; h0 < per; h0 += SUM_HEADS) {
         const uint32_t heads = min(per - h0, (uint32_t)SUM_HEADS);
-        if (live) {
-#pragma unroll 4
-            for (uint32_t h = 0; h < heads; h++) {
-                const float4* p = reinterpret_cast<const float4*>(src + (h0 + h) * step);
-                const float4 v[4] = {p[0], p[1], p[64], p[65]};
-                f2 dot = {0.f, 0.f};
+        for (uint32_t h1 = 0; h1 < heads; h1 += SUM_AHEAD) {
+            float4 x[SUM_AHEAD][2];
 #pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    const f2 x = {v[k].x, v[k].y}, y = {v[k].z, v[k].w};
-                    sum[2 * k] = add2(sum[2 * k], x), sum[2 * k + 1] = add2(sum[2 * k + 1], y);
-                    dot = fma2(u[2 * k + 1], y, fma2(u[2 * k], x, dot));
+            for (uint32_t h = 0; h < SUM_AHEAD; h++)
+                if (there && h1 + h < heads) {
+                    const float4* p = reinterpret_cast<const float4*>(src + (h0 + h1 + h) * step);
+                    x[h][0] = p[0], x[h][1] = p[1];
                 }
-                dots[h][warp][lane] = dot.x + dot.y;
-            }
+#pragma unroll
+            for (uint32_t h = 0; h < SUM_AHEAD; h++)
+                if (h1 + h < heads) {
+                    f2 dot = {0.f, 0.f};
+                    if (there) {
+#pragma unroll
+                        for (int k = 0; k < 2; k++) {
+                            const f2 p = {x[h][k].x, x[h][k].y}, q = {x[h][k].z, x[h][k].w};
+                            sum[2 * k] = add2(sum[2 * k], p), sum[2 * k + 1] = add2(sum[2 * k + 1], q);
+                            dot = fma2(u[2 * k + 1], q, fma2(u[2 * k], p, dot));
+                        }
+                    }
+                    dots[h1 + h][warp][lane] = dot.x + dot.y;
+                }
         }
         __syncthreads();
-        for (uint32_t i = warp; i < heads; i += 8)
+        for (uint32_t i = warp; i < heads; i += 16)
             if (live) {
                 float s = 0.f;
 #pragma unroll
-                for (int w = 0; w < 8; w++) s += dots[i][w][lane];
+                for (int w = 0; w < 16; w++) s += dots[i][w][lane];
                 out[((size_t)b * vheads + grp * per + h0 + i) * a.L + t] = s;
             }
         __syncthreads();
     }
-    if (live) {
-#pragma unroll
-        for (int k = 0; k < 2; k++)
-            if (n + 8 * k < a.N)
-                *reinterpret_cast<uint4*>(dst + n + 8 * k) = make_uint4(pack_bf16(sum[4 * k].x, sum[4 * k].y), pack_bf16(sum[4 * k + 1].x, sum[4 * k + 1].y),
-                                                                       pack_bf16(sum[4 * k + 2].x, sum[4 * k + 2].y), pack_bf16(sum[4 * k + 3].x, sum[4 * k + 3].y));
-    }
+    if (there)
+        *reinterpret_cast<uint4*>(dst + n) = make_uint4(pack_bf16(sum[0].x, sum[0].y), pack_bf16(sum[1].x, sum[1].y), pack_bf16(sum[2].x, sum[2].y), pack_bf16(sum[3].x, sum[3].y));
 }
 cudaError_t scan_tc_sums(const TcSums& a, uint32_t batch, cudaStream_t st) {
-    return launch(k_clear_scan_tc_sums, dim3(8 * a.segments * (a.seg_chunks / 2), a.G, batch), dim3(256), 0, st, a);
+    return launch(k_clear_scan_tc_sums, dim3(8 * a.segments * (a.seg_chunks / 2), a.G, batch), dim3(512), 0, st, a);
 }
 
 cudaError_t scan_tc_launch(const ScanSet& s, int mode, cudaStream_t st) {
