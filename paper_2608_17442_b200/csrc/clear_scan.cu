@@ -333,8 +333,12 @@ static bool scan_strides(const int64_t (&s)[3], uint64_t b, uint64_t t, uint64_t
     return true;
 }
 static ScanOperand operand(const void* p, const int64_t (&s)[3], bool tiled, uint32_t bytes) {
-    ScanOperand o = {p, s[0], s[1], s[2], tiled, 0};
-    o.wide = ((size_t)p & 15) == 0 && s[0] * bytes % 16 == 0 && s[1] * bytes % 16 == 0 && s[2] * bytes % 16 == 0;
+    ScanOperand o = {p, s[0], s[1], s[2], tiled, bytes};
+    for (uint32_t to = 16; to > bytes; to /= 2)
+        if ((size_t)p % to == 0 && s[0] * bytes % to == 0 && s[1] * bytes % to == 0 && s[2] * bytes % to == 0) {
+            o.align = to;
+            break;
+        }
     return o;
 }
 static uint32_t out_width(const void* p, const int64_t (&s)[3], uint32_t bytes) {
@@ -390,7 +394,7 @@ extern "C" int fesc_clear_scan(const fesc_clear_scan_desc* desc, const void* d_x
     const uint32_t bytes = clear_type_bytes(d.type);
     ScanArgs a = scan_args(desc, s, d_g, d_lengths);
     a.q = operand(d_C, d.C, false, bytes), a.k = operand(d_B, d.B, false, bytes), a.v = operand(d_x, d.x, true, bytes);
-    const bool tc = s.tc && a.q.wide && a.k.wide && a.v.wide && out_width(d_y, d.y, bytes);
+    const bool tc = s.tc && a.q.align == 16 && a.k.align == 16 && a.v.align == 16 && out_width(d_y, d.y, bytes);
     a.init = d_h0;
     if (s.segments > 1) {
         float* states = (float*)d_work;
@@ -444,7 +448,7 @@ extern "C" int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const 
     const uint32_t bytes = clear_type_bytes(d.type);
     const ScanOperand x = operand(d_x, d.x, true, bytes), B = operand(d_B, d.B, false, bytes), C = operand(d_C, d.C, false, bytes),
                       dy = operand(d_dy, d.y, true, bytes);
-    const bool tc = s.tc && x.wide && B.wide && C.wide && dy.wide && out_width(d_dx, d.dx, bytes) && out_width(d_dB, d.dB, bytes) && out_width(d_dC, d.dC, bytes);
+    const bool tc = s.tc && x.align == 16 && B.align == 16 && C.align == 16 && dy.align == 16 && out_width(d_dx, d.dx, bytes) && out_width(d_dB, d.dB, bytes) && out_width(d_dC, d.dC, bytes);
     const ScanArgs base = scan_args(desc, s, d_g, d_lengths);
     const float *h = d_h0, *dh = d_dh_out;
     if (s.segments > 1) {

@@ -32,7 +32,7 @@ struct ScanOperand {
     const void* p;
     long long sb, st, sh;    // strides of batch, token and head (or group), in elements
     uint32_t tiled;          // 1: a head's channels (64 of P from the tile), 0: a group's columns (N)
-    uint32_t wide;           // 16-byte accesses are possible
+    uint32_t align;          // bytes that rows are aligned to: 16, 8, 4 or less
 };
 struct ScanArgs {
     ScanOperand q, k, v, u;          // u (MODE_GRAD): the row that the output's row is multiplied with, for the gradient of the log decays
@@ -94,27 +94,87 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
 }
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// SCAN_Q rows of up to D columns into shared memory, plane by plane; zeros beyond `rows` and `width`.  step: elements from one row to the next.
-template <class T, int D, int THREADS>
-__device__ __forceinline__ void load_tile(__nv_bfloat16* dst, const T* src, long long step, int rows, int width, bool wide) {
-    constexpr int NI = ClearType<T>::planes, STR = D + SCAN_PAD;
-    const uint32_t base = (uint32_t)__cvta_generic_to_shared(dst);
+// a piece of `SIZE` bytes of every row's end to end copy, `bytes` of them from memory and zeros behind
+template <int SIZE>
+__device__ __forceinline__ void cp_async_part(uint32_t dst, const void* src, uint32_t bytes) {
+    if constexpr (SIZE == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(bytes), "n"(SIZE) : "memory");
+}
+template <int SIZE, int D, int THREADS, class T>
+__device__ __forceinline__ void copy_tile(uint32_t base, const T* src, long long step, int rows, int width) {
+    constexpr int E = SIZE / 2;       // numbers in a piece
 #pragma unroll 4
-    for (int i = threadIdx.x; i < SCAN_Q * D / 8; i += THREADS) {
-        const int r = i / (D / 8), c = i % (D / 8) * 8, count = r < rows ? width - c : 0;
-        const T* p = src + r * step + c;
-        if (NI == 1 && wide && count >= 8) {
-            cp_async16(base + (r * STR + c) * 2, p);
-            continue;
+    for (int i = threadIdx.x; i < SCAN_Q * D / E; i += THREADS) {
+        const int r = i / (D / E), c = i % (D / E) * E, bytes = r < rows ? min(max(width - c, 0), E) * 2 : 0;
+        cp_async_part<SIZE>(base + (r * (D + SCAN_PAD) + c) * 2, bytes ? src + r * step + c : src, bytes);
+    }
+}
+
+// SCAN_Q rows of up to D columns into shared memory, plane by plane; zeros beyond `rows` and `width`.  step: elements from one row to the next.
+// align: bytes that rows are aligned to.  bfloat16 rows are copied asynchronously in the largest pieces that allows; what has to be cut into planes
+// passes through registers, several loads at a time.
+template <class T, int D, int THREADS>
+__device__ __forceinline__ void load_tile(__nv_bfloat16* dst, const T* src, long long step, int rows, int width, uint32_t align) {
+    constexpr int NI = ClearType<T>::planes, STR = D + SCAN_PAD, AHEAD = 4;
+    static_assert(SCAN_Q * D / 8 % (THREADS * AHEAD) == 0, "whole turns");
+    if (align < (NI == 1 ? 4 : 16)) {
+        // element by element, neighbouring threads neighbouring columns, 16 loads at a time
+#pragma unroll 1
+        for (int i0 = threadIdx.x; i0 < SCAN_Q * D; i0 += THREADS * 16) {
+            float v[16];
+#pragma unroll
+            for (int k = 0; k < 16; k++) {
+                const int i = i0 + k * THREADS, r = i / D, c = i % D;
+                v[k] = r < rows && c < width ? ClearType<T>::to(src[r * step + c]) : 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < 16; k++) {
+                const int i = i0 + k * THREADS, r = i / D, c = i % D;
+                uint32_t pl[NI];
+                split<NI>(v[k], 0.f, pl);
+#pragma unroll
+                for (int j = 0; j < NI; j++) reinterpret_cast<uint16_t*>(dst)[j * SCAN_Q * STR + r * STR + c] = (uint16_t)pl[j];
+            }
         }
-        float v[8];
-        clear_load8(p, count, wide, v);
-        uint32_t pl[4][NI];
+        return;
+    }
+    if constexpr (NI == 1) {
+        const uint32_t base = (uint32_t)__cvta_generic_to_shared(dst);
+        if (align >= 16) copy_tile<16, D, THREADS>(base, src, step, rows, width);
+        else if (align >= 8) copy_tile<8, D, THREADS>(base, src, step, rows, width);
+        else copy_tile<4, D, THREADS>(base, src, step, rows, width);
+    } else {
+#pragma unroll 1
+        for (int i0 = threadIdx.x; i0 < SCAN_Q * D / 8; i0 += THREADS * AHEAD) {
+            float v[AHEAD][8];
 #pragma unroll
-        for (int e = 0; e < 4; e++) split<NI>(v[2 * e], v[2 * e + 1], pl[e]);
+            for (int k = 0; k < AHEAD; k++) {
+                const int i = i0 + k * THREADS, r = i / (D / 8), c = i % (D / 8) * 8, count = r < rows ? width - c : 0;
+                clear_load8(src + r * step + c, count >= 8 ? 8 : 0, count >= 8, v[k]);
+            }
 #pragma unroll
-        for (int j = 0; j < NI; j++)
-            *reinterpret_cast<uint4*>(dst + j * SCAN_Q * STR + r * STR + c) = make_uint4(pl[0][j], pl[1][j], pl[2][j], pl[3][j]);
+            for (int k = 0; k < AHEAD; k++) {
+                const int i = i0 + k * THREADS, r = i / (D / 8), c = i % (D / 8) * 8;
+                uint32_t pl[4][NI];
+#pragma unroll
+                for (int e = 0; e < 4; e++) split<NI>(v[k][2 * e], v[k][2 * e + 1], pl[e]);
+#pragma unroll
+                for (int j = 0; j < NI; j++)
+                    *reinterpret_cast<uint4*>(dst + j * SCAN_Q * STR + r * STR + c) = make_uint4(pl[0][j], pl[1][j], pl[2][j], pl[3][j]);
+            }
+        }
+        if (width & 7) {         // the columns behind the last eight, over the zeros
+            __syncthreads();
+#pragma unroll 1
+            for (int i = threadIdx.x; i < rows * 8; i += THREADS) {
+                const int r = i >> 3, c = (width & ~7) + (i & 7);
+                if (c >= width) continue;
+                uint32_t pl[NI];
+                split<NI>(ClearType<T>::to(src[r * step + c]), 0.f, pl);
+#pragma unroll
+                for (int j = 0; j < NI; j++) reinterpret_cast<uint16_t*>(dst)[j * SCAN_Q * STR + r * STR + c] = (uint16_t)pl[j];
+            }
+        }
     }
 }
 
@@ -127,7 +187,8 @@ struct ScanShared {
     static constexpr int words = s + (MODE ? NO * SCAN_Q * S_STR : 0);                        // in bfloat16 numbers
     static constexpr int O_STR = DV + 4;                                                       // floats; the outputs' rows lie over v .. s
     static_assert(!MODE || (words - q) * 2 >= SCAN_Q * O_STR * 4, "outputs fit over q and the scores");
-    static constexpr size_t bytes = (size_t)words * 2;
+    static constexpr int H_STR = (MODE == MODE_GRAD ? DV : DK) + 4;                           // floats; states pass through all of it, 64 rows
+    static constexpr size_t bytes = std::max((size_t)words * 2, (size_t)SCAN_TILE * H_STR * 4);
 };
 
 template <class T, int DK, int DV, int MODE>
@@ -183,41 +244,56 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
 
     // this warp's quarter of the state: rows (of v) warp * DV/4 + 16 m + g8 (+ 8), columns (of k) 8 n + 2 q4 (+ 1)
     float st[MT][KT][4];
-    const float* init = MODE && a.init ? a.init + (a.segments > 1 ? slot : b) * states + state_at : nullptr;
-    auto state_index = [&](int m, int n, int e) {   // -1: not part of the state
+    float* sh = reinterpret_cast<float*>(sm);
+    // states go between global memory and the registers by way of shared memory: [channel][column] as in global memory
+    auto state_word = [&](int m, int n, int e) -> float& {
         const int rv = warp * (DV / 4) + 16 * m + g8 + (e & 2 ? 8 : 0), ck = 8 * n + 2 * q4 + (e & 1);
-        const int p = a.v.tiled ? rv : ck, c = a.v.tiled ? ck : rv;
-        return p < pw && c < (int)a.N ? p * (int)a.N + c : -1;
+        return MODE == MODE_GRAD ? sh[ck * S::H_STR + rv] : sh[rv * S::H_STR + ck];
     };
+    auto fetch_state = [&](const float* src) {      // zeros beyond the tile and its columns, and without a source
+        constexpr int NC = MODE == MODE_GRAD ? DV : DK;
+#pragma unroll 4
+        for (int i = tid; i < SCAN_TILE * NC; i += 128) {
+            const int p = i / NC, c = i % NC;
+            sh[p * S::H_STR + c] = src && p < pw && c < (int)a.N ? src[p * (int)a.N + c] : 0.f;
+        }
+    };
+    const float* init = MODE && a.init ? a.init + (a.segments > 1 ? slot : b) * states + state_at : nullptr;
+    if (init) fetch_state(init);
+    __syncthreads();
 #pragma unroll
     for (int m = 0; m < MT; m++)
 #pragma unroll
         for (int n = 0; n < KT; n++)
 #pragma unroll
-            for (int e = 0; e < 4; e++) {
-                const int at = init ? state_index(m, n, e) : -1;
-                st[m][n][e] = at >= 0 ? init[at] : 0.f;
-            }
+            for (int e = 0; e < 4; e++) st[m][n][e] = init ? state_word(m, n, e) : 0.f;
+    __syncthreads();
 
     const int chunks = t_hi > t_lo ? (t_hi - t_lo + SCAN_Q - 1) / SCAN_Q : 0;
     float diag = 0.f;
     double through = 0.0;                        // log2 of the decay over the segment (thread 0)
+    // warp 0: log decays of two positions a lane, read a chunk ahead.  The decay that applies on the way to a position is its own token's forwards, the
+    // token's behind it backwards (none at the end).
+    float gv[2] = {};
+    auto read_decays = [&](int c) {
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const int pos = c * SCAN_Q + 2 * lane + i, t = a.backwards ? t_hi - pos : t_lo + pos;
+            gv[i] = t_lo + pos < t_hi && t < length ? a.g[b * a.gb + t * a.gt + head * a.gh] : 0.f;
+        }
+    };
+    if (warp == 0 && chunks) read_decays(0);
     for (int c = 0; c < chunks; c++) {
         // token of position i of the chunk: t0 + dir * i
         const int valid = min(SCAN_Q, t_hi - t_lo - c * SCAN_Q), dir = a.backwards ? -1 : 1, t0 = a.backwards ? t_hi - 1 - c * SCAN_Q : t_lo + c * SCAN_Q;
-        load_tile<T, DK, 128>(sk, scan_row<T>(a.k, b, t0, head, group, tile), dir * a.k.st, valid, kw, a.k.wide);
-        load_tile<T, DV, 128>(sv, scan_row<T>(a.v, b, t0, head, group, tile), dir * a.v.st, valid, vw, a.v.wide);
-        if (MODE) load_tile<T, DK, 128>(sq, scan_row<T>(a.q, b, t0, head, group, tile), dir * a.q.st, valid, kw, a.q.wide);
+        load_tile<T, DK, 128>(sk, scan_row<T>(a.k, b, t0, head, group, tile), dir * a.k.st, valid, kw, a.k.align);
+        load_tile<T, DV, 128>(sv, scan_row<T>(a.v, b, t0, head, group, tile), dir * a.v.st, valid, vw, a.v.align);
+        if (MODE) load_tile<T, DK, 128>(sq, scan_row<T>(a.q, b, t0, head, group, tile), dir * a.q.st, valid, kw, a.q.align);
         if (warp == 0) {
-            // the decay that applies on the way to a position is its own token's forwards, the token's behind it backwards (none at the end)
             double sum[2];
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
-                const int pos = 2 * lane + i, t = t0 + dir * pos + (a.backwards ? 1 : 0);
-                float gv = pos < valid && t < length ? a.g[b * a.gb + t * a.gt + head * a.gh] : 0.f;
-                gv = gv < SCAN_DROP ? SCAN_DROP : gv;
-                sum[i] = (double)gv * 1.4426950408889634 + (i ? sum[0] : 0.0);
-            }
+            for (int i = 0; i < 2; i++) sum[i] = (double)(gv[i] < SCAN_DROP ? SCAN_DROP : gv[i]) * 1.4426950408889634 + (i ? sum[0] : 0.0);
+            if (c + 1 < chunks) read_decays(c + 1);
             double run = sum[1];
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -241,26 +317,25 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
 
         if (MODE) {
             // scores of 16 rows i per warp, columns j <= i: S_ij = G_ij (q_i . k_j), cut into planes
-            uint32_t qf[NI][DK / 16][4];
-#pragma unroll
-            for (int p = 0; p < NI; p++)
-#pragma unroll
-                for (int kk = 0; kk < DK / 16; kk++)
-                    ldsm4(qf[p][kk], aq + (p * SCAN_Q * S::K_STR + (16 * warp + row_l) * S::K_STR + 16 * kk + col_l) * 2);
-            const int i0 = 16 * warp + g8;
+            const int i0 = 16 * warp + g8, ks = (kw + 15) / 16;
             const float2 ci[2] = {cum[i0], cum[i0 + 8]};
+#pragma unroll 1
             for (int j = 0; j <= (int)warp; j++) {
                 float d[2][4] = {};
+#pragma unroll 2
+                for (int kk = 0; kk < ks; kk++) {
+                    uint32_t qf[NI][4], kf[NI][4];
 #pragma unroll
-                for (int kk = 0; kk < DK / 16; kk++)
+                    for (int p = 0; p < NI; p++) {
+                        ldsm4(qf[p], aq + (p * SCAN_Q * S::K_STR + (16 * warp + row_l) * S::K_STR + 16 * kk + col_l) * 2);
+                        ldsm4(kf[p], ak + (p * SCAN_Q * S::K_STR + (16 * j + row_r) * S::K_STR + 16 * kk + col_r) * 2);
+                    }
 #pragma unroll
-                    for (int pk = 0; pk < NI; pk++) {
-                        uint32_t kf[4];
-                        ldsm4(kf, ak + (pk * SCAN_Q * S::K_STR + (16 * j + row_r) * S::K_STR + 16 * kk + col_r) * 2);
+                    for (int pk = 0; pk < NI; pk++)
 #pragma unroll
                         for (int pq = 0; pq < NI; pq++)
-                            if (pk + pq < 3) mma(d[0], qf[pq][kk], kf[0], kf[1]), mma(d[1], qf[pq][kk], kf[2], kf[3]);
-                    }
+                            if (pk + pq < 3) mma(d[0], qf[pq], kf[pk][0], kf[pk][1]), mma(d[1], qf[pq], kf[pk][2], kf[pk][3]);
+                }
 #pragma unroll
                 for (int n = 0; n < 2; n++) {
                     const int jc = 16 * j + 8 * n + 2 * q4;
@@ -291,6 +366,7 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
                     for (int e = 0; e < 4; e++) acc[m][n][e] = 0.f;
 #pragma unroll
             for (int kk = 0; kk < DK / 16; kk++) {
+                if (16 * kk >= kw) break;         // columns that do not exist
                 uint32_t sf[MT][NO][4];
 #pragma unroll
                 for (int m = 0; m < MT; m++)
@@ -332,7 +408,7 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
 #pragma unroll
                     for (int e = 0; e < 4; e++) st[m][n][e] *= keep;
         }
-#pragma unroll
+#pragma unroll 1
         for (int kk = 0; kk < SCAN_Q / 16; kk++) {
             uint32_t vf[MT][NI][4], wf[MT][NS][4];
 #pragma unroll
@@ -370,7 +446,8 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
                 }
             }
 #pragma unroll
-            for (int n = 0; n < DK / 16; n++)
+            for (int n = 0; n < DK / 16; n++) {
+                if (16 * n >= kw) break;
 #pragma unroll
                 for (int pk = 0; pk < NI; pk++) {
                     uint32_t kf[4];
@@ -381,6 +458,7 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
 #pragma unroll
                             for (int m = 0; m < MT; m++) mma(st[m][2 * n], wf[m][p], kf[0], kf[1]), mma(st[m][2 * n + 1], wf[m][p], kf[2], kf[3]);
                 }
+            }
         }
 
         if (MODE) {
@@ -398,7 +476,7 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
             if (MODE == MODE_OUT) {
                 T* out = (T*)a.out + b * a.ob + head * a.oh + tile * SCAN_TILE;
                 const float skip = a.skip ? a.skip[head] : 0.f;
-#pragma unroll
+#pragma unroll 2
                 for (int i = tid; i < SCAN_Q * DV / 8; i += 128) {
                     const int r = i / (DV / 8), cc = i % (DV / 8) * 8;
                     float v[8];
@@ -436,7 +514,7 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
         __syncthreads();
     }
 
-    // the state behind the sweep
+    // the state behind the sweep (shared memory is free: every chunk ends with a barrier)
     if (a.last && (MODE == MODE_STATE || is_last)) {
         float* last = a.last + (MODE == MODE_STATE ? slot : b) * states + state_at;
         // backwards the state belongs to the first token: the gradient of the state before it is one decay further
@@ -446,26 +524,25 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
 #pragma unroll
             for (int n = 0; n < KT; n++)
 #pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const int at = state_index(m, n, e);
-                    if (at >= 0) last[at] = st[m][n][e] * f;
-                }
+                for (int e = 0; e < 4; e++) state_word(m, n, e) = st[m][n][e] * f;
+        __syncthreads();
+#pragma unroll 4
+        for (int i = tid; i < pw * (int)a.N; i += 128) last[i] = sh[i / a.N * S::H_STR + i % a.N];
+        __syncthreads();
     }
-    if (MODE == MODE_STATE && tid == 0 && tile == 0) a.decay[slot * a.H + head] = (float)exp2(through);
+    if (MODE == MODE_STATE && tid == 0 && tile == 0) a.decay[slot * a.H + head] = exp2f((float)through) * exp2f((float)(through - (float)through));
     if (MODE == MODE_GRAD && a.ends) {
         // <state, gradient of the state> at the segment's end, one decay on from what the sweep backwards starts this segment with
         float sum = 0.f;
-        const float* meet = a.meet ? a.meet + (a.segments > 1 ? slot : b) * states + state_at : nullptr;
-        if (meet) {
+        if (a.meet) {
+            fetch_state(a.meet + (a.segments > 1 ? slot : b) * states + state_at);
+            __syncthreads();
 #pragma unroll
             for (int m = 0; m < MT; m++)
 #pragma unroll
                 for (int n = 0; n < KT; n++)
 #pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        const int at = state_index(m, n, e);
-                        if (at >= 0) sum += st[m][n][e] * meet[at];
-                    }
+                    for (int e = 0; e < 4; e++) sum += st[m][n][e] * state_word(m, n, e);
             if (t_hi < length) sum *= expf(a.g[b * a.gb + t_hi * a.gt + head * a.gh]);
         }
 #pragma unroll
