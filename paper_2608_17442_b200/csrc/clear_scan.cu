@@ -272,8 +272,8 @@ static ScanShape scan_shape(const fesc_clear_scan_desc* d, bool backward) {
     s.tiles = (d->P + SCAN_TILE - 1) / SCAN_TILE, s.vheads = d->H * s.tiles, s.np = d->N > 64 ? 128 : 64;
     const uint64_t pieces = ((uint64_t)d->L + 127) / 128, ctas = (uint64_t)d->batch * s.vheads, sweeps = backward ? 3 : 1;
     const double START = s.tc ? 2.0 : 0.5, CHAIN = s.tc ? 1.5 : 0.5, STATE = s.tc ? 0.35 : 0.5;
-    // CTAs of a sweep on an SM, by shared memory
-    const uint64_t places = 148 * (s.tc ? 1 : d->type == FESC_BF16 ? 3 : d->type == FESC_F16 ? (d->N > 64 ? 2 : 3) : (d->N > 64 ? 1 : 2));
+    // CTAs of a sweep on an SM, by registers and shared memory
+    const uint64_t places = 148 * (s.tc ? 1 : d->type == FESC_BF16 ? (d->N > 64 ? 2 : 3) : d->type == FESC_F32 && d->N > 64 ? 1 : 2);
     uint64_t each = pieces ? pieces : 1, last = 0;
     double least = 1e300;
     for (uint64_t want = 1; want <= pieces && want <= 1024; want++) {

@@ -5,7 +5,7 @@
 // (x, dy, C) and dC the sweep forwards with (dy, x, B).  Heads of more than 64 channels are cut into tiles of 64, which act as heads of their own.
 //
 // Tokens go in chunks of 64.  Within a chunk the sum is two matrix products with the decays between them (64 x 64 scores); the state carries
-// everything before it.  The state of a head tile (64 channels x up to 128) stays in registers, a quarter per warp, in the accumulator layout of
+// everything before it.  The state of a head tile (64 channels x up to 128) stays in the warps' registers in the accumulator layout of
 // mma.m16n8k16, which is also the layout of a left operand: the products are formed transposed (out^T = state q^T + v^T S^T) so that the state
 // multiplies q without going through memory.
 // A long sequence is cut into segments when there are too few heads to fill the SMs: k_clear_scan in MODE_STATE gives what every
@@ -115,8 +115,7 @@ __device__ __forceinline__ void copy_tile(uint32_t base, const T* src, long long
 // passes through registers, several loads at a time.
 template <class T, int D, int THREADS>
 __device__ __forceinline__ void load_tile(__nv_bfloat16* dst, const T* src, long long step, int rows, int width, uint32_t align) {
-    constexpr int NI = ClearType<T>::planes, STR = D + SCAN_PAD, AHEAD = 4;
-    static_assert(SCAN_Q * D / 8 % (THREADS * AHEAD) == 0, "whole turns");
+    constexpr int NI = ClearType<T>::planes, STR = D + SCAN_PAD, AHEAD = SCAN_Q * D / 8 / THREADS;      // all of a thread's pieces at once
     if (align < (NI == 1 ? 4 : 16)) {
         // element by element, neighbouring threads neighbouring columns, 16 loads at a time
 #pragma unroll 1
@@ -178,6 +177,13 @@ __device__ __forceinline__ void load_tile(__nv_bfloat16* dst, const T* src, long
     }
 }
 
+// A CTA has four warps for four slices of v's columns, and as many again where two share a slice, one for each half of k's columns: with operands of
+// several planes one CTA or two fill an SM's shared memory, and four warps each wait for their own products (8 x 1024 tokens of 12 heads in
+// float32 284 us against 210).  With one plane three CTAs fit, and what two warps of a slice both have to do costs more (66 against 89).
+template <class T>
+struct ScanWarps {
+    static constexpr int halves = ClearType<T>::planes == 1 ? 1 : 2, threads = 128 * halves;
+};
 template <class T, int DK, int DV, int MODE>
 struct ScanShared {
     static constexpr int NI = ClearType<T>::planes;
@@ -194,12 +200,13 @@ struct ScanShared {
 template <class T, int DK, int DV, int MODE>
 __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
     using S = ScanShared<T, DK, DV, MODE>;
-    constexpr int NI = S::NI, NO = S::NO, NS = 3, MT = DV / 64, KT = DK / 8;
+    constexpr int NI = S::NI, NO = S::NO, NS = 3, MT = DV / 64, HALVES = ScanWarps<T>::halves, THREADS = ScanWarps<T>::threads, KH = DK / HALVES, KT = KH / 8;
     extern __shared__ __align__(128) __nv_bfloat16 sm[];
     __shared__ __align__(16) float2 cum[SCAN_Q];               // log2 of the decay up to a token of the chunk, as a sum of two floats
     __shared__ __align__(16) float grow[SCAN_Q], fade[SCAN_Q]; // decay from the chunk's start to a token; from a token to the chunk's end
-    __shared__ float words[4];
-    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, q4 = lane & 3;
+    __shared__ float words[2][THREADS / 32];
+    // a warp's slice of the columns of v, and its half of those of k (or all of them); the halves of a slice's outputs are added up at the end
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, slice = warp & 3, half = HALVES == 1 ? 0 : warp >> 2, lane = tid & 31, g8 = lane >> 2, q4 = lane & 3;
     // heads vary fastest: neighbours in the grid share the rows of their group
     const uint32_t vheads = a.H * a.tiles, vh = block % vheads, seg = block / vheads % a.segments, b = block / vheads / a.segments;
     const uint32_t head = vh / a.tiles, tile = vh % a.tiles, group = head / (a.H / a.G);
@@ -242,18 +249,18 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
     const int row_l = lane & 15, col_l = lane >> 4 << 3, row_r = (lane & 7) | (lane >> 4 << 3), col_r = lane & 8;
     const int row_t = (lane & 7) | (lane >> 4 << 3), col_t = lane & 8;   // transposed left operands
 
-    // this warp's quarter of the state: rows (of v) warp * DV/4 + 16 m + g8 (+ 8), columns (of k) 8 n + 2 q4 (+ 1)
+    // this warp's part of the state: rows (of v) slice * DV/4 + 16 m + g8 (+ 8), columns (of k) half * KH + 8 n + 2 q4 (+ 1)
     float st[MT][KT][4];
     float* sh = reinterpret_cast<float*>(sm);
     // states go between global memory and the registers by way of shared memory: [channel][column] as in global memory
     auto state_word = [&](int m, int n, int e) -> float& {
-        const int rv = warp * (DV / 4) + 16 * m + g8 + (e & 2 ? 8 : 0), ck = 8 * n + 2 * q4 + (e & 1);
+        const int rv = slice * (DV / 4) + 16 * m + g8 + (e & 2 ? 8 : 0), ck = half * KH + 8 * n + 2 * q4 + (e & 1);
         return MODE == MODE_GRAD ? sh[ck * S::H_STR + rv] : sh[rv * S::H_STR + ck];
     };
     auto fetch_state = [&](const float* src) {      // zeros beyond the tile and its columns, and without a source
         constexpr int NC = MODE == MODE_GRAD ? DV : DK;
 #pragma unroll 4
-        for (int i = tid; i < SCAN_TILE * NC; i += 128) {
+        for (int i = tid; i < SCAN_TILE * NC; i += THREADS) {
             const int p = i / NC, c = i % NC;
             sh[p * S::H_STR + c] = src && p < pw && c < (int)a.N ? src[p * (int)a.N + c] : 0.f;
         }
@@ -286,9 +293,9 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
     for (int c = 0; c < chunks; c++) {
         // token of position i of the chunk: t0 + dir * i
         const int valid = min(SCAN_Q, t_hi - t_lo - c * SCAN_Q), dir = a.backwards ? -1 : 1, t0 = a.backwards ? t_hi - 1 - c * SCAN_Q : t_lo + c * SCAN_Q;
-        load_tile<T, DK, 128>(sk, scan_row<T>(a.k, b, t0, head, group, tile), dir * a.k.st, valid, kw, a.k.align);
-        load_tile<T, DV, 128>(sv, scan_row<T>(a.v, b, t0, head, group, tile), dir * a.v.st, valid, vw, a.v.align);
-        if (MODE) load_tile<T, DK, 128>(sq, scan_row<T>(a.q, b, t0, head, group, tile), dir * a.q.st, valid, kw, a.q.align);
+        load_tile<T, DK, THREADS>(sk, scan_row<T>(a.k, b, t0, head, group, tile), dir * a.k.st, valid, kw, a.k.align);
+        load_tile<T, DV, THREADS>(sv, scan_row<T>(a.v, b, t0, head, group, tile), dir * a.v.st, valid, vw, a.v.align);
+        if (MODE) load_tile<T, DK, THREADS>(sq, scan_row<T>(a.q, b, t0, head, group, tile), dir * a.q.st, valid, kw, a.q.align);
         if (warp == 0) {
             double sum[2];
 #pragma unroll
@@ -317,25 +324,36 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
 
         if (MODE) {
             // scores of 16 rows i per warp, columns j <= i: S_ij = G_ij (q_i . k_j), cut into planes
-            const int i0 = 16 * warp + g8, ks = (kw + 15) / 16;
+            const int i0 = 16 * slice + g8, ks = (kw + 15) / 16;
             const float2 ci[2] = {cum[i0], cum[i0 + 8]};
 #pragma unroll 1
-            for (int j = 0; j <= (int)warp; j++) {
-                float d[2][4] = {};
+            for (int j = half; j <= (int)slice; j += HALVES) {
+                // products that depend on one another wait: each plane of k has sums of its own, with one plane every other step
+                float ds[NI == 1 ? 2 : NI][2][4] = {};
 #pragma unroll 2
                 for (int kk = 0; kk < ks; kk++) {
                     uint32_t qf[NI][4], kf[NI][4];
 #pragma unroll
                     for (int p = 0; p < NI; p++) {
-                        ldsm4(qf[p], aq + (p * SCAN_Q * S::K_STR + (16 * warp + row_l) * S::K_STR + 16 * kk + col_l) * 2);
+                        ldsm4(qf[p], aq + (p * SCAN_Q * S::K_STR + (16 * slice + row_l) * S::K_STR + 16 * kk + col_l) * 2);
                         ldsm4(kf[p], ak + (p * SCAN_Q * S::K_STR + (16 * j + row_r) * S::K_STR + 16 * kk + col_r) * 2);
                     }
-#pragma unroll
-                    for (int pk = 0; pk < NI; pk++)
+                    if constexpr (NI == 1) {
+                        if (kk & 1) mma(ds[1][0], qf[0], kf[0][0], kf[0][1]), mma(ds[1][1], qf[0], kf[0][2], kf[0][3]);
+                        else mma(ds[0][0], qf[0], kf[0][0], kf[0][1]), mma(ds[0][1], qf[0], kf[0][2], kf[0][3]);
+                    } else {
 #pragma unroll
                         for (int pq = 0; pq < NI; pq++)
-                            if (pk + pq < 3) mma(d[0], qf[pq], kf[pk][0], kf[pk][1]), mma(d[1], qf[pq], kf[pk][2], kf[pk][3]);
+#pragma unroll
+                            for (int pk = 0; pk < NI; pk++)
+                                if (pk + pq < 3) mma(ds[pk][0], qf[pq], kf[pk][0], kf[pk][1]), mma(ds[pk][1], qf[pq], kf[pk][2], kf[pk][3]);
+                    }
                 }
+                float d[2][4];
+#pragma unroll
+                for (int n = 0; n < 2; n++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) d[n][e] = NI == 3 ? ds[0][n][e] + (ds[1][n][e] + ds[NI == 3 ? 2 : 1][n][e]) : ds[0][n][e] + ds[1][n][e];
 #pragma unroll
                 for (int n = 0; n < 2; n++) {
                     const int jc = 16 * j + 8 * n + 2 * q4;
@@ -365,8 +383,8 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
 #pragma unroll
                     for (int e = 0; e < 4; e++) acc[m][n][e] = 0.f;
 #pragma unroll
-            for (int kk = 0; kk < DK / 16; kk++) {
-                if (16 * kk >= kw) break;         // columns that do not exist
+            for (int kk = 0; kk < KH / 16; kk++) {
+                if ((int)half * KH + 16 * kk >= kw) break;         // columns that do not exist
                 uint32_t sf[MT][NO][4];
 #pragma unroll
                 for (int m = 0; m < MT; m++)
@@ -379,17 +397,19 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
                         for (int p = 0; p < NO; p++) sf[m][p][r] = pl[p];
                     }
 #pragma unroll
-                for (int n = 0; n < 4; n++)
+                for (int pq = 0; pq < NI; pq++) {
+                    uint32_t qf[4][4];
 #pragma unroll
-                    for (int pq = 0; pq < NI; pq++) {
-                        uint32_t qf[4];
-                        ldsm4(qf, aq + (pq * SCAN_Q * S::K_STR + (16 * n + row_r) * S::K_STR + 16 * kk + col_r) * 2);
+                    for (int n = 0; n < 4; n++)
+                        ldsm4(qf[n], aq + (pq * SCAN_Q * S::K_STR + (16 * n + row_r) * S::K_STR + half * KH + 16 * kk + col_r) * 2);
 #pragma unroll
-                        for (int p = 0; p < NO; p++)
-                            if (p + pq < NO || NI == 1)
+                    for (int p = 0; p < NO; p++)
+                        if (p + pq < NO || NI == 1)
 #pragma unroll
-                                for (int m = 0; m < MT; m++) mma(acc[m][2 * n], sf[m][p], qf[0], qf[1]), mma(acc[m][2 * n + 1], sf[m][p], qf[2], qf[3]);
-                    }
+                            for (int n = 0; n < 4; n++)
+#pragma unroll
+                                for (int m = 0; m < MT; m++) mma(acc[m][2 * n], sf[m][p], qf[n][0], qf[n][1]), mma(acc[m][2 * n + 1], sf[m][p], qf[n][2], qf[n][3]);
+                }
             }
 #pragma unroll
             for (int n = 0; n < 8; n++) {
@@ -415,7 +435,7 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
             for (int m = 0; m < MT; m++) {
 #pragma unroll
                 for (int p = 0; p < NI; p++)
-                    ldsm4t(vf[m][p], av + (p * SCAN_Q * S::V_STR + (16 * kk + row_t) * S::V_STR + warp * (DV / 4) + 16 * m + col_t) * 2);
+                    ldsm4t(vf[m][p], av + (p * SCAN_Q * S::V_STR + (16 * kk + row_t) * S::V_STR + slice * (DV / 4) + 16 * m + col_t) * 2);
                 // rows of the block are positions 16 kk + 2 q4 (+ 1), + 8 for the right half
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
@@ -429,35 +449,37 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
                     for (int p = 0; p < NS; p++) wf[m][p][r] = pl[p];
                 }
             }
-            if (MODE) {
+            if (MODE && (HALVES == 1 || (kk & 1) == (int)half)) {
 #pragma unroll
-                for (int n = 0; n < 4; n++) {
-                    if (n < kk) continue;             // positions i before all of these j
+                for (int p = 0; p < NO; p++) {
+                    uint32_t sf[4][4];
 #pragma unroll
-                    for (int p = 0; p < NO; p++) {
-                        uint32_t sf[4];
-                        ldsm4(sf, as + (p * SCAN_Q * S::S_STR + (16 * n + row_r) * S::S_STR + 16 * kk + col_r) * 2);
+                    for (int n = 0; n < 4; n++)
+                        if (n >= kk) ldsm4(sf[n], as + (p * SCAN_Q * S::S_STR + (16 * n + row_r) * S::S_STR + 16 * kk + col_r) * 2);      // positions i before all of these j have none
 #pragma unroll
-                        for (int pv = 0; pv < NI; pv++)
-                            if (p + pv < NO || NI == 1)
+                    for (int pv = 0; pv < NI; pv++)
+                        if (p + pv < NO || NI == 1)
 #pragma unroll
-                                for (int m = 0; m < MT; m++) mma(acc[m][2 * n], vf[m][pv], sf[0], sf[1]), mma(acc[m][2 * n + 1], vf[m][pv], sf[2], sf[3]);
-                    }
+                            for (int n = 0; n < 4; n++)
+                                if (n >= kk)
+#pragma unroll
+                                    for (int m = 0; m < MT; m++) mma(acc[m][2 * n], vf[m][pv], sf[n][0], sf[n][1]), mma(acc[m][2 * n + 1], vf[m][pv], sf[n][2], sf[n][3]);
                 }
             }
 #pragma unroll
-            for (int n = 0; n < DK / 16; n++) {
-                if (16 * n >= kw) break;
+            for (int pk = 0; pk < NI; pk++) {
+                uint32_t kf[KH / 16][4];
 #pragma unroll
-                for (int pk = 0; pk < NI; pk++) {
-                    uint32_t kf[4];
-                    ldsm4t(kf, ak + (pk * SCAN_Q * S::K_STR + (16 * kk + row_l) * S::K_STR + 16 * n + col_l) * 2);
+                for (int n = 0; n < KH / 16; n++)
+                    ldsm4t(kf[n], ak + (pk * SCAN_Q * S::K_STR + (16 * kk + row_l) * S::K_STR + half * KH + 16 * n + col_l) * 2);
 #pragma unroll
-                    for (int p = 0; p < NS; p++)
-                        if (p + pk < NS)
+                for (int p = 0; p < NS; p++)
+                    if (p + pk < NS)
 #pragma unroll
-                            for (int m = 0; m < MT; m++) mma(st[m][2 * n], wf[m][p], kf[0], kf[1]), mma(st[m][2 * n + 1], wf[m][p], kf[2], kf[3]);
-                }
+                        for (int n = 0; n < KH / 16; n++)
+                            if ((int)half * KH + 16 * n < kw)
+#pragma unroll
+                                for (int m = 0; m < MT; m++) mma(st[m][2 * n], wf[m][p], kf[n][0], kf[n][1]), mma(st[m][2 * n + 1], wf[m][p], kf[n][2], kf[n][3]);
             }
         }
 
@@ -466,18 +488,24 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
             __syncthreads();
             float* so = reinterpret_cast<float*>(sq);
 #pragma unroll
-            for (int m = 0; m < MT; m++)
+            for (int h = 0; h < HALVES; h++) {
+                if ((int)half == h)
 #pragma unroll
-                for (int n = 0; n < 8; n++)
+                    for (int m = 0; m < MT; m++)
 #pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        so[(8 * n + 2 * q4 + (e & 1)) * S::O_STR + warp * (DV / 4) + 16 * m + g8 + (e & 2 ? 8 : 0)] = acc[m][n][e];
-            __syncthreads();
+                        for (int n = 0; n < 8; n++)
+#pragma unroll
+                            for (int e = 0; e < 4; e++) {
+                                float& o = so[(8 * n + 2 * q4 + (e & 1)) * S::O_STR + slice * (DV / 4) + 16 * m + g8 + (e & 2 ? 8 : 0)];
+                                o = h ? o + acc[m][n][e] : acc[m][n][e];
+                            }
+                __syncthreads();
+            }
             if (MODE == MODE_OUT) {
                 T* out = (T*)a.out + b * a.ob + head * a.oh + tile * SCAN_TILE;
                 const float skip = a.skip ? a.skip[head] : 0.f;
 #pragma unroll 2
-                for (int i = tid; i < SCAN_Q * DV / 8; i += 128) {
+                for (int i = tid; i < SCAN_Q * DV / 8; i += THREADS) {
                     const int r = i / (DV / 8), cc = i % (DV / 8) * 8;
                     float v[8];
 #pragma unroll
@@ -494,7 +522,7 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
                 constexpr int E = DV / 32;
                 float* part = a.part + ((size_t)b * vheads + vh) * a.L * DV;
                 float* dots = a.dots + ((size_t)b * vheads + vh) * a.L;
-                for (int r = warp; r < valid; r += 4) {
+                for (int r = warp; r < valid; r += THREADS / 32) {
                     const int t = t0 + dir * r;
                     const T* u = scan_row<T>(a.u, b, t, head, group, tile) + lane * E;
                     float v[E], dot = 0.f;
@@ -527,7 +555,7 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
                 for (int e = 0; e < 4; e++) state_word(m, n, e) = st[m][n][e] * f;
         __syncthreads();
 #pragma unroll 4
-        for (int i = tid; i < pw * (int)a.N; i += 128) last[i] = sh[i / a.N * S::H_STR + i % a.N];
+        for (int i = tid; i < pw * (int)a.N; i += THREADS) last[i] = sh[i / a.N * S::H_STR + i % a.N];
         __syncthreads();
     }
     if (MODE == MODE_STATE && tid == 0 && tile == 0) a.decay[slot * a.H + head] = exp2f((float)through) * exp2f((float)(through - (float)through));
@@ -547,29 +575,30 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o), diag += __shfl_xor_sync(~0u, diag, o);
-        __shared__ float dw[4];
-        if (lane == 0) words[warp] = sum, dw[warp] = diag;
+        if (lane == 0) words[0][warp] = sum, words[1][warp] = diag;
         __syncthreads();
         if (tid == 0) {
-            a.ends[slot * vheads + vh] = (words[0] + words[1]) + (words[2] + words[3]);
-            a.diag[slot * vheads + vh] = (dw[0] + dw[1]) + (dw[2] + dw[3]);
+            float s0 = 0.f, s1 = 0.f;
+            for (int w = 0; w < THREADS / 32; w++) s0 += words[0][w], s1 += words[1][w];
+            a.ends[slot * vheads + vh] = s0, a.diag[slot * vheads + vh] = s1;
         }
     }
 }
 
 // one grid for the sweeps of a call: those of the backward pass are independent
+#define SCAN_CTAS(T, NP) (ClearType<T>::planes == 1 ? (NP == 64 ? 3 : 2) : ClearType<T>::planes == 3 && NP == 128 ? 1 : 2)      // of an SM
 template <class T, int NP>
-__global__ void __launch_bounds__(128) k_clear_scan_state(const __grid_constant__ ScanSet s) {
+__global__ void __launch_bounds__(ScanWarps<T>::threads, SCAN_CTAS(T, NP)) k_clear_scan_state(const __grid_constant__ ScanSet s) {
     pdl_begin();
     sweep<T, NP, 64, MODE_STATE>(s.a[blockIdx.x % s.count], blockIdx.x / s.count);
 }
 template <class T, int NP>
-__global__ void __launch_bounds__(128) k_clear_scan(const __grid_constant__ ScanSet s) {
+__global__ void __launch_bounds__(ScanWarps<T>::threads, SCAN_CTAS(T, NP)) k_clear_scan(const __grid_constant__ ScanSet s) {
     pdl_begin();
     sweep<T, NP, 64, MODE_OUT>(s.a[0], blockIdx.x);
 }
 template <class T, int NP>
-__global__ void __launch_bounds__(128) k_clear_scan_backward(const __grid_constant__ ScanSet s) {
+__global__ void __launch_bounds__(ScanWarps<T>::threads, SCAN_CTAS(T, NP)) k_clear_scan_backward(const __grid_constant__ ScanSet s) {
     pdl_begin();
     const uint32_t which = blockIdx.x % 3, block = blockIdx.x / 3;
     if (which < 2) sweep<T, 64, NP, MODE_GRAD>(s.a[which], block);
@@ -582,7 +611,7 @@ cudaError_t scan_launch(const ScanSet& s, int mode, cudaStream_t st) {
     auto go = [&](auto kernel, size_t smem) {
         cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         const ScanArgs& a = s.a[0];
-        return e != cudaSuccess ? e : launch(kernel, dim3(s.count * a.b * a.segments * a.H * a.tiles), dim3(128), smem, st, s);
+        return e != cudaSuccess ? e : launch(kernel, dim3(s.count * a.b * a.segments * a.H * a.tiles), dim3(ScanWarps<T>::threads), smem, st, s);
     };
     auto pick = [&](auto np) {
         constexpr int NP = decltype(np)::value;
