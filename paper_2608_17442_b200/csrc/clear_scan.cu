@@ -268,8 +268,8 @@ struct ScanShape {
 // segments, 30 us, with one 65; backwards 2, 95 us, with 6 128.)
 static ScanShape scan_shape(const fesc_clear_scan_desc* d, bool backward) {
     ScanShape s;
-    s.tc = d->type == FESC_BF16 && d->N > 64 && d->N % 8 == 0 && d->P % 8 == 0;
-    s.tiles = (d->P + SCAN_TILE - 1) / SCAN_TILE, s.vheads = d->H * s.tiles, s.np = d->N > 64 ? 128 : 64;
+    s.tc = d->type == FESC_BF16 && d->N % 8 == 0 && d->P % 8 == 0;
+    s.tiles = (d->P + SCAN_TILE - 1) / SCAN_TILE, s.vheads = d->H * s.tiles, s.np = s.tc || d->N > 64 ? 128 : 64;
     const uint64_t pieces = ((uint64_t)d->L + 127) / 128, ctas = (uint64_t)d->batch * s.vheads, sweeps = backward ? 3 : 1;
     const double START = s.tc ? 2.0 : 0.5, CHAIN = s.tc ? 1.5 : 0.5, STATE = s.tc ? 0.35 : 0.5;
     // CTAs of a sweep on an SM, by registers and shared memory
@@ -472,13 +472,13 @@ extern "C" int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const 
     f.dB = d_dB, f.dC = d_dC, f.dg = d_dg, f.dskip = d_dskip, f.lengths = d_lengths, f.g = d_g, f.ib = d.g[0], f.it = d.g[1], f.ih = d.g[2];
     f.Bb = d.dB[0], f.Bt = d.dB[1], f.Bg = d.dB[2], f.Cb = d.dC[0], f.Ct = d.dC[1], f.Cg = d.dC[2], f.gb = d.dg[0], f.gt = d.dg[1], f.gh = d.dg[2];
     f.b = d.batch, f.L = d.L, f.H = d.H, f.G = d.G, f.N = d.N, f.tiles = s.tiles, f.segments = s.segments, f.seg_chunks = s.seg_chunks;
-    f.log_quads = s.np == 128 ? 5 : 4, f.dg_blocks = d.batch * d.H * s.segments;
+    f.log_quads = d.N > 64 ? 5 : 4, f.dg_blocks = d.batch * d.H * s.segments;
     if (tc) {        // sums of their own; the decays after them
         TcSums t = {part_b, part_c, B, C, (__nv_bfloat16*)d_dB, (__nv_bfloat16*)d_dC, row, col, d_lengths, f.Bb, f.Bt, f.Bg, f.Cb, f.Ct, f.Cg,
                     d.L, d.H, d.G, d.N, s.tiles, s.segments, s.seg_chunks};
         CLEAR_CUDA(scan_tc_sums(t, d.batch, st));
     } else {
-        f.sum_each = (uint32_t)(((size_t)d.L * (s.np / 4) + 255) / 256), f.sum_blocks = 2 * d.batch * d.G * f.sum_each;
+        f.sum_each = (uint32_t)((((size_t)d.L << f.log_quads) + 255) / 256), f.sum_blocks = 2 * d.batch * d.G * f.sum_each;
     }
     auto finish = [&](auto kernel, uint32_t threads) {
         return launch(kernel, dim3(f.sum_blocks + f.dg_blocks + (d.H + threads / 32 - 1) / (threads / 32)), dim3(threads), 0, st, f);

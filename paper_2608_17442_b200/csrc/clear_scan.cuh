@@ -598,7 +598,7 @@ __global__ void __launch_bounds__(ScanWarps<T>::threads, SCAN_CTAS(T, NP)) k_cle
     sweep<T, NP, 64, MODE_OUT>(s.a[0], blockIdx.x);
 }
 template <class T, int NP>
-__global__ void __launch_bounds__(ScanWarps<T>::threads, SCAN_CTAS(T, NP)) k_clear_scan_backward(const __grid_constant__ ScanSet s) {
+__global__ void __launch_bounds__(ScanWarps<T>::threads, NP == 128 ? 1 : SCAN_CTAS(T, NP)) k_clear_scan_backward(const __grid_constant__ ScanSet s) {
     pdl_begin();
     const uint32_t which = blockIdx.x % 3, block = blockIdx.x / 3;
     if (which < 2) sweep<T, 64, NP, MODE_GRAD>(s.a[which], block);
@@ -625,7 +625,8 @@ cudaError_t scan_launch(const ScanSet& s, int mode, cudaStream_t st) {
 extern template cudaError_t scan_launch<__nv_bfloat16>(const ScanSet&, int, cudaStream_t);
 extern template cudaError_t scan_launch<__half>(const ScanSet&, int, cudaStream_t);
 extern template cudaError_t scan_launch<float>(const ScanSet&, int, cudaStream_t);
-// The same on tcgen05: bfloat16, states of 65 to 128 columns, N and P multiples of 8, operands and outputs with 16-byte rows (clear_scan_tc.cu).
+// The same on tcgen05: bfloat16, N and P multiples of 8, operands and outputs with 16-byte rows (clear_scan_tc.cu; states of 8 columns take as long as
+// states of 64 there, and still less than on mma.sync).
 // part is [b][head tile][segment][chunk of 128][16384] in an order of its own there, and dots is left to the kernel that sums it up over heads.
 cudaError_t scan_tc_launch(const ScanSet& s, int mode, cudaStream_t st);
 struct TcSums {

@@ -1,4 +1,4 @@
-// The sweep of the cleartext recurrence on the fifth-generation tensor cores (tcgen05), for bfloat16 and states of 65 to 128 columns: the
+// The sweep of the cleartext recurrence on the fifth-generation tensor cores (tcgen05), for bfloat16 and rows that allow 16-byte accesses: the
 // deployed layer's.  The mathematics is that of clear_scan.cuh, with chunks of 128 tokens.
 //
 // Of its operands one pair is broad (a group's rows of N columns) and one narrow (a head's 64 channels); the state H [N][64] is always
@@ -244,7 +244,8 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                 if (c) wait(b_o, c - 1);                             // the scores' planes lie over the scores
                 tc_after();
 #pragma unroll
-                for (uint32_t j = 0; j < QK / 4; j++) product(Lay::S, pq + j * STEP, 2, (Lay::OUT ? pb : pn) + j * STEP, 2, I_S, 4, j, SHARED);
+                for (uint32_t j = 0; j < QK / 4; j++)
+                    if (!j || a.N > 64) product(Lay::S, pq + j * STEP, 2, (Lay::OUT ? pb : pn) + j * STEP, 2, I_S, 4, j, SHARED);
                 tc_commit(b_s);
             }
             wait(b_wv + 8 * set, c >> 1);
@@ -258,7 +259,8 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                 tc_after();
                 if (Lay::OUT) {
 #pragma unroll
-                    for (uint32_t j = 0; j < 2; j++) product(Lay::O1, pq + j * STEP, 2, ps + 512 * j, 128, I_O1, 4, j, SHARED);
+                    for (uint32_t j = 0; j < 2; j++)
+                        if (!j || a.N > 64) product(Lay::O1, pq + j * STEP, 2, ps + 512 * j, 128, I_O1, 4, j, SHARED);
                 } else {
 #pragma unroll
                     for (uint32_t p = 0; p < NO; p++) product(Lay::O1, pq, 2, ps + p * STEP, 2, I_O1, 4, p, SHARED);
@@ -341,19 +343,21 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
             for (int j = 0; j < n; j++, src += 64, width -= 64) {
                 const int bytes = min(max(width - (int)col, 0), 8) * 2;
                 const uint32_t dst = to + (first + j) * PANEL;
-                const T* p = src;
-                if (valid == TC_Q && bytes == 16) {
+                const T* p = bytes ? src : (const T*)a.g;
+                const long long by = bytes ? step : 0;
+                if (valid == TC_Q) {
 #pragma unroll 8
-                    for (uint32_t i = 0; i < TC_Q / 8; i++, p += step) cp_async16(dst + 1024 * i, p);
+                    for (uint32_t i = 0; i < TC_Q / 8; i++, p += by) cp_async16_part(dst + 1024 * i, p, bytes);
                 } else {
 #pragma unroll 1
-                    for (uint32_t i = 0; i < TC_Q / 8; i++, p += step) {
+                    for (uint32_t i = 0; i < TC_Q / 8; i++, p += by) {
                         const int some = (int)(r0 + 8 * i) < valid ? bytes : 0;
                         cp_async16_part(dst + 1024 * i, some ? p : (const T*)a.g, some);
                     }
                 }
             }
         };
+        const int wide_panels = a.N > 64 ? 2 : 1;        // the second panel of narrower rows is zero from the first chunk of its set on
         auto landed = [&](uint32_t which) {
             cp_async_wait();
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -364,12 +368,12 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
         for (int c = 0; c < chunks; c++) {
             const uint32_t set = c & 1;
             if (c >= 2) wait(b_used + 8 * set, (c >> 1) - 1);
-            copy(Lay::broad + 2 * set, 2, pb, sb, (int)a.N, left(c));
+            copy(Lay::broad + 2 * set, c < 2 ? 2 : wide_panels, pb, sb, (int)a.N, left(c));
             copy(Lay::narrow + set, 1, pn, sn, pw, left(c));
             landed(b_kv + 8 * set);
             if (MODE) {
                 if (c) wait(b_o1, c - 1);
-                copy(Lay::q, Lay::QP, pq, sq, qw, left(c));
+                copy(Lay::q, Lay::OUT ? wide_panels : 1, pq, sq, qw, left(c));
                 landed(b_q);
             }
             pb += sb * (TC_Q / 8), pn += sn * (TC_Q / 8), pq += sq * (TC_Q / 8);
