@@ -6,6 +6,8 @@
 //   dg_t = <h_t, dh_t>' summed back from the segment's end:  R_t = R_{t+1} + row_t - col_t,  R behind a segment = <h, dh> there,
 // so no state has to be kept per token.  Rounding adds up over a segment only, whose end is computed from the states themselves.
 #define FESC_DBG_FILE 20   // file id in the sites a debug build reports
+#include <initializer_list>
+
 #include "clear_scan.cuh"
 
 static thread_local std::string clear_error;
@@ -258,7 +260,9 @@ __global__ void __launch_bounds__(256) k_clear_scan_step(const StepArgs a) {
 // ---------------------------------------------------------------------------------------
 struct ScanShape {
     uint32_t tiles, vheads, segments, seg_chunks, np;
-    bool tc;                   // the sweeps run on tcgen05 if the operands' alignment allows
+    bool tc;                   // the sweeps run on tcgen05 (if the operands' addresses allow)
+    bool pack;                 // their operands are copied into rows of 16 bytes first
+    size_t x_pack, b_pack;     // floats of a copy of x or dy, and of B or C
     size_t states, state_floats, decay_floats, part_floats, dot_floats, end_floats;
 };
 
@@ -268,7 +272,9 @@ struct ScanShape {
 // segments, 30 us, with one 65; backwards 2, 95 us, with 6 128.)
 static ScanShape scan_shape(const fesc_clear_scan_desc* d, bool backward) {
     ScanShape s;
-    s.tc = d->type == FESC_BF16 && d->N % 8 == 0 && d->P % 8 == 0;
+    s.tc = d->type == FESC_BF16;
+    auto odd = [](const int64_t(&st)[3]) { return (st[0] | st[1] | st[2]) % 8 != 0; };
+    s.pack = s.tc && (d->N % 8 || d->P % 8 || odd(d->x) || odd(d->B) || odd(d->C) || (backward && odd(d->y)));
     s.tiles = (d->P + SCAN_TILE - 1) / SCAN_TILE, s.vheads = d->H * s.tiles, s.np = s.tc || d->N > 64 ? 128 : 64;
     const uint64_t pieces = ((uint64_t)d->L + 127) / 128, ctas = (uint64_t)d->batch * s.vheads, sweeps = backward ? 3 : 1;
     const double START = s.tc ? 2.0 : 0.5, CHAIN = s.tc ? 1.5 : 0.5, STATE = s.tc ? 0.35 : 0.5;
@@ -296,6 +302,8 @@ static ScanShape scan_shape(const fesc_clear_scan_desc* d, bool backward) {
     s.part_floats = whole((size_t)d->batch * s.vheads * s.np * (s.tc ? (size_t)s.segments * s.seg_chunks * SCAN_Q : d->L));
     s.dot_floats = whole((size_t)d->batch * s.vheads * d->L);
     s.end_floats = whole((size_t)d->batch * s.segments * s.vheads);
+    s.x_pack = s.pack ? whole((size_t)d->batch * d->L * d->H * ((d->P + 7) / 8 * 4)) : 0;
+    s.b_pack = s.pack ? whole((size_t)d->batch * d->L * d->G * ((d->N + 7) / 8 * 4)) : 0;
     return s;
 }
 
@@ -363,15 +371,34 @@ static cudaError_t combine(const fesc_clear_scan_desc* d, const ScanShape& s, co
                   s.states);
 }
 
+// Copies of operands in rows of whole 16-byte pieces, at `w` and on; the operands then are the copies.
+struct Packed {
+    ScanOperand* o;
+    uint32_t heads, width;
+    size_t floats;
+};
+static cudaError_t pack(const fesc_clear_scan_desc* d, std::initializer_list<Packed> list, float* w, const int* lengths, cudaStream_t st) {
+    TcPack a = {};
+    a.lengths = lengths, a.L = d->L;
+    for (const Packed& p : list) {
+        auto& o = a.o[a.count++];
+        const long long row = (p.width + 7) / 8 * 8;
+        o.src = p.o->p, o.dst = w, o.sb = p.o->sb, o.st = p.o->st, o.sh = p.o->sh, o.heads = p.heads, o.width = p.width;
+        *p.o = {w, (long long)d->L * p.heads * row, p.heads * row, row, p.o->tiled, 16};
+        w += p.floats;
+    }
+    return scan_tc_pack(a, d->batch, st);
+}
+
 extern "C" size_t fesc_clear_scan_work(const fesc_clear_scan_desc* desc) {
     if (!desc || scan_check(desc)) return 0;
     const ScanShape s = scan_shape(desc, false);
-    return (s.state_floats + s.decay_floats) * sizeof(float);
+    return (s.state_floats + s.decay_floats + s.x_pack + 2 * s.b_pack) * sizeof(float);
 }
 extern "C" size_t fesc_clear_scan_backward_work(const fesc_clear_scan_desc* desc) {
     if (!desc || scan_check(desc)) return 0;
     const ScanShape s = scan_shape(desc, true);
-    return (2 * (s.state_floats + s.decay_floats + s.part_floats + s.dot_floats + s.end_floats)) * sizeof(float);
+    return (2 * (s.state_floats + s.decay_floats + s.part_floats + s.dot_floats + s.end_floats + s.x_pack + s.b_pack)) * sizeof(float);
 }
 
 extern "C" int fesc_clear_scan(const fesc_clear_scan_desc* desc, const void* d_x, const float* d_g, const void* d_B, const void* d_C, const float* d_skip,
@@ -394,7 +421,10 @@ extern "C" int fesc_clear_scan(const fesc_clear_scan_desc* desc, const void* d_x
     const uint32_t bytes = clear_type_bytes(d.type);
     ScanArgs a = scan_args(desc, s, d_g, d_lengths);
     a.q = operand(d_C, d.C, false, bytes), a.k = operand(d_B, d.B, false, bytes), a.v = operand(d_x, d.x, true, bytes);
-    const bool tc = s.tc && a.q.align == 16 && a.k.align == 16 && a.v.align == 16 && out_width(d_y, d.y, bytes);
+    if (s.pack)
+        CLEAR_CUDA(pack(desc, {{&a.v, d.H, d.P, s.x_pack}, {&a.k, d.G, d.N, s.b_pack}, {&a.q, d.G, d.N, s.b_pack}}, (float*)d_work + s.state_floats + s.decay_floats,
+                        d_lengths, st));
+    const bool tc = s.tc && a.q.align == 16 && a.k.align == 16 && a.v.align == 16;
     a.init = d_h0;
     if (s.segments > 1) {
         float* states = (float*)d_work;
@@ -446,9 +476,10 @@ extern "C" int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const 
     float *part_b = take(s.part_floats), *part_c = take(s.part_floats), *row = take(s.dot_floats), *col = take(s.dot_floats);
     float *ends = take(s.end_floats), *diag = take(s.end_floats);
     const uint32_t bytes = clear_type_bytes(d.type);
-    const ScanOperand x = operand(d_x, d.x, true, bytes), B = operand(d_B, d.B, false, bytes), C = operand(d_C, d.C, false, bytes),
-                      dy = operand(d_dy, d.y, true, bytes);
-    const bool tc = s.tc && x.align == 16 && B.align == 16 && C.align == 16 && dy.align == 16 && out_width(d_dx, d.dx, bytes) && out_width(d_dB, d.dB, bytes) && out_width(d_dC, d.dC, bytes);
+    ScanOperand x = operand(d_x, d.x, true, bytes), B = operand(d_B, d.B, false, bytes), C = operand(d_C, d.C, false, bytes), dy = operand(d_dy, d.y, true, bytes);
+    if (s.pack)
+        CLEAR_CUDA(pack(desc, {{&x, d.H, d.P, s.x_pack}, {&dy, d.H, d.P, s.x_pack}, {&B, d.G, d.N, s.b_pack}, {&C, d.G, d.N, s.b_pack}}, w, d_lengths, st));
+    const bool tc = s.tc && x.align == 16 && B.align == 16 && C.align == 16 && dy.align == 16;
     const ScanArgs base = scan_args(desc, s, d_g, d_lengths);
     const float *h = d_h0, *dh = d_dh_out;
     if (s.segments > 1) {
@@ -475,7 +506,7 @@ extern "C" int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const 
     f.log_quads = d.N > 64 ? 5 : 4, f.dg_blocks = d.batch * d.H * s.segments;
     if (tc) {        // sums of their own; the decays after them
         TcSums t = {part_b, part_c, B, C, (__nv_bfloat16*)d_dB, (__nv_bfloat16*)d_dC, row, col, d_lengths, f.Bb, f.Bt, f.Bg, f.Cb, f.Ct, f.Cg,
-                    d.L, d.H, d.G, d.N, s.tiles, s.segments, s.seg_chunks};
+                    d.L, d.H, d.G, d.N, s.tiles, s.segments, s.seg_chunks, out_width(d_dB, d.dB, bytes) && out_width(d_dC, d.dC, bytes)};
         CLEAR_CUDA(scan_tc_sums(t, d.batch, st));
     } else {
         f.sum_each = (uint32_t)((((size_t)d.L << f.log_quads) + 255) / 256), f.sum_blocks = 2 * d.batch * d.G * f.sum_each;

@@ -625,7 +625,7 @@ cudaError_t scan_launch(const ScanSet& s, int mode, cudaStream_t st) {
 extern template cudaError_t scan_launch<__nv_bfloat16>(const ScanSet&, int, cudaStream_t);
 extern template cudaError_t scan_launch<__half>(const ScanSet&, int, cudaStream_t);
 extern template cudaError_t scan_launch<float>(const ScanSet&, int, cudaStream_t);
-// The same on tcgen05: bfloat16, N and P multiples of 8, operands and outputs with 16-byte rows (clear_scan_tc.cu; states of 8 columns take as long as
+// The same on tcgen05: bfloat16, operands with 16-byte rows (clear_scan_tc.cu; others are copied into such rows first; states of 8 columns take as long as
 // states of 64 there, and still less than on mma.sync).
 // part is [b][head tile][segment][chunk of 128][16384] in an order of its own there, and dots is left to the kernel that sums it up over heads.
 cudaError_t scan_tc_launch(const ScanSet& s, int mode, cudaStream_t st);
@@ -637,5 +637,17 @@ struct TcSums {
     const int* lengths;
     long long Bb, Bt, Bg, Cb, Ct, Cg;
     uint32_t L, H, G, N, tiles, segments, seg_chunks;
+    uint32_t wide;              // rows of dB and dC allow 16-byte accesses
 };
 cudaError_t scan_tc_sums(const TcSums& a, uint32_t batch, cudaStream_t st);
+struct TcPack {
+    struct {
+        const void* src;
+        void* dst;               // [b][L][heads][width in pieces of 8]
+        long long sb, st, sh;
+        uint32_t heads, width;
+    } o[4];
+    const int* lengths;
+    uint32_t L, count;
+};
+cudaError_t scan_tc_pack(const TcPack& a, uint32_t batch, cudaStream_t st);

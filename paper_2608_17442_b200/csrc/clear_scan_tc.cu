@@ -557,9 +557,13 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                 }
                 if (a.out_wide > 1 && count >= 16) {
                     st32(out, o);
-                } else {
+                } else if (a.out_wide && !(count & 7)) {
                     if (count >= 8) *reinterpret_cast<uint4*>(out) = make_uint4(o[0], o[1], o[2], o[3]);
                     if (count >= 16) *reinterpret_cast<uint4*>(out + 8) = make_uint4(o[4], o[5], o[6], o[7]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; e++)
+                        if (e < count) reinterpret_cast<uint16_t*>(out)[e] = (uint16_t)(o[e / 2] >> (e & 1 ? 16 : 0));
                 }
             } else {
                 // A warp's 32 rows x 32 columns lie together, a thread's eight columns after another's (the sums read them the same way): as rows of
@@ -705,8 +709,15 @@ __global__ void __launch_bounds__(512) k_clear_scan_tc_sums(const TcSums a) {
             }
         __syncthreads();
     }
-    if (there)
-        *reinterpret_cast<uint4*>(dst + n) = make_uint4(pack_bf16(sum[0].x, sum[0].y), pack_bf16(sum[1].x, sum[1].y), pack_bf16(sum[2].x, sum[2].y), pack_bf16(sum[3].x, sum[3].y));
+    if (!there) return;
+    const uint32_t r[4] = {pack_bf16(sum[0].x, sum[0].y), pack_bf16(sum[1].x, sum[1].y), pack_bf16(sum[2].x, sum[2].y), pack_bf16(sum[3].x, sum[3].y)};
+    if (a.wide && n + 8 <= a.N) {
+        *reinterpret_cast<uint4*>(dst + n) = make_uint4(r[0], r[1], r[2], r[3]);
+    } else {
+#pragma unroll
+        for (uint32_t e = 0; e < 8; e++)
+            if (n + e < a.N) reinterpret_cast<uint16_t*>(dst)[n + e] = (uint16_t)(r[e / 2] >> (e & 1 ? 16 : 0));
+    }
 }
 cudaError_t scan_tc_sums(const TcSums& a, uint32_t batch, cudaStream_t st) {
     return launch(k_clear_scan_tc_sums, dim3(8 * a.segments * (a.seg_chunks / 2), a.G, batch), dim3(512), 0, st, a);
@@ -721,6 +732,32 @@ cudaError_t scan_tc_launch(const ScanSet& s, int mode, cudaStream_t st) {
     return mode == MODE_STATE ? go(k_clear_scan_tc_state, TcLayout<MODE_STATE>::bytes)
          : mode == MODE_OUT   ? go(k_clear_scan_tc, TcLayout<MODE_OUT>::bytes)
                               : go(k_clear_scan_tc_backward, std::max(TcLayout<MODE_GRAD>::bytes, TcLayout<MODE_OUT>::bytes));
+}
+
+// Copies operands whose rows do not allow 16-byte accesses into rows that do, with zeros behind their columns: at the price of one pass over them the
+// sweeps run on tcgen05 (2048 tokens of 24 heads and 127 columns 98 -> 37 us).  A warp takes a token, blockIdx.z an operand.
+__global__ void __launch_bounds__(256) k_clear_scan_pack(const TcPack a) {
+    pdl_begin();
+    const auto& o = a.o[blockIdx.z];
+    const uint32_t lane = threadIdx.x & 31, b = blockIdx.y;
+    const long long t = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int length = a.lengths ? min(max(a.lengths[b], 0), (int)a.L) : (int)a.L;
+    if (t >= length) return;
+    const uint32_t pieces = (o.width + 7) / 8;
+    const uint16_t* src = (const uint16_t*)o.src + b * o.sb + t * o.st;
+    uint4* dst = (uint4*)o.dst + ((size_t)b * a.L + t) * o.heads * pieces;
+    if (!DBG_REGION(src, ((o.heads - 1) * o.sh + o.width) * 2) || !DBG_REGION(dst, (size_t)o.heads * pieces * 16)) return;
+    for (uint32_t i = lane; i < o.heads * pieces; i += 32) {
+        const uint32_t h = i / pieces, c = i % pieces * 8;
+        const uint16_t* p = src + h * o.sh + c;
+        uint32_t v[4];
+#pragma unroll
+        for (uint32_t e = 0; e < 4; e++) v[e] = (c + 2 * e < o.width ? (uint32_t)p[2 * e] : 0u) | (c + 2 * e + 1 < o.width ? (uint32_t)p[2 * e + 1] << 16 : 0u);
+        dst[i] = make_uint4(v[0], v[1], v[2], v[3]);
+    }
+}
+cudaError_t scan_tc_pack(const TcPack& a, uint32_t batch, cudaStream_t st) {
+    return a.L ? launch(k_clear_scan_pack, dim3((a.L + 7) / 8, batch, a.count), dim3(256), 0, st, a) : cudaSuccess;
 }
 
 extern "C" int fesc_clear_sync(void* stream) {

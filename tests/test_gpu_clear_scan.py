@@ -158,7 +158,7 @@ def test_negative_and_excessive_lengths_are_taken_into_range():
 
 
 @pytest.mark.parametrize("t", ["bf16", "fp16", "fp32"])
-@pytest.mark.parametrize("kind", ["columns", "odd", "time_major", "shared"])
+@pytest.mark.parametrize("kind", ["columns", "odd", "shifted", "time_major", "shared"])
 def test_strides_and_alignment(kind, t):
     c = case(2, 131, 2, 40, 24, 2, t, True)
     s = make(c, 7)
@@ -170,9 +170,9 @@ def test_strides_and_alignment(kind, t):
         return view
 
     y = None
-    if kind in ("columns", "odd"):
-        extra = 3 if kind == "odd" else 8
-        wide_ = torch.zeros((b, L, H * P + 2 * G * N + 2 * extra), dtype=T, device="cuda")
+    if kind in ("columns", "odd", "shifted"):        # shifted: strides that allow 16-byte accesses, addresses that do not
+        extra = {"columns": 8, "odd": 3, "shifted": 1}[kind]
+        wide_ = torch.zeros((b, L, H * P + 2 * G * N + {"columns": 16, "odd": 6, "shifted": 8}[kind]), dtype=T, device="cuda")
         cols = wide_[..., extra:]
         r["x"] = into(s["x"], cols[..., :H * P].unflatten(-1, (H, P)))
         r["B"] = into(s["B"], cols[..., H * P:H * P + G * N].unflatten(-1, (G, N)))
