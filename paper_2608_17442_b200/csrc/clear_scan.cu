@@ -190,17 +190,17 @@ __global__ void __launch_bounds__(THREADS) k_clear_scan_finish(const FinishArgs 
     if (lane == 0 && DBG_REGION(a.dskip + head, sizeof(float))) a.dskip[head] = (float)s;
 }
 
-// One token.  A warp takes rows of the state, a lane up to four of its columns; read and written once, bound by that.
+// One token.  A warp takes ROWS rows of the state, a lane up to four of its columns; read and written once, past what the caches hold on to: bound
+// by that (192 sequences of 24 heads: 303 MB in 51 us; with four rows on their way 60).
 struct StepArgs {
     const void *x, *B, *C;
     const float *g, *skip, *state;
     float* out;
     void* y;
     long long xb, xh, Bb, Bg, Cb, Cg, gb, gh, yb, yh;
-    uint32_t H, P, N, G, rows;     // rows of the state per warp
-    uint32_t wide;
+    uint32_t H, P, N, G;
 };
-template <class T, bool WIDE>
+template <class T, bool WIDE, int ROWS>
 __global__ void __launch_bounds__(256) k_clear_scan_step(const StepArgs a) {
     pdl_begin();
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, head = blockIdx.x % a.H, b = blockIdx.x / a.H, group = head / (a.H / a.G);
@@ -219,39 +219,44 @@ __global__ void __launch_bounds__(256) k_clear_scan_step(const StepArgs a) {
         const uint32_t n = WIDE ? lane * 4 + e : lane + 32 * e;
         vB[e] = n < a.N ? ClearType<T>::to(B[n]) : 0.f, vC[e] = n < a.N ? ClearType<T>::to(C[n]) : 0.f;
     }
-    const uint32_t first = (blockIdx.y * 8 + warp) * a.rows, end = min(first + a.rows, a.P);
-#pragma unroll 4
-    for (uint32_t p = first; p < end; p++) {
-        const float xv = ClearType<T>::to(x[p]);
+    const uint32_t first = (blockIdx.y * 8 + warp) * ROWS;
+    float h[ROWS][4], xv[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; r++) {       // all of a warp's rows on their way before the first is used
+        const uint32_t p = first + r;
         const float* s = a.state + at + (size_t)p * a.N;
-        float* o = a.out + at + (size_t)p * a.N;
-        float h[4] = {}, sum = 0.f;
+        const bool live = p < a.P;
+        xv[r] = live ? ClearType<T>::to(x[p]) : 0.f;
         if (WIDE) {
-            if (lane * 4 < a.N) {
-                const float4 v = *reinterpret_cast<const float4*>(s + lane * 4);
-                h[0] = v.x, h[1] = v.y, h[2] = v.z, h[3] = v.w;
-            }
+            const float4 v = live && lane * 4 < a.N ? __ldcs(reinterpret_cast<const float4*>(s + lane * 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            h[r][0] = v.x, h[r][1] = v.y, h[r][2] = v.z, h[r][3] = v.w;
         } else {
 #pragma unroll
-            for (int e = 0; e < 4; e++)
-                if (lane + 32 * e < a.N) h[e] = s[lane + 32 * e];
+            for (int e = 0; e < 4; e++) h[r][e] = live && lane + 32 * e < a.N ? s[lane + 32 * e] : 0.f;
         }
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; r++) {
+        const uint32_t p = first + r;
+        if (p >= a.P) break;
+        float* o = a.out + at + (size_t)p * a.N;
+        float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             // a decay of zero drops what the state holds, also infinities
-            h[e] = (keep > 0.f || keep != keep ? keep * h[e] : 0.f) + xv * vB[e];
-            if ((WIDE ? lane * 4 : lane + 32 * e) < a.N) sum += h[e] * vC[e];
+            h[r][e] = (keep > 0.f || keep != keep ? keep * h[r][e] : 0.f) + xv[r] * vB[e];
+            sum += h[r][e] * vC[e];        // B and C are zero beyond the columns
         }
         if (WIDE) {
-            if (lane * 4 < a.N) *reinterpret_cast<float4*>(o + lane * 4) = make_float4(h[0], h[1], h[2], h[3]);
+            if (lane * 4 < a.N) __stcs(reinterpret_cast<float4*>(o + lane * 4), make_float4(h[r][0], h[r][1], h[r][2], h[r][3]));
         } else {
 #pragma unroll
             for (int e = 0; e < 4; e++)
-                if (lane + 32 * e < a.N) o[lane + 32 * e] = h[e];
+                if (lane + 32 * e < a.N) o[lane + 32 * e] = h[r][e];
         }
 #pragma unroll
         for (int w = 16; w; w >>= 1) sum += __shfl_xor_sync(~0u, sum, w);
-        if (lane == 0) y[p] = ClearType<T>::from(sum + skip * xv);
+        if (lane == 0) y[p] = ClearType<T>::from(sum + skip * xv[r]);
     }
 }
 
@@ -534,12 +539,15 @@ extern "C" int fesc_clear_scan_step(const fesc_clear_scan_desc* desc, const void
     if (same_buffer(d_y, d_x) || same_buffer(d_y, d_B) || same_buffer(d_y, d_C)) return clear_fail(FESC_EINVAL, "clear_scan_step: y is an input");
     if ((uint64_t)d.batch * d.H >= (1ull << 31)) return clear_fail(FESC_EINVAL, "clear_scan_step: too many sequences and heads for one call");
     StepArgs a = {d_x, d_B, d_C, d_g, d_skip, d_state, d_state_out, d_y, d.x[0], d.x[2], d.B[0], d.B[2], d.C[0], d.C[2], d.g[0], d.g[2], d.y[0], d.y[2],
-                  d.H, d.P, d.N, d.G, 0, 0};
+                  d.H, d.P, d.N, d.G};
     const bool wide = d.N % 4 == 0 && ((size_t)d_state & 15) == 0 && ((size_t)d_state_out & 15) == 0;
-    // eight rows per warp share B and C; where that leaves SMs without a CTA, one
-    a.rows = (uint64_t)d.batch * d.H * ((d.P + 63) / 64) >= 4 * 148 ? 8 : 1;
-    const dim3 grid(d.batch * d.H, (d.P + 8 * a.rows - 1) / (8 * a.rows));
-    auto pick = [&](auto t) { return wide ? k_clear_scan_step<decltype(t), true> : k_clear_scan_step<decltype(t), false>; };
+    // eight rows per warp share B and C; where that leaves SMs without a CTA, one (a token of 24 heads: 192 CTAs instead of 24)
+    const bool many = (uint64_t)d.batch * d.H * ((d.P + 63) / 64) >= 4 * 148;
+    const dim3 grid(d.batch * d.H, many ? (d.P + 63) / 64 : (d.P + 7) / 8);
+    auto pick = [&](auto t) {
+        using T = decltype(t);
+        return wide ? many ? k_clear_scan_step<T, true, 8> : k_clear_scan_step<T, true, 1> : many ? k_clear_scan_step<T, false, 8> : k_clear_scan_step<T, false, 1>;
+    };
     auto kernel = d.type == FESC_BF16 ? pick(__nv_bfloat16()) : d.type == FESC_F16 ? pick(__half()) : pick(float());
     CLEAR_CUDA(launch(kernel, grid, dim3(256), 0, (cudaStream_t)stream, a));
     return FESC_OK;
