@@ -4,7 +4,7 @@
 //
 // The gradient of the log decays comes from what the sweeps give: with row_t = C_t . dC_t and col_t = B_t . dB_t of one head,
 //   dg_t = <h_t, dh_t>' summed back from the segment's end:  R_t = R_{t+1} + row_t - col_t,  R behind a segment = <h, dh> there,
-// so no state has to be kept per token.  Rounding adds up over a segment only, whose end is computed from the states themselves.
+// so no state has to be kept per token.  Rounding adds up over a segment only, whose ends are computed from the states themselves.
 #define FESC_DBG_FILE 20   // file id in the sites a debug build reports
 #include <initializer_list>
 
@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(256) k_clear_combine(const Chain forwards, con
 }
 
 struct FinishArgs {
-    const float *part_b, *part_c, *row, *col, *ends, *diag, *g;
+    const float *part_b, *part_c, *row, *col, *ends, *starts, *diag, *g;
     void *dB, *dC;
     float *dg, *dskip;
     const int* lengths;
@@ -116,7 +116,9 @@ __global__ void __launch_bounds__(THREADS) k_clear_scan_finish(const FinishArgs 
     }
     const uint32_t blk = blockIdx.x - a.sum_blocks;
     if (blk < a.dg_blocks) {
-        // R_t = R_{t+1} + row_t - col_t from the segment's end, a token a thread; the next ones' words are read while these are summed
+        // R_t = R_{t+1} + row_t - col_t from the segment's end, where R is known; it is known at the segment's beginning, too, and what the sum
+        // misses it by is spread over the tokens: the products' rounding leans to one side and adds up with the tokens (1024 of them took the error
+        // from 1e-6 to 2e-6).  A token a thread; the next ones' words are read while these are summed
         const uint32_t head = blk % a.H, seg = blk / a.H % a.segments, b = blk / a.H / a.segments;
         const int length = tokens(b), lo = (int)(seg * a.seg_chunks) * SCAN_Q, hi = min(length, lo + (int)a.seg_chunks * SCAN_Q);
         if (lo >= hi) return;
@@ -127,6 +129,23 @@ __global__ void __launch_bounds__(THREADS) k_clear_scan_finish(const FinishArgs 
         if (!DBG_REGION(dg + lo * a.gt, ((long long)(hi - 1 - lo) * a.gt + 1) * sizeof(float))) return;
         double run = 0.0;
         for (uint32_t s = 0; s < a.tiles; s++) run += a.ends[((size_t)b * a.segments + seg) * vheads + head * a.tiles + s];
+        double low = 0.0, total = 0.0, slope = 0.0;
+        const float* begin = seg ? a.ends + ((size_t)b * a.segments + seg - 1) * vheads : a.starts ? a.starts + (size_t)b * a.segments * vheads : nullptr;
+        for (uint32_t s = 0; begin && s < a.tiles; s++) low += begin[head * a.tiles + s];
+        bool dropped = false;
+        for (int t = hi - 1 - (int)tid; t >= lo; t -= THREADS) {
+            for (uint32_t s = 0; s < a.tiles; s++) total += (double)row[(size_t)s * a.L + t] - (double)col[(size_t)s * a.L + t];
+            dropped = dropped || g[t * a.it] < SCAN_DROP;
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(~0u, total, o);
+        if (lane == 0) words[0][warp] = total;
+        if (!__syncthreads_or(dropped)) {        // a dropped state is a beginning of its own
+            total = 0.0;
+            for (uint32_t w = 0; w < WARPS; w++) total += words[0][w];
+            slope = (run + total - low) / (double)(hi - lo);
+        }
+        __syncthreads();
         double next = 0.0;
         bool next_drop = false;
         auto read = [&](int t) {
@@ -174,7 +193,7 @@ __global__ void __launch_bounds__(THREADS) k_clear_scan_finish(const FinishArgs 
                 if ((int)lane >= o) sums += u;
             }
             const double before = __shfl_sync(~0u, sums, warp ? warp - 1 : 0);
-            if (t >= lo) dg[t * a.gt] = (float)(run + (warp ? before : 0.0) + v);
+            if (t >= lo) dg[t * a.gt] = (float)(run + (warp ? before : 0.0) + v - slope * (double)(hi - t));
             run += __shfl_sync(~0u, sums, WARPS - 1);
         }
         return;
@@ -403,7 +422,7 @@ extern "C" size_t fesc_clear_scan_work(const fesc_clear_scan_desc* desc) {
 extern "C" size_t fesc_clear_scan_backward_work(const fesc_clear_scan_desc* desc) {
     if (!desc || scan_check(desc)) return 0;
     const ScanShape s = scan_shape(desc, true);
-    return (2 * (s.state_floats + s.decay_floats + s.part_floats + s.dot_floats + s.end_floats + s.x_pack + s.b_pack)) * sizeof(float);
+    return (2 * (s.state_floats + s.decay_floats + s.part_floats + s.dot_floats + s.x_pack + s.b_pack) + 3 * s.end_floats) * sizeof(float);
 }
 
 extern "C" int fesc_clear_scan(const fesc_clear_scan_desc* desc, const void* d_x, const float* d_g, const void* d_B, const void* d_C, const float* d_skip,
@@ -479,7 +498,7 @@ extern "C" int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const 
     auto take = [&](size_t floats) { float* p = w; w += floats; return p; };
     float *before = take(s.state_floats), *behind = take(s.state_floats), *decay = take(s.decay_floats), *decay_back = take(s.decay_floats);
     float *part_b = take(s.part_floats), *part_c = take(s.part_floats), *row = take(s.dot_floats), *col = take(s.dot_floats);
-    float *ends = take(s.end_floats), *diag = take(s.end_floats);
+    float *ends = take(s.end_floats), *diag = take(s.end_floats), *starts = take(s.end_floats);
     const uint32_t bytes = clear_type_bytes(d.type);
     ScanOperand x = operand(d_x, d.x, true, bytes), B = operand(d_B, d.B, false, bytes), C = operand(d_C, d.C, false, bytes), dy = operand(d_dy, d.y, true, bytes);
     if (s.pack)
@@ -499,12 +518,13 @@ extern "C" int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const 
     ScanArgs &c = set.a[0], &b = set.a[1], &o = set.a[2];
     c.q = dy, c.k = x, c.v = B, c.u = C, c.init = h, c.meet = dh, c.part = part_c, c.dots = row, c.ends = ends, c.diag = diag;      // dC
     b.q = x, b.k = dy, b.v = C, b.u = B, b.init = dh, b.part = part_b, b.dots = col, b.backwards = 1;                               // dB
+    if (d_h0) b.meet = d_h0, b.ends = starts;
     // dx, and the gradient of the state before the first token
     o.q = B, o.k = C, o.v = dy, o.init = dh, o.last = d_dh0, o.skip = d_skip, o.out = d_dx, o.ob = d.dx[0], o.ot = d.dx[1], o.oh = d.dx[2];
     o.out_wide = out_width(d_dx, d.dx, bytes), o.backwards = 1;
     CLEAR_CUDA(scan_go(desc, tc, set, MODE_GRAD, st));
     FinishArgs f = {};
-    f.part_b = part_b, f.part_c = part_c, f.row = row, f.col = col, f.ends = ends, f.diag = diag;
+    f.part_b = part_b, f.part_c = part_c, f.row = row, f.col = col, f.ends = ends, f.starts = d_h0 ? starts : nullptr, f.diag = diag;
     f.dB = d_dB, f.dC = d_dC, f.dg = d_dg, f.dskip = d_dskip, f.lengths = d_lengths, f.g = d_g, f.ib = d.g[0], f.it = d.g[1], f.ih = d.g[2];
     f.Bb = d.dB[0], f.Bt = d.dB[1], f.Bg = d.dB[2], f.Cb = d.dC[0], f.Ct = d.dC[1], f.Cg = d.dC[2], f.gb = d.dg[0], f.gt = d.dg[1], f.gh = d.dg[2];
     f.b = d.batch, f.L = d.L, f.H = d.H, f.G = d.G, f.N = d.N, f.tiles = s.tiles, f.segments = s.segments, f.seg_chunks = s.seg_chunks;

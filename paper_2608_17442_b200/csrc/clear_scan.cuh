@@ -49,7 +49,7 @@ struct ScanArgs {
     float* part;                     // MODE_GRAD: [b][head tile][L][NP], NP = 64 or 128
     float* dots;                     // MODE_GRAD: [b][head tile][L], u . out
     const float* meet;               // MODE_GRAD forwards: states of the sweep backwards, as `init`; their product with this one's at the segments' ends
-    float* ends;                     //   [b][segment][head tile]
+    float* ends;                     //   [b][segment][head tile]; backwards: of h0 (meet) with the gradient before the first token, segment 0
     float* diag;                     //   sum over a segment's tokens of q . k, [b][segment][head tile]
     uint32_t b, L, H, P, G, N, tiles, segments, seg_chunks, backwards;
 };
@@ -218,7 +218,10 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
     const size_t slot = (size_t)b * a.segments + seg;
     if (MODE != MODE_STATE && t_lo >= length && !is_last) {
         // nothing of the sequence lies here; what later kernels read is zero
-        if (MODE == MODE_GRAD && a.ends && tid == 0) a.ends[slot * vheads + vh] = 0.f, a.diag[slot * vheads + vh] = 0.f;
+        if (MODE == MODE_GRAD && a.ends && tid == 0) {
+            a.ends[slot * vheads + vh] = 0.f;
+            if (a.diag) a.diag[slot * vheads + vh] = 0.f;
+        }
         return;
     }
     const int kw = a.k.tiled ? pw : (int)a.N, vw = a.v.tiled ? pw : (int)a.N;
@@ -238,7 +241,7 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
     }
     if ((MODE && a.init && !DBG_REGION(a.init + (a.segments > 1 ? slot : b) * states + state_at, (size_t)pw * a.N * 4)) ||
         (a.last && !DBG_REGION(a.last + (MODE == MODE_STATE ? slot : b) * states + state_at, (size_t)pw * a.N * 4)) ||
-        (MODE == MODE_GRAD && a.meet && !DBG_REGION(a.meet + (a.segments > 1 ? slot : b) * states + state_at, (size_t)pw * a.N * 4)))
+        (MODE == MODE_GRAD && a.meet && !DBG_REGION(a.meet + (a.segments > 1 && !a.backwards ? slot : b) * states + state_at, (size_t)pw * a.N * 4)))
         return;
 #endif
     __nv_bfloat16 *sk = sm + S::k, *sv = sm + S::v, *sq = sm + S::q, *ss = sm + S::s;
@@ -562,8 +565,8 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
     if (MODE == MODE_GRAD && a.ends) {
         // <state, gradient of the state> at the segment's end, one decay on from what the sweep backwards starts this segment with
         float sum = 0.f;
-        if (a.meet) {
-            fetch_state(a.meet + (a.segments > 1 ? slot : b) * states + state_at);
+        if (a.meet && (!a.backwards || seg == 0)) {
+            fetch_state(a.meet + (a.segments > 1 && !a.backwards ? slot : b) * states + state_at);
             __syncthreads();
 #pragma unroll
             for (int m = 0; m < MT; m++)
@@ -571,7 +574,8 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
                 for (int n = 0; n < KT; n++)
 #pragma unroll
                     for (int e = 0; e < 4; e++) sum += st[m][n][e] * state_word(m, n, e);
-            if (t_hi < length) sum *= expf(a.g[b * a.gb + t_hi * a.gt + head * a.gh]);
+            const int next = a.backwards ? 0 : t_hi;
+            if (next < length) sum *= expf(a.g[b * a.gb + next * a.gt + head * a.gh]);
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o), diag += __shfl_xor_sync(~0u, diag, o);
@@ -580,7 +584,8 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
         if (tid == 0) {
             float s0 = 0.f, s1 = 0.f;
             for (int w = 0; w < THREADS / 32; w++) s0 += words[0][w], s1 += words[1][w];
-            a.ends[slot * vheads + vh] = s0, a.diag[slot * vheads + vh] = s1;
+            a.ends[slot * vheads + vh] = s0;
+            if (a.diag) a.diag[slot * vheads + vh] = s1;
         }
     }
 }

@@ -162,7 +162,10 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
     const size_t state_at = (size_t)head * a.P * a.N + (size_t)tile * SCAN_TILE * a.N, states = (size_t)a.H * a.P * a.N;
     const size_t slot = (size_t)b * a.segments + seg;
     if (MODE != MODE_STATE && t_lo >= length && !is_last) {
-        if (MODE == MODE_GRAD && a.ends && tid == 0) a.ends[slot * vheads + vh] = 0.f, a.diag[slot * vheads + vh] = 0.f;
+        if (MODE == MODE_GRAD && a.ends && tid == 0) {
+            a.ends[slot * vheads + vh] = 0.f;
+            if (a.diag) a.diag[slot * vheads + vh] = 0.f;
+        }
         return;
     }
     const ScanOperand& ob = MODE == MODE_GRAD ? a.v : a.k;      // broad
@@ -184,7 +187,7 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
     }
     if ((MODE && a.init && !DBG_REGION(a.init + (a.segments > 1 ? slot : b) * states + state_at, (size_t)pw * a.N * 4)) ||
         (a.last && !DBG_REGION(a.last + (MODE == MODE_STATE ? slot : b) * states + state_at, (size_t)pw * a.N * 4)) ||
-        (MODE == MODE_GRAD && a.meet && !DBG_REGION(a.meet + (a.segments > 1 ? slot : b) * states + state_at, (size_t)pw * a.N * 4)))
+        (MODE == MODE_GRAD && a.meet && !DBG_REGION(a.meet + (a.segments > 1 && !a.backwards ? slot : b) * states + state_at, (size_t)pw * a.N * 4)))
         return;
 #endif
     const uint32_t base = ((uint32_t)__cvta_generic_to_shared(tc_smem) + 1023) & ~1023u, bar = (uint32_t)__cvta_generic_to_shared(bars);
@@ -601,14 +604,15 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
         }
         if (Lay::GRAD && a.ends) {
             float sum = 0.f;
-            const float* meet = a.meet ? a.meet + (a.segments > 1 ? slot : b) * states + state_at : nullptr;
+            const float* meet = a.meet && (!a.backwards || seg == 0) ? a.meet + (a.segments > 1 && !a.backwards ? slot : b) * states + state_at : nullptr;
             if (meet) {
 #pragma unroll
                 for (int i = 0; i < 16; i++) {
                     const int p = 16 * part + i;
                     if (p < pw && row < a.N) sum += (i & 1 ? st[i / 2].y : st[i / 2].x) * meet[(size_t)p * a.N + row];
                 }
-                if (t_hi < length) sum *= expf(a.g[b * a.gb + t_hi * a.gt + head * a.gh]);
+                const int next = a.backwards ? 0 : t_hi;
+                if (next < length) sum *= expf(a.g[b * a.gb + next * a.gt + head * a.gh]);
             }
 #pragma unroll
             for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o), diag += __shfl_xor_sync(~0u, diag, o);
@@ -617,7 +621,8 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
             if (tid == 0) {
                 float s0 = 0.f, s1 = 0.f;
                 for (int w = 0; w < TC_WARPS; w++) s0 += words[0][w], s1 += words[1][w];
-                a.ends[slot * vheads + vh] = s0, a.diag[slot * vheads + vh] = s1;
+                a.ends[slot * vheads + vh] = s0;
+                if (a.diag) a.diag[slot * vheads + vh] = s1;
             }
         }
     }
