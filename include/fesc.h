@@ -501,7 +501,8 @@ int fesc_scan_contract(fesc_ctx* ctx, const uint64_t* d_x, const uint64_t* d_a, 
  * the single token that serving it in the clear needs.  They take no context: sizes, strides and workspace come with the call, nothing is kept
  * between calls, and calls on different streams or in different threads do not meet (each needs a workspace of its own).
  *   - Activations are bfloat16, float16 or float32 (desc->type); log decays, states, weights of norms and their gradients float32.  All sums
- *     are held in float32 or more.  Results do not depend on the order in which anything runs.
+ *     are held in float32 or more.  The same call gives the same bits; which kernels
+ *     run, and so in which order sums are formed, goes by sizes, types and alignment.
  *   - Strides are in elements and not negative; the innermost dimension is contiguous.  Any alignment of the type is taken; 16 bytes (addresses
  *     and strides) are faster.  Outputs may not overlap inputs or one another, except where said.
  *   - Device pointers belong to the device that is current.  Calls enqueue work on `stream`, allocate nothing and can be captured into a graph.
@@ -511,6 +512,9 @@ enum { FESC_BF16 = 0, FESC_F16 = 1, FESC_F32 = 2 };
 const char* fesc_clear_last_error(void);
 /* Wait for `stream`; FESC_ETIMEOUT if a kernel's bounded wait gave up since the last such call on this device (its results are worth nothing). */
 int fesc_clear_sync(void* stream);
+/* Self-test of these waits: a warp waits on a barrier that nothing completes, until the wait gives up (about a second); the next fesc_clear_sync
+ * returns FESC_ETIMEOUT.  Nothing faults, traps or hangs. */
+int fesc_clear_selftest_wait_limit(void* stream);
 
 /*
  * Gated linear recurrence (Sec. 5.4, Eqs. fesc_recurrence / fesc_contract; g = log a), per sequence and head, h in R^{P x N}:
@@ -521,8 +525,7 @@ int fesc_clear_sync(void* stream);
  *   d_lengths int32 [batch] (DEVICE), tokens of every sequence, taken into [0, L], or NULL (L): tokens behind are neither read nor written
  *   d_h_out  [batch][H][P][N], the states behind the last token (length 0: before the first), or NULL; not d_h0
  * A log decay of -inf (any below -300) drops the state.  N <= 128, P <= 4096, L < 2^30, batch <= 65535.
- * Tokens of a chunk of 64 are multiplied with zeros among themselves: an infinity or NaN in a token reaches the other tokens of its chunk, and
- * everything after it.
+ * Tokens are multiplied with zeros in chunks of up to 128: an infinity or NaN in a token reaches the other tokens of its chunk, and everything after it.
  * Workspace: fesc_clear_scan_work(desc) bytes, aligned to 256 (0: none needed).
  */
 typedef struct fesc_clear_scan_desc {

@@ -117,6 +117,7 @@ def lib():
             "fesc_clear_scan_backward": [c.POINTER(ClearScanDesc)] + [vp] * 16 + [sz, vp],
             "fesc_clear_scan_step": [c.POINTER(ClearScanDesc)] + [vp] * 9,
             "fesc_clear_sync": [vp],
+            "fesc_clear_selftest_wait_limit": [vp],
             "fesc_clear_norm": [c.POINTER(ClearNormDesc)] + [vp] * 8,
             "fesc_clear_norm_backward": [c.POINTER(ClearNormDesc)] + [vp] * 13 + [sz, vp],
             "fesc_debug_bounds_register": [vp, sz],
@@ -413,6 +414,12 @@ def clear_sync():
     rc = lib().fesc_clear_sync(_stream())
     if rc != OK:
         raise FescError(rc, lib().fesc_clear_last_error().decode())
+
+
+def clear_selftest_wait_limit():
+    """A wait that runs out: the next clear_sync raises FescError(ETIMEOUT)."""
+    if lib().fesc_clear_selftest_wait_limit(_stream()) != OK:
+        raise FescError(ECUDA, lib().fesc_clear_last_error().decode())
 
 
 def clear_scan(x, g, B, C, y, skip=None, h0=None, h_out=None, lengths=None, work=None):

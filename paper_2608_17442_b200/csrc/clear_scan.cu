@@ -549,8 +549,9 @@ extern "C" int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const 
 extern "C" int fesc_clear_scan_step(const fesc_clear_scan_desc* desc, const void* d_x, const float* d_g, const void* d_B, const void* d_C, const float* d_skip,
                                     const float* d_state, float* d_state_out, void* d_y, void* stream) {
     if (!desc) return clear_fail(FESC_EINVAL, "clear_scan_step: no descriptor");
-    if (const char* what = scan_check(desc)) return clear_fail(FESC_EINVAL, what);
-    const fesc_clear_scan_desc& d = *desc;
+    fesc_clear_scan_desc d = *desc;
+    d.L = 1;
+    if (const char* what = scan_check(&d)) return clear_fail(FESC_EINVAL, what);
     if (d.batch == 0) return FESC_OK;
     if (!d_x || !d_g || !d_B || !d_C || !d_state || !d_state_out || !d_y) return clear_fail(FESC_EINVAL, "clear_scan_step: x, g, B, C, the states and y have to be given");
     if (!scan_strides(d.x, d.batch, 1, d.H, d.P, false) || !scan_strides(d.g, d.batch, 1, d.H, 1, false) || !scan_strides(d.B, d.batch, 1, d.G, d.N, false) ||

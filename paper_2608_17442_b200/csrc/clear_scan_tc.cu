@@ -64,7 +64,13 @@ __device__ __forceinline__ float ex2(float x) {
 }
 // The longer part of a wait, out of line: the kernel has some thirty of them, and its instructions have to stay in the cache of one SM.
 static __device__ __noinline__ void wait_on(uint32_t bar, uint32_t parity, volatile uint32_t* dead) {
-    if (!*dead && mbar_wait_bounded(bar, parity)) *dead = 1, g_clear_status = 1;
+    if (*dead) return;
+#pragma unroll 1
+    for (uint32_t it = 0; it < (1u << 18); it++) {      // about a second; a chunk takes microseconds
+        if (mbar_try_wait(bar, parity)) return;
+        if (it > 64) __nanosleep(64);
+    }
+    *dead = 1, g_clear_status = 1;
 }
 // bytes of (row, 16-byte chunk c of eight) in a panel
 __device__ __forceinline__ uint32_t panel_at(uint32_t row, uint32_t c) { return row * 128 + ((c ^ (row & 7)) << 4); }
@@ -647,7 +653,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc(const __grid_co
 __global__ void __launch_bounds__(TC_THREADS, 1) k_clear_scan_tc_backward(const __grid_constant__ ScanSet s) {
     __shared__ TcShared sh;
     pdl_begin();
-    const uint32_t which = blockIdx.x % 3, block = blockIdx.x / 3;
+    // one sweep after the other, the shortest at the end: neighbouring SMs mostly run the same instructions
+    const uint32_t each = gridDim.x / 3, which = blockIdx.x / each, block = blockIdx.x % each;
     if (which < 2) tc_sweep<MODE_GRAD, TC_BACK_UNROLL>(s.a[which], block, sh);
     else tc_sweep<MODE_OUT, TC_BACK_UNROLL>(s.a[2], block, sh);
 }
@@ -763,6 +770,23 @@ __global__ void __launch_bounds__(256) k_clear_scan_pack(const TcPack a) {
 }
 cudaError_t scan_tc_pack(const TcPack& a, uint32_t batch, cudaStream_t st) {
     return a.L ? launch(k_clear_scan_pack, dim3((a.L + 7) / 8, batch, a.count), dim3(256), 0, st, a) : cudaSuccess;
+}
+
+// One warp waits on a barrier that nothing completes; the wait runs out, the kernel records it and returns.
+__global__ void k_clear_wait_limit() {
+    __shared__ __align__(8) u64 bar;
+    __shared__ volatile uint32_t dead;
+    pdl_begin();
+    const uint32_t at = (uint32_t)__cvta_generic_to_shared(&bar);
+    if (threadIdx.x == 0) {
+        mbar_init(at, 1);
+        dead = 0;
+        wait_on(at, 0, &dead);
+    }
+}
+extern "C" int fesc_clear_selftest_wait_limit(void* stream) {
+    CLEAR_CUDA(launch(k_clear_wait_limit, dim3(1), dim3(32), 0, (cudaStream_t)stream));
+    return FESC_OK;
 }
 
 extern "C" int fesc_clear_sync(void* stream) {

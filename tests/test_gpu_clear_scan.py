@@ -322,3 +322,37 @@ def test_empty_calls():
     forward(nobody)
     assert (backward(nobody)["skip"] == 0).all()
     fesc.clear_scan_step(*(nobody[k][:, 0] for k in ("x", "g", "B", "C")), nobody["h0"], nobody["x"][:, 0].clone())
+
+
+def test_a_wait_that_runs_out_is_reported_and_nothing_else_is_lost():
+    c = case(1, 300, 2, 64, 128, 1, "bf16", True)
+    s = make(c, 15)
+    fesc.clear_sync()
+    fesc.clear_selftest_wait_limit()
+    with pytest.raises(fesc.FescError) as e:
+        fesc.clear_sync()
+    assert e.value.code == fesc.ETIMEOUT
+    check_forward(s, c, *forward(s))       # and a later call is sound again
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+def test_many_calls_with_different_inputs_in_turn(t):
+    """Three sets of inputs in turn, many times: the waits inside the kernels hold at every interleaving, and each set gives its own bits."""
+    sets = [make(case(1, 600 + 17 * k, 4, 64, 128, 1, t, True), 20 + k) for k in range(3)]
+    want = [(forward(s), backward(s)) for s in sets]
+    for k in range(60):
+        s, (f, b) = sets[k % 3], want[k % 3]
+        got, o = forward(s), backward(s)
+        if k >= 57:
+            assert torch.equal(got[0], f[0]) and torch.equal(got[1], f[1]) and all(torch.equal(o[n], b[n]) for n in o)
+    fesc.clear_sync()
+
+
+def test_step_reads_no_length():
+    d = fesc.ClearScanDesc(1, 0xffffffff, 1, 8, 1, 8, 2)
+    d.x[:], d.y[:], d.g[:], d.B[:], d.C[:] = (0, 0, 0), (0, 0, 0), (0, 0, 0), (0, 0, 0), (0, 0, 0)
+    z = {k: torch.ones(n, device="cuda") for k, n in (("x", 8), ("g", 1), ("B", 8), ("C", 8), ("h", 64), ("y", 8))}
+    p = {k: v.data_ptr() for k, v in z.items()}
+    assert fesc.lib().fesc_clear_scan_step(d, p["x"], p["g"], p["B"], p["C"], None, p["h"], p["h"], p["y"], fesc._stream()) == fesc.OK
+    torch.cuda.synchronize()
+    assert torch.allclose(z["h"], torch.full_like(z["h"], 2.718281828 + 1), rtol=1e-6)
