@@ -25,7 +25,7 @@
 
 #define TC_Q 128
 #define PANEL 16384u
-#define TC_BACK_UNROLL 2        // products in a row in the backward pass: 469 us (1: 470, 4: 482; all of them in the scan 299, 4 there 314)
+#define TC_BACK_UNROLL 2        // products in a row in the backward pass: 8 x 2048 tokens 431 us, 2048 101 (8: 427 and 104); in the scan all of them (299 us; 4: 314)
 #define TC_WARPS 16             // that compute; one more issues, one more sums decays, two copy
 #define TC_THREADS (32 * (TC_WARPS + 4))
 
@@ -442,7 +442,7 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
         };
         if (chunks) provide(0);
         for (int c = 0; c < chunks; c++) {
-            const int valid = left(c), set = c & 1;
+            const int set = c & 1;
             const TcDecays& d = decays[set];
             if (MODE) {
                 // decayed scores of this row and the columns 32 part .. 32 part + 31
@@ -527,7 +527,6 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                     st[e] = fma2(st[e], {keep, keep}, v);
                 }
             }
-            const float grow = d.grow[row];
             if (MODE && c + 1 < chunks) {
                 wait(b_o1, c);                 // the state's panels are free
                 provide(c + 1);                // before the outputs: O2 is under way
@@ -537,7 +536,8 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                 continue;
             }
 
-            const bool live = (int)row < valid;
+            const float grow = d.grow[row];
+            const bool live = (int)row < left(c);
             const long long t = t_first + (long long)dir * (c * TC_Q + (int)row);
             if (Lay::OUT) {
                 uint32_t skipped[8] = {};
