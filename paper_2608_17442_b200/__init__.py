@@ -5,6 +5,7 @@ libfesc_b200.so (declared in include/fesc.h); all arithmetic runs in the CUDA ke
 Tensors are torch CUDA tensors of dtype int64 (bit pattern = the uint64 residue); the
 binding passes their data pointers and the current torch stream.  There is no CPU
 fallback: importing succeeds without the library, but the first call raises.
+The operators on cleartext activations (clear_*) take tensors of activations and no context.
 """
 from __future__ import annotations
 
