@@ -524,7 +524,7 @@ int fesc_clear_selftest_wait_limit(void* stream);
  *   d_h0     [batch][H][P][N], the states before the first token, or NULL (0)
  *   d_lengths int32 [batch] (DEVICE), tokens of every sequence, taken into [0, L], or NULL (L): tokens behind are neither read nor written
  *   d_h_out  [batch][H][P][N], the states behind the last token (length 0: before the first), or NULL; not d_h0
- * A log decay of -inf (any below -300) drops the state.  N <= 128, P <= 4096, L < 2^30, batch <= 65535.
+ * Log decays are not positive; -inf (any below -300) drops the state.  N <= 128, P <= 4096, L < 2^30, batch <= 65535.
  * Tokens are multiplied with zeros in chunks of up to 128: an infinity or NaN in a token reaches the other tokens of its chunk, and everything after it.
  * Workspace: fesc_clear_scan_work(desc) bytes, aligned to 256 (0: none needed).
  */

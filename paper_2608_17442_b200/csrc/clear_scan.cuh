@@ -8,13 +8,16 @@
 // everything before it.  The state of a head tile (64 channels x up to 128) stays in the warps' registers in the accumulator layout of
 // mma.m16n8k16, which is also the layout of a left operand: the products are formed transposed (out^T = state q^T + v^T S^T) so that the state
 // multiplies q without going through memory.
-// A long sequence is cut into segments when there are too few heads to fill the SMs: k_clear_scan in MODE_STATE gives what every
-// segment adds to its state, k_clear_combine chains the segments, and every segment then runs with the state before it.
+// A long sequence is cut into segments when there are too few heads to fill the SMs: the sweep in MODE_STATE gives what every segment adds to
+// its state, k_clear_combine chains the segments, and every segment then runs with the state before it.
+// Measured (24 heads, 128 columns, 2048 tokens): float16 93 us, float32 113; 8 x 1024 tokens of 12 heads in float32 210.  A chunk is loads, scores,
+// products, outputs one after the other, with three to six matrix instructions per product of float32 planes; what bounds it are those chains.
 //
 // Operands are sums of bfloat16 numbers ("planes"): bfloat16 inputs one, float16 two (exact), float32 three (24 bits).  What the kernel
 // computes itself (decayed scores, weighted values, states) is cut into two planes (17 bits) where only outputs of 16 bits depend on it, and
-// into three (25 bits) where a float32 result does: states and the gradient of the log decays.  One plane, as 16-bit results alone would
-// stand, doubles their error (each of three roundings adds as much as the one at the end).  All sums are in float32.
+// into three (25 bits) where a float32 result does: states and the gradient of the log decays.  One plane would take
+// the error of 16-bit results to 1.4 times theirs (another rounding as large as the one at the end) and that of states to 2^-9.  All sums are in
+// float32.
 //
 // Log decays are summed in float64 per chunk and kept as two floats: with |g| up to 300 a token (below that a decay is zero: also -inf), one
 // float would leave 2^-10 of an exponent behind a strong decay.

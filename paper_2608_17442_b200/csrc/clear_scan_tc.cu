@@ -501,7 +501,6 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                     }
                 } else {
                     const uint32_t pl[8][NO] = {};
-                    
 #pragma unroll 1
                     for (int h = 0; h < 2; h++) write(pl, h);
                 }
