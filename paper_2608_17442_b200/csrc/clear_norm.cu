@@ -156,6 +156,7 @@ __global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : 4) k_clear_norm(c
 
 // dh_tot = dh + rho w - h rho^3 mean(w h),  w = gamma dn;  dr = dh_tot;  ds = sum_rows dh_tot v;  dv = s dh_tot;
 // dy = dv silu(z);  dz = dv y sigma (1 + z (1 - sigma)) = dv y (sigma + silu(z) (1 - sigma));  dgamma = sum_rows dn h rho
+// RESIDUAL: a residual, dh, or both
 template <class T, bool GATE, bool RESIDUAL, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : RESIDUAL ? 2 : 3) k_clear_norm_backward(const NormArgs a) {
     __shared__ float2 words[2][32];
@@ -174,11 +175,11 @@ __global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : RESIDUAL ? 2 : 3)
         int left = row < a.rows ? width : 0;
         const size_t bytes = span8<T>(left, a.wide);
         if (left > 0 && !(DBG_REGION(py + row * a.sy, bytes) && DBG_REGION(pn + row * a.sdn, bytes) && (!GATE || DBG_REGION(pz + row * a.sgate, bytes)) &&
-                          (!RESIDUAL || DBG_REGION(pr + row * a.sresidual, bytes)) && (!dh || DBG_REGION(ph + row * a.sdh, bytes))))
+                          (!RESIDUAL || !a.residual || DBG_REGION(pr + row * a.sresidual, bytes)) && (!dh || DBG_REGION(ph + row * a.sdh, bytes))))
             left = 0;
         ny.load(py + row * a.sy, left, a.wide), nw.load(pn + row * a.sdn, left, a.wide);
         if (GATE) nz.load(pz + row * a.sgate, left, a.wide);
-        if (RESIDUAL) nr.load(pr + row * a.sresidual, left, a.wide);
+        if (RESIDUAL) nr.load(pr + row * a.sresidual, a.residual ? left : 0, a.wide);
         if (dh) nh.load(ph + row * a.sdh, left, a.wide);
     };
     fetch(blockIdx.x * teams + team);
@@ -201,13 +202,13 @@ __global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : RESIDUAL ? 2 : 3)
         }
         float sum = sums.x + sums.y, dot = dots.x + dots.y;
         team_sum(sum, dot, words[turn], a.team_warps);
-        const float rho = rsqrtf(sum / (float)a.width + a.eps), k = rho * rho * rho * (dot / (float)a.width);
+        const float rho = rsqrtf(sum / (float)a.width + a.eps), k = rho * (rho * (rho * (dot / (float)a.width)));      // rho cubed alone may overflow
         int left = row < a.rows ? width : 0;
         T* dy = (T*)a.dy + (long long)row * a.sdy + first + c;
         T* dz = GATE ? (T*)a.dgate + (long long)row * a.sdgate + first + c : nullptr;
-        T* dr = RESIDUAL ? (T*)a.dresidual + (long long)row * a.sdresidual + first + c : nullptr;
+        T* dr = RESIDUAL && a.dresidual ? (T*)a.dresidual + (long long)row * a.sdresidual + first + c : nullptr;
         const size_t bytes = span8<T>(left, a.wide);
-        if (left > 0 && !(DBG_REGION(dy, bytes) && (!GATE || DBG_REGION(dz, bytes)) && (!RESIDUAL || DBG_REGION(dr, bytes)))) left = 0;
+        if (left > 0 && !(DBG_REGION(dy, bytes) && (!GATE || DBG_REGION(dz, bytes)) && (!dr || DBG_REGION(dr, bytes)))) left = 0;
         f2 d[4];
 #pragma unroll
         for (int e = 0; e < 4; e++) {
@@ -216,7 +217,7 @@ __global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : RESIDUAL ? 2 : 3)
             if (dh) d[e] = add2(d[e], hh[e]);
             dgamma[e] = fma2(wr, h[e], dgamma[e]);
         }
-        if (RESIDUAL) store8(dr, left, a.wide, d);
+        if (RESIDUAL && dr) store8(dr, left, a.wide, d);
         f2 o[4];
 #pragma unroll
         for (int e = 0; e < 4; e++) {
@@ -326,7 +327,7 @@ static auto by_type(uint32_t type, F f) {
 }
 
 // CTAs per group of channels, to which rows are dealt out: as many as are resident (a thread has up to 64 registers forwards, 80 backwards, 128
-// backwards with a residual).
+// backwards with a residual or dh).
 // Backwards their column sums are added up afterwards.
 static uint32_t norm_ctas(const fesc_clear_norm_desc* desc, const NormShape& s, bool backward, bool residual) {
     const uint64_t all = (desc->rows + s.teams - 1) / s.teams;
@@ -415,9 +416,10 @@ extern "C" int fesc_clear_norm_backward(const fesc_clear_norm_desc* desc, const 
              norm_wide(desc, d_gamma, 0, 4) && norm_wide(desc, d_scale, 0, 4);
     const NormShape s = norm_shape(desc);
     a.team_warps = s.warps;
-    const uint32_t ctas = norm_ctas(desc, s, true, d_residual);
+    const bool both = d_residual || d_dh;
+    const uint32_t ctas = norm_ctas(desc, s, true, both);
     auto kernel = by_type(desc->type, [&](auto t) {
-        return s.warps > NORM_WARPS ? norm_backward_kernel<decltype(t), 1024>(d_gate, d_residual) : norm_backward_kernel<decltype(t), 256>(d_gate, d_residual);
+        return s.warps > NORM_WARPS ? norm_backward_kernel<decltype(t), 1024>(d_gate, both) : norm_backward_kernel<decltype(t), 256>(d_gate, both);
     });
     CLEAR_CUDA(launch(kernel, dim3(ctas, desc->groups), dim3(s.teams * s.warps * 32), 0, st, a));
     CLEAR_CUDA(launch(k_clear_norm_columns, dim3((desc->d + 31) / 32, d_dscale ? 2 : 1), dim3(1024), 0, st, (const float*)a.part, d_dgamma, d_dscale, ctas, desc->d));

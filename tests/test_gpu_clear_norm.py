@@ -126,6 +126,40 @@ def test_rows_of_zeros_and_extreme_gates():
     assert off(o["residual"][0], want["residual"][0], 2.0 ** -18 * want["residual"][0].abs() + 1e-3, F32) <= 0
 
 
+@pytest.mark.parametrize("rows, d, groups, t, gate", [(5, 770, 2, "fp32", 1), (40, 1536, 1, "bf16", 1), (7, 2050, 1, "fp16", 0), (3, 8192, 1, "bf16", 1)])
+def test_the_gradient_of_h_without_a_residual(rows, d, groups, t, gate):
+    s = inputs(rows, d, t, gate, 0, 0, d)
+    s["dh"] = inputs(rows, d, t, 0, 1, 0, d + 1)["dh"]
+    n, h = forward(s, groups)
+    o = backward(s, groups)
+    wn, wh, grads = reference(s, groups)
+    # as in check(), with the magnitude of dh
+    u = 2.0 ** -18
+    sig = 1 / (1 + torch.exp(-wide(s["gate"]))) if gate else 1
+    slope = wide(s["gate"]).abs() * sig if gate else 1
+    hm = wide(s["y"]).abs() * slope
+    spread = lambda m: m.expand(rows, groups, d // groups).reshape(rows, d)  # noqa: E731
+    rho = 1 / torch.sqrt(wh.reshape(rows, groups, -1).square().mean(2, keepdim=True) + EPS)
+    w = wide(s["gamma"]).abs() * wide(s["dn"]).abs()
+    part = spread(rho ** 2 * (hm * hm).reshape(rows, groups, -1).mean(2, keepdim=True))
+    dt = (spread(rho) * w + hm * spread(rho ** 3 * (w * hm).reshape(rows, groups, -1).mean(2, keepdim=True))) * (2 + part) + wide(s["dh"]).abs()
+    T = s["y"].dtype
+    assert off(o["y"], grads["y"], u * dt * slope, T) <= 0
+    if gate:
+        assert off(o["gate"], grads["gate"], u * dt * wide(s["y"]).abs() * sig * (1 + wide(s["gate"]).abs() * (1 - sig)), T) <= 0
+    assert off(o["gamma"], grads["gamma"], (2 * u * wide(s["dn"]).abs() * hm * spread(rho) * (2 + part)).sum(0), F32) <= 0
+
+
+def test_a_row_of_zeros_with_a_tiny_eps():
+    y, dn = torch.randn((3, 64), device="cuda"), torch.randn((3, 64), device="cuda")
+    y[1] = 0
+    gamma, dy, dgamma = torch.ones(64, device="cuda"), torch.full((3, 64), 7.0, device="cuda"), torch.empty(64, device="cuda")
+    fesc.clear_norm_backward(y, gamma, dn, dy, dgamma, 1e-30)        # 1 / sqrt(eps) = 1e15, its cube is beyond float32
+    assert torch.isfinite(dy).all() and torch.isfinite(dgamma).all()
+    want = dn[1].double() / torch.tensor(1e-30, dtype=torch.float32).double().sqrt().item()
+    assert off(dy[1], want, 2.0 ** -20 * want.abs(), F32) <= 0
+
+
 def test_streams_graphs_and_the_same_bits_again():
     s = inputs(3000, 768, "bf16", 1, 1, 1, 5)
     n, h = forward(s)
