@@ -435,7 +435,7 @@ extern "C" int fesc_clear_scan(const fesc_clear_scan_desc* desc, const void* d_x
         !scan_strides(d.C, d.batch, d.L, d.G, d.N, false) || !scan_strides(d.y, d.batch, d.L, d.H, d.P, true))
         return clear_fail(FESC_EINVAL, "clear_scan: a stride is negative or beyond 2^40, or elements of y overlap");
     if (d.L && (!d_x || !d_g || !d_B || !d_C || !d_y)) return clear_fail(FESC_EINVAL, "clear_scan: x, g, B, C and y have to be given");
-    if (same_buffer(d_y, d_x) || same_buffer(d_y, d_B) || same_buffer(d_y, d_C) || same_buffer(d_h_out, d_h0))
+    if (same_buffer(d_y, d_x) || same_buffer(d_y, d_g) || same_buffer(d_y, d_B) || same_buffer(d_y, d_C) || same_buffer(d_h_out, d_h0))
         return clear_fail(FESC_EINVAL, "clear_scan: an output is an input");
     const ScanShape s = scan_shape(desc, false);
     const size_t need = fesc_clear_scan_work(desc);
@@ -557,7 +557,8 @@ extern "C" int fesc_clear_scan_step(const fesc_clear_scan_desc* desc, const void
     if (!scan_strides(d.x, d.batch, 1, d.H, d.P, false) || !scan_strides(d.g, d.batch, 1, d.H, 1, false) || !scan_strides(d.B, d.batch, 1, d.G, d.N, false) ||
         !scan_strides(d.C, d.batch, 1, d.G, d.N, false) || !scan_strides(d.y, d.batch, 1, d.H, d.P, true))
         return clear_fail(FESC_EINVAL, "clear_scan_step: a stride is negative or beyond 2^40, or elements of y overlap");
-    if (same_buffer(d_y, d_x) || same_buffer(d_y, d_B) || same_buffer(d_y, d_C)) return clear_fail(FESC_EINVAL, "clear_scan_step: y is an input");
+    if (same_buffer(d_y, d_x) || same_buffer(d_y, d_g) || same_buffer(d_y, d_B) || same_buffer(d_y, d_C))
+        return clear_fail(FESC_EINVAL, "clear_scan_step: y is an input");
     if ((uint64_t)d.batch * d.H >= (1ull << 31)) return clear_fail(FESC_EINVAL, "clear_scan_step: too many sequences and heads for one call");
     StepArgs a = {d_x, d_B, d_C, d_g, d_skip, d_state, d_state_out, d_y, d.x[0], d.x[2], d.B[0], d.B[2], d.C[0], d.C[2], d.g[0], d.g[2], d.y[0], d.y[2],
                   d.H, d.P, d.N, d.G};

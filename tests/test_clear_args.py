@@ -69,6 +69,13 @@ def test_scan_refuses_buffers():
     assert fesc.lib().fesc_clear_scan(None, *[None] * 10, 0, None) == fesc.EINVAL
 
 
+def test_scan_refuses_log_decays_as_an_output():
+    d = scan_desc(type=2)
+    refused(scan(d, y=A[1]), "output is an input")
+    refused(scan_backward(d, dg=A[1]), "output is an input")
+    refused(fesc.lib().fesc_clear_scan_step(d, A[0], A[1], A[2], A[3], None, A[4], A[5], A[1], None), "y is an input")
+
+
 def test_calls_without_work_succeed_without_a_gpu():
     assert scan(scan_desc(batch=0)) == fesc.OK
     assert fesc.lib().fesc_clear_scan_step(scan_desc(batch=0), *[None] * 9) == fesc.OK
