@@ -6,7 +6,7 @@
 // group of channels needs form a team (3 for 768 channels, 6 for 1536), sums go through shuffles and one exchange in shared memory, and what
 // depends on them is written from the registers.  Rows are dealt out to the CTAs that are resident, and the next row's loads are under way while a
 // row is computed.  Bound by memory forwards (32768 x 768 with residual: 201 MB in 35 us, 0.89 of the copy rate); the gate's backward pass issues some 40
-// instructions per channel and is bound by that and by one exchange per row (16384 x 1536: 252 MB in 63 us).
+// instructions per channel and is bound by that and by one exchange per row (16384 x 1536: 252 MB in 61 us).
 // The gradients of gamma and s are sums over rows: a CTA adds up its own rows in a fixed order, a second kernel adds up the CTAs, so the
 // results do not depend on the order in which CTAs run.
 #define FESC_DBG_FILE 16   // file id in the sites a debug build reports

@@ -353,6 +353,8 @@ def test_step_reads_no_length():
     d.x[:], d.y[:], d.g[:], d.B[:], d.C[:] = (0, 0, 0), (0, 0, 0), (0, 0, 0), (0, 0, 0), (0, 0, 0)
     z = {k: torch.ones(n, device="cuda") for k, n in (("x", 8), ("g", 1), ("B", 8), ("C", 8), ("h", 64), ("y", 8))}
     p = {k: v.data_ptr() for k, v in z.items()}
+    for v in z.values() if fesc.debug_bounds() else ():       # the binding does it elsewhere
+        fesc.lib().fesc_debug_bounds_register(v.data_ptr(), v.numel() * 4)
     assert fesc.lib().fesc_clear_scan_step(d, p["x"], p["g"], p["B"], p["C"], None, p["h"], p["h"], p["y"], fesc._stream()) == fesc.OK
     torch.cuda.synchronize()
     assert torch.allclose(z["h"], torch.full_like(z["h"], 2.718281828 + 1), rtol=1e-6)
