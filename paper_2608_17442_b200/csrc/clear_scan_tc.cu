@@ -346,13 +346,15 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
             pb = scan_row<T>(ob, b, t_first + dir * (int)r0, head, group, tile) + col, pn = scan_row<T>(on, b, t_first + dir * (int)r0, head, group, tile) + col;
             if (MODE) pq = scan_row<T>(a.q, b, t_first + dir * (int)r0, head, group, tile) + col;
         }
-        // panels first .. first + n - 1 of a chunk; what does not exist is not read: zero bytes of an address that does
+        // Panels first .. first + n - 1 of a chunk.  What does not exist is not read: zero bytes are copied from the start of an operand, which lies on
+        // 16 bytes, as the source of a copy of 16 has to however few of them are read (g may lie on four).
+        const T* const none = (const T*)ob.p;
         auto copy = [&](uint32_t first, int n, const T* src, long long step, int width, int valid) {
 #pragma unroll 1
             for (int j = 0; j < n; j++, src += 64, width -= 64) {
                 const int bytes = min(max(width - (int)col, 0), 8) * 2;
                 const uint32_t dst = to + (first + j) * PANEL;
-                const T* p = bytes ? src : (const T*)a.g;
+                const T* p = bytes ? src : none;
                 const long long by = bytes ? step : 0;
                 if (valid == TC_Q) {
 #pragma unroll 8
@@ -361,7 +363,7 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
 #pragma unroll 1
                     for (uint32_t i = 0; i < TC_Q / 8; i++, p += by) {
                         const int some = (int)(r0 + 8 * i) < valid ? bytes : 0;
-                        cp_async16_part(dst + 1024 * i, some ? p : (const T*)a.g, some);
+                        cp_async16_part(dst + 1024 * i, some ? p : none, some);
                     }
                 }
             }

@@ -1,0 +1,32 @@
+"""The cleartext operators at the edges of what they promise: addresses, dropped states, buffers of autograd, waits that run out."""
+import pytest
+import torch
+
+import paper_2608_17442_b200 as fesc
+from clear_ref import make
+from test_gpu_clear_scan import backward, case, check_backward, check_forward, forward
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("c", [case(2, 131, 2, 40, 24, 2, "bf16", True), case(3, 300, 3, 72, 128, 1, "bf16", True, [300, 129, 1]), case(1, 70, 3, 64, 64, 1, "bf16"),
+                               case(2, 200, 1, 33, 127, 1, "bf16", True), case(2, 90, 3, 40, 72, 1, "fp16", True), case(1, 131, 2, 64, 128, 1, "fp32", True)],
+                         ids=lambda c: "-".join(str(v) for v in c.values()).replace(" ", ""))
+@pytest.mark.parametrize("shift", [1, 2, 3])
+def test_log_decays_at_any_address(c, shift):
+    """g and its gradient as a column range of a wider float32 buffer, on 4 or 8 bytes, where the other operands lie on 16."""
+    s = make(c, 30)
+    b, L, H = s["g"].shape
+    room = torch.full((b, L, H + 3 + shift), float("nan"), device="cuda")
+    g = room[..., shift:shift + H]
+    g.copy_(s["g"])
+    assert g.data_ptr() % 16 == 4 * shift
+    s["g"] = g
+    check_forward(s, c, *forward(s))
+    o = backward(s)
+    room_out = torch.full((b, L, H + 3 + shift), 7.0, device="cuda")
+    dg = room_out[..., shift:shift + H]
+    rest = {k: torch.empty_like(o[k]) for k in ("x", "B", "C")}
+    fesc.clear_scan_backward(s["x"], g, s["B"], s["C"], s["dy"], rest["x"], dg, rest["B"], rest["C"], skip=s["skip"], h0=s["h0"], dh_out=s["dh_out"], lengths=s["lengths"])
+    assert torch.equal(dg, o["g"]) and (room_out[..., :shift] == 7.0).all() and (room_out[..., shift + H:] == 7.0).all()
+    check_backward(s, c, o)
