@@ -512,8 +512,8 @@ enum { FESC_BF16 = 0, FESC_F16 = 1, FESC_F32 = 2 };
 const char* fesc_clear_last_error(void);
 /* Wait for `stream`; FESC_ETIMEOUT if a kernel's bounded wait gave up since the last such call on this device (its results are worth nothing). */
 int fesc_clear_sync(void* stream);
-/* Self-test of these waits: a warp waits on a barrier that nothing completes, until the wait gives up (about a second); the next fesc_clear_sync
- * returns FESC_ETIMEOUT.  Nothing faults, traps or hangs. */
+/* Self-test of these waits: a warp waits twice on a barrier that nothing completes, as a kernel does under way and before its end, until the waits give
+ * up (about two seconds); the next fesc_clear_sync returns FESC_ETIMEOUT, and its text says both.  Nothing faults, traps or hangs. */
 int fesc_clear_selftest_wait_limit(void* stream);
 
 /*

@@ -45,7 +45,7 @@ struct TcLayout {
     static constexpr size_t bytes = (size_t)panels * PANEL + 1024;  // panels start on 1024 bytes
 };
 
-static __device__ uint32_t g_clear_status;      // not 0: a bounded wait gave up
+static __device__ uint32_t g_clear_status[2];   // not 0: a bounded wait gave up; products were still under way at a kernel's end
 
 // what the decays' warp leaves for a chunk
 struct alignas(16) TcDecays {      // read four words at a time
@@ -62,15 +62,22 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// The longer part of a wait, out of line: the kernel has some thirty of them, and its instructions have to stay in the cache of one SM.
-static __device__ __noinline__ void wait_on(uint32_t bar, uint32_t parity, volatile uint32_t* dead) {
-    if (*dead) return;
+__device__ __forceinline__ bool poll(uint32_t bar, uint32_t parity) {
 #pragma unroll 1
     for (uint32_t it = 0; it < (1u << 18); it++) {      // about a second; a chunk takes microseconds
-        if (mbar_try_wait(bar, parity)) return;
+        if (mbar_try_wait(bar, parity)) return true;
         if (it > 64) __nanosleep(64);
     }
-    *dead = 1, g_clear_status = 1;
+    return false;
+}
+// The longer part of a wait, out of line: the kernel has some thirty of them, and its instructions have to stay in the cache of one SM.
+static __device__ __noinline__ void wait_on(uint32_t bar, uint32_t parity, volatile uint32_t* dead) {
+    if (*dead || poll(bar, parity)) return;
+    *dead = 1, g_clear_status[0] = 1;
+}
+// The last wait, for the products under way, before tensor memory is given back: also after another one gave up.
+static __device__ __noinline__ void drain(uint32_t bar) {
+    if (!poll(bar, 0)) g_clear_status[1] = 1;
 }
 // bytes of (row, 16-byte chunk c of eight) in a panel
 __device__ __forceinline__ uint32_t panel_at(uint32_t row, uint32_t c) { return row * 128 + ((c ^ (row & 7)) << 4); }
@@ -293,7 +300,7 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                 for (int c = 0; c < chunks; c++) chunk(c, c & 1);
             }
             tc_commit(drained);
-            mbar_wait_bounded(drained, 0);
+            drain(drained);
         }
         __syncwarp();
     } else if (warp == TC_WARPS + 1) {
@@ -773,7 +780,8 @@ cudaError_t scan_tc_pack(const TcPack& a, uint32_t batch, cudaStream_t st) {
     return a.L ? launch(k_clear_scan_pack, dim3((a.L + 7) / 8, batch, a.count), dim3(256), 0, st, a) : cudaSuccess;
 }
 
-// One warp waits on a barrier that nothing completes; the wait runs out, the kernel records it and returns.
+// One warp waits on a barrier that nothing completes, as a sweep does under way and as it does at its end; the waits run out, the kernel records
+// both and returns.
 __global__ void k_clear_wait_limit() {
     __shared__ __align__(8) u64 bar;
     __shared__ volatile uint32_t dead;
@@ -783,6 +791,7 @@ __global__ void k_clear_wait_limit() {
         mbar_init(at, 1);
         dead = 0;
         wait_on(at, 0, &dead);
+        drain(at);
     }
 }
 extern "C" int fesc_clear_selftest_wait_limit(void* stream) {
@@ -793,10 +802,11 @@ extern "C" int fesc_clear_selftest_wait_limit(void* stream) {
 extern "C" int fesc_clear_sync(void* stream) {
     CLEAR_CUDA(cudaStreamSynchronize((cudaStream_t)stream));
     CLEAR_CUDA(cudaGetLastError());
-    uint32_t status = 0;
-    CLEAR_CUDA(cudaMemcpyFromSymbol(&status, g_clear_status, sizeof(status)));
-    if (!status) return FESC_OK;
-    status = 0;
-    CLEAR_CUDA(cudaMemcpyToSymbol(g_clear_status, &status, sizeof(status)));
-    return clear_fail(FESC_ETIMEOUT, "a bounded wait on the tensor cores gave up");
+    uint32_t status[2] = {};
+    CLEAR_CUDA(cudaMemcpyFromSymbol(status, g_clear_status, sizeof(status)));
+    if (!status[0] && !status[1]) return FESC_OK;
+    const uint32_t none[2] = {};
+    CLEAR_CUDA(cudaMemcpyToSymbol(g_clear_status, none, sizeof(none)));
+    return clear_fail(FESC_ETIMEOUT, status[1] ? "a bounded wait on the tensor cores gave up, with products still under way at a kernel's end"
+                                               : "a bounded wait on the tensor cores gave up");
 }

@@ -30,3 +30,12 @@ def test_log_decays_at_any_address(c, shift):
     fesc.clear_scan_backward(s["x"], g, s["B"], s["C"], s["dy"], rest["x"], dg, rest["B"], rest["C"], skip=s["skip"], h0=s["h0"], dh_out=s["dh_out"], lengths=s["lengths"])
     assert torch.equal(dg, o["g"]) and (room_out[..., :shift] == 7.0).all() and (room_out[..., shift + H:] == 7.0).all()
     check_backward(s, c, o)
+
+
+def test_a_wait_that_runs_out_at_a_kernels_end_is_reported_too():
+    fesc.clear_sync()
+    fesc.clear_selftest_wait_limit()
+    with pytest.raises(fesc.FescError, match="still under way") as e:
+        fesc.clear_sync()
+    assert e.value.code == fesc.ETIMEOUT
+    fesc.clear_sync()
