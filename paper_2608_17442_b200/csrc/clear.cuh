@@ -39,6 +39,8 @@ struct ClearType<float> {
     static __device__ __forceinline__ float to(float v) { return v; }
     static __device__ __forceinline__ float from(float v) { return v; }
 };
+// A decay of zero leaves nothing of a state, also of an infinite one or of NaN.
+__device__ __forceinline__ float decayed(float f, float v) { return f == 0.f ? 0.f : f * v; }
 static inline uint32_t clear_type_bytes(uint32_t type) { return type == FESC_F32 ? 4 : 2; }
 
 // two float32 numbers at a time

@@ -59,7 +59,8 @@ __global__ void __launch_bounds__(256) k_clear_combine(const Chain forwards, con
                 if (c + k < segments) {
                     const uint32_t at = backwards ? segments - 1 - c - k : c + k;
                     *reinterpret_cast<float4*>(s + (size_t)at * per_b) = make_float4(run[0], run[1], run[2], run[3]);
-                    run[0] = f[k] * run[0] + add[k].x, run[1] = f[k] * run[1] + add[k].y, run[2] = f[k] * run[2] + add[k].z, run[3] = f[k] * run[3] + add[k].w;
+                    run[0] = decayed(f[k], run[0]) + add[k].x, run[1] = decayed(f[k], run[1]) + add[k].y, run[2] = decayed(f[k], run[2]) + add[k].z,
+                    run[3] = decayed(f[k], run[3]) + add[k].w;
                 }
         }
         return;
@@ -70,7 +71,7 @@ __global__ void __launch_bounds__(256) k_clear_combine(const Chain forwards, con
         for (uint32_t e = 0; e < n; e++) {
             const float add = p[e];
             p[e] = run[e];
-            run[e] = decay[((size_t)b * segments + at) * H + ((uint32_t)i + e) / per_head] * run[e] + add;
+            run[e] = decayed(decay[((size_t)b * segments + at) * H + ((uint32_t)i + e) / per_head], run[e]) + add;
         }
     }
 }
@@ -144,6 +145,7 @@ __global__ void __launch_bounds__(THREADS) k_clear_scan_finish(const FinishArgs 
             total = 0.0;
             for (uint32_t w = 0; w < WARPS; w++) total += words[0][w];
             slope = (run + total - low) / (double)(hi - lo);
+            if (!(fabs(slope) < 1e300)) slope = 0.0;      // an infinity or NaN stays with the tokens that it reaches
         }
         __syncthreads();
         double next = 0.0;
@@ -262,8 +264,7 @@ __global__ void __launch_bounds__(256) k_clear_scan_step(const StepArgs a) {
         float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-            // a decay of zero drops what the state holds, also infinities
-            h[r][e] = (keep > 0.f || keep != keep ? keep * h[r][e] : 0.f) + xv[r] * vB[e];
+            h[r][e] = decayed(keep, h[r][e]) + xv[r] * vB[e];
             sum += h[r][e] * vC[e];        // B and C are zero beyond the columns
         }
         if (WIDE) {

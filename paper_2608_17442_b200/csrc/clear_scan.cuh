@@ -421,7 +421,9 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
             for (int n = 0; n < 8; n++) {
                 const float2 e = *reinterpret_cast<const float2*>(grow + 8 * n + 2 * q4);
 #pragma unroll
-                for (int m = 0; m < MT; m++) acc[m][n][0] *= e.x, acc[m][n][1] *= e.y, acc[m][n][2] *= e.x, acc[m][n][3] *= e.y;
+                for (int m = 0; m < MT; m++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) acc[m][n][i] = decayed(i & 1 ? e.y : e.x, acc[m][n][i]);
             }
         }
         // state <- G_last state + (fade v)^T k
@@ -432,7 +434,7 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
 #pragma unroll
                 for (int n = 0; n < KT; n++)
 #pragma unroll
-                    for (int e = 0; e < 4; e++) st[m][n][e] *= keep;
+                    for (int e = 0; e < 4; e++) st[m][n][e] = decayed(keep, st[m][n][e]);
         }
 #pragma unroll 1
         for (int kk = 0; kk < SCAN_Q / 16; kk++) {
@@ -558,7 +560,7 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
 #pragma unroll
             for (int n = 0; n < KT; n++)
 #pragma unroll
-                for (int e = 0; e < 4; e++) state_word(m, n, e) = st[m][n][e] * f;
+                for (int e = 0; e < 4; e++) state_word(m, n, e) = decayed(f, st[m][n][e]);
         __syncthreads();
 #pragma unroll 4
         for (int i = tid; i < pw * (int)a.N; i += THREADS) last[i] = sh[i / a.N * S::H_STR + i % a.N];
@@ -578,7 +580,7 @@ __device__ __forceinline__ void sweep(const ScanArgs& a, uint32_t block) {
 #pragma unroll
                     for (int e = 0; e < 4; e++) sum += st[m][n][e] * state_word(m, n, e);
             const int next = a.backwards ? 0 : t_hi;
-            if (next < length) sum *= expf(a.g[b * a.gb + next * a.gt + head * a.gh]);
+            if (next < length) sum = decayed(expf(a.g[b * a.gb + next * a.gt + head * a.gh]), sum);
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o), diag += __shfl_xor_sync(~0u, diag, o);

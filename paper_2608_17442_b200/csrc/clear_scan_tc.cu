@@ -526,6 +526,10 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
 #pragma unroll
                 for (int p = 0; p < (int)Lay::H_PARTS; p++) tc_ld16(x[p], lanes + Lay::H + Lay::H_SET * set + 64 * p + 16 * part);
                 tc_wait_ld();
+                if (keep == 0.f) {         // also an infinite state is dropped
+#pragma unroll
+                    for (int e = 0; e < 8; e++) st[e] = {0.f, 0.f};
+                }
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
                     auto pair = [&](int p) { return f2{__uint_as_float(x[p][2 * e]), __uint_as_float(x[p][2 * e + 1])}; };
@@ -563,6 +567,10 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                 tc_wait_ld();
                 tc_before();
                 arrive(b_used + 8 * set);
+                if (grow == 0.f) {
+#pragma unroll
+                    for (int e = 0; e < 16; e++) x[e] = x1[e] = 0;
+                }
                 T* out = (T*)a.out + b * a.ob + t * a.ot + head * a.oh + tile * SCAN_TILE + 16 * part;
                 const int count = live ? vw - 16 * (int)part : 0;
                 uint32_t o[8];
@@ -598,6 +606,10 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                         tc_before();
                         arrive(b_used + 8 * set);
                     }
+                    if (grow == 0.f) {
+#pragma unroll
+                        for (int e = 0; e < 16; e++) x[e] = 0;
+                    }
 #pragma unroll
                     for (int e = 0; e < 8; e++) {
                         const f2 v = fma2({grow, grow}, {__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])}, {__uint_as_float(y[2 * e]), __uint_as_float(y[2 * e + 1])});
@@ -613,7 +625,7 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
 #pragma unroll
             for (int i = 0; i < 16; i++) {
                 const int p = 16 * part + i;
-                if (p < pw && row < a.N) last[(size_t)p * a.N + row] = (i & 1 ? st[i / 2].y : st[i / 2].x) * f;
+                if (p < pw && row < a.N) last[(size_t)p * a.N + row] = decayed(f, i & 1 ? st[i / 2].y : st[i / 2].x);
             }
         }
         if (Lay::GRAD && a.ends) {
@@ -626,7 +638,7 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                     if (p < pw && row < a.N) sum += (i & 1 ? st[i / 2].y : st[i / 2].x) * meet[(size_t)p * a.N + row];
                 }
                 const int next = a.backwards ? 0 : t_hi;
-                if (next < length) sum *= expf(a.g[b * a.gb + next * a.gt + head * a.gh]);
+                if (next < length) sum = decayed(expf(a.g[b * a.gb + next * a.gt + head * a.gh]), sum);
             }
 #pragma unroll
             for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o), diag += __shfl_xor_sync(~0u, diag, o);

@@ -39,3 +39,43 @@ def test_a_wait_that_runs_out_at_a_kernels_end_is_reported_too():
         fesc.clear_sync()
     assert e.value.code == fesc.ETIMEOUT
     fesc.clear_sync()
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("L, drop, P, N", [(1, 0, 64, 128), (40, 17, 40, 24), (300, 150, 64, 128), (1500, 700, 40, 72), (1500, 1024, 64, 128)])
+def test_a_dropped_state_leaves_nothing_behind_also_an_infinite_one(L, drop, P, N, t):
+    """A log decay of -inf between infinities and finite tokens: what lies on the far side is what it is without them, bit for bit."""
+    s = make(case(2, L, 2, P, N, 1, t, True), 31)
+    s["g"][:, drop] = -float("inf")
+    y, h = forward(s)
+    o = backward(s)
+    # states before the drop: outputs and gradients from the drop on
+    lost = dict(s, h0=s["h0"].clone())
+    lost["h0"][:, 0], lost["h0"][0, 1] = float("inf"), float("nan")
+    y2, h2 = forward(lost)
+    o2 = backward(lost)
+    assert torch.isfinite(h).all() and torch.equal(h, h2) and torch.equal(y[:, drop:], y2[:, drop:])
+    for k in ("g", "C"):
+        assert torch.equal(o[k][:, drop:], o2[k][:, drop:]), k
+    for k in ("x", "B", "skip", "h0"):
+        assert torch.equal(o[k], o2[k]), k
+    # gradients of the state behind the drop: gradients before it
+    lost = dict(s, dh_out=s["dh_out"].clone())
+    lost["dh_out"][:, 1], lost["dh_out"][1, 0] = -float("inf"), float("nan")
+    o2 = backward(lost)
+    for k in ("x", "B", "g"):
+        assert torch.equal(o[k][:, :drop], o2[k][:, :drop]), k
+    for k in ("C", "skip", "h0"):
+        assert torch.equal(o[k], o2[k]), k
+    assert (o2["g"][:, drop] == 0).all()
+
+
+def test_one_token_and_a_scan_of_one_token_drop_alike():
+    s = make(case(3, 1, 2, 40, 24, 1, "fp32", True), 32)
+    s["g"][0], s["g"][1] = -float("inf"), -150.0          # both are decays of zero in float32
+    s["h0"][:2] = float("inf")
+    y, h = forward(s)
+    y1, h1 = torch.empty_like(s["x"][:, 0]), torch.empty_like(h)
+    fesc.clear_scan_step(s["x"][:, 0], s["g"][:, 0], s["B"][:, 0], s["C"][:, 0], s["h0"], y1, skip=s["skip"], state_out=h1)
+    assert all(torch.isfinite(v).all() for v in (y, h, y1, h1))
+    assert (h[:2] - h1[:2]).abs().max() <= 2.0 ** -20 * h1[:2].abs().max()      # one product each
