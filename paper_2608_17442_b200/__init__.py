@@ -382,7 +382,8 @@ class Context:
 # ---- operators on cleartext activations (no context; see include/fesc.h) ----------------------------------------------------
 # Tensors may be views with strides whose innermost dimension is contiguous (column ranges of a projection's output).  Calls run on the
 # current stream of the tensors' device.  `work` is a uint8 CUDA tensor of at least the *_work bytes; without one the call takes its
-# workspace from torch's allocator.
+# workspace from torch's allocator.  Autograd does not record these calls: outputs carry no graph, also where an input requires a gradient (the
+# *_backward calls are the gradients, for the backward pass of a torch.autograd.Function), and what a call writes counts as changed in place.
 #
 # Tensors are checked and handed over by binding/clear.cpp (_clear.so): from Python that takes longer than a token's step.
 

@@ -7,6 +7,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <initializer_list>
 #include <string>
 
 #include "fesc.h"
@@ -103,6 +104,14 @@ struct Call {
         if (lib.debug_register && w.bytes) lib.debug_register(w.p, w.bytes);
         return w;
     }
+    // what the call has written counts as changed in place: autograd refuses gradients that would need the values before
+    void wrote(std::initializer_list<PyObject*> list) const {
+        for (PyObject* o : list)
+            if (o != Py_None) {
+                const at::Tensor& t = THPVariable_Unpack(o);
+                if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+            }
+    }
     void* stream() const { return c10::cuda::getCurrentCUDAStream(device).stream(); }
     void done(int rc) const {
         if (rc != FESC_OK) throw Refused{rc, lib.last_error()};
@@ -164,6 +173,7 @@ PyObject* clear_scan(PyObject*, PyObject* const* args, Py_ssize_t n) {      // x
         steps(s.d.x, a[0], true), steps(s.d.y, a[4], true), steps(s.d.g, a[1], true), steps(s.d.B, a[2], true), steps(s.d.C, a[3], true);
         const Call::Work w = c.work(a[9], lib.scan_work(&s.d));
         c.done(lib.scan(&s.d, x, g, B, C, skip, h0, len, y, h, w.p, w.bytes, c.stream()));
+        c.wrote({a[4], a[7], a[9]});
     });
 }
 
@@ -182,6 +192,7 @@ PyObject* clear_scan_backward(PyObject*, PyObject* const* args, Py_ssize_t n) { 
         steps(s.d.dx, a[5], true), steps(s.d.dg, a[6], true), steps(s.d.dB, a[7], true), steps(s.d.dC, a[8], true);
         const Call::Work w = c.work(a[15], lib.scan_backward_work(&s.d));
         c.done(lib.scan_backward(&s.d, x, g, B, C, skip, h0, len, dy, dh, dx, dg, dB, dC, dskip, dh0, w.p, w.bytes, c.stream()));
+        c.wrote({a[5], a[6], a[7], a[8], a[10], a[13], a[15]});
     });
 }
 
@@ -196,6 +207,7 @@ PyObject* clear_scan_step(PyObject*, PyObject* const* args, Py_ssize_t n) {     
               *to = a[7] == Py_None ? h : c.f32("state_out", a[7], st);
         steps(s.d.x, a[0], false), steps(s.d.y, a[5], false), steps(s.d.g, a[1], false), steps(s.d.B, a[2], false), steps(s.d.C, a[3], false);
         c.done(lib.scan_step(&s.d, x, g, B, C, skip, h, to, y, c.stream()));
+        c.wrote({a[5], a[7] == Py_None ? a[4] : a[7]});
     });
 }
 
@@ -233,6 +245,7 @@ PyObject* clear_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {      // y
         float *gamma = c.f32("gamma", a[1], d), *scale = c.f32("scale", a[6], d);
         s.d.y_stride = step(a[0]), s.d.n_stride = step(a[2]), s.d.gate_stride = step(a[4]), s.d.residual_stride = step(a[5]), s.d.h_stride = step(a[7]);
         c.done(lib.norm(&s.d, y, gamma, z, r, scale, out, h, c.stream()));
+        c.wrote({a[2], a[7]});
     });
 }
 
@@ -249,6 +262,7 @@ PyObject* clear_norm_backward(PyObject*, PyObject* const* args, Py_ssize_t n) { 
         s.d.residual_stride = step(a[8]), s.d.dresidual_stride = step(a[9]), s.d.dh_stride = step(a[12]);
         const Call::Work w = c.work(a[14], lib.norm_backward_work(&s.d));
         c.done(lib.norm_backward(&s.d, y, gamma, z, r, scale, dn, dh, dy, dgamma, dz, dr, dscale, w.p, w.bytes, c.stream()));
+        c.wrote({a[3], a[4], a[7], a[9], a[11], a[14]});
     });
 }
 

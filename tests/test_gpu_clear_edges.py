@@ -79,3 +79,37 @@ def test_one_token_and_a_scan_of_one_token_drop_alike():
     fesc.clear_scan_step(s["x"][:, 0], s["g"][:, 0], s["B"][:, 0], s["C"][:, 0], s["h0"], y1, skip=s["skip"], state_out=h1)
     assert all(torch.isfinite(v).all() for v in (y, h, y1, h1))
     assert (h[:2] - h1[:2]).abs().max() <= 2.0 ** -20 * h1[:2].abs().max()      # one product each
+
+
+def test_what_a_call_writes_counts_as_changed_in_place():
+    s = make(case(1, 70, 2, 40, 24, 1, "bf16", True), 33)
+    f = {"device": "cuda", "dtype": torch.float32}
+
+    def written(call, *outputs):
+        before = [t._version for t in outputs]
+        call()
+        assert all(t._version > v for t, v in zip(outputs, before))
+
+    y, h = torch.empty_like(s["x"]), torch.empty_like(s["h0"])
+    written(lambda: fesc.clear_scan(s["x"], s["g"], s["B"], s["C"], y, h_out=h), y, h)
+    o = [torch.empty_like(s[k]) for k in ("x", "g", "B", "C", "skip", "h0")]
+    written(lambda: fesc.clear_scan_backward(s["x"], s["g"], s["B"], s["C"], s["dy"], *o[:4], skip=s["skip"], dskip=o[4], h0=s["h0"], dh0=o[5]), *o)
+    token = [s[k][:, 0] for k in ("x", "g", "B", "C")]
+    written(lambda: fesc.clear_scan_step(*token, h, y[:, 0]), h, y)            # in place; a view counts for its base
+    other = torch.empty_like(h)
+    left = h._version
+    written(lambda: fesc.clear_scan_step(*token, h, y[:, 0], state_out=other), other, y)
+    assert h._version == left and s["x"]._version == 0
+    rows, gamma = torch.randn((6, 48), **f), torch.randn(48, **f)
+    n, hh = torch.empty_like(rows), torch.empty_like(rows)
+    written(lambda: fesc.clear_norm(rows, gamma, n, 1e-5, h=hh), n, hh)
+    d = [torch.empty_like(t) for t in (rows, gamma, rows, rows, gamma)]
+    written(lambda: fesc.clear_norm_backward(rows, gamma, n, d[0], d[1], 1e-5, gate=hh, dgate=d[2], residual=rows, dresidual=d[3], scale=gamma, dscale=d[4]), *d)
+    # autograd notices: the values that this product's gradient needs are gone
+    w = torch.ones((6, 48), **f, requires_grad=True)
+    total = (w * n).sum()
+    fesc.clear_norm(rows, gamma, n, 1e-5)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        total.backward()
+    with torch.inference_mode():
+        fesc.clear_norm(rows, gamma, torch.empty_like(rows), 1e-5)
