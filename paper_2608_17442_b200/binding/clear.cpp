@@ -155,6 +155,11 @@ PyObject* run(PyObject* const* args, Py_ssize_t n, Py_ssize_t count, F body) {
     } catch (const Refused& r) {
         PyObject* e = PyObject_CallFunction(error_class, "is", r.code, r.what.c_str());
         if (e) PyErr_SetObject(error_class, e), Py_DECREF(e);
+    } catch (const c10::OutOfMemoryError& e) {      // of the workspace
+        PyObject* torch = PyImport_ImportModule("torch");
+        PyObject* type = torch ? PyObject_GetAttrString(torch, "OutOfMemoryError") : nullptr;
+        if (type) PyErr_SetString(type, e.what_without_backtrace());
+        Py_XDECREF(type), Py_XDECREF(torch);
     } catch (const std::exception& e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
     }

@@ -113,3 +113,12 @@ def test_what_a_call_writes_counts_as_changed_in_place():
         total.backward()
     with torch.inference_mode():
         fesc.clear_norm(rows, gamma, torch.empty_like(rows), 1e-5)
+
+
+def test_a_workspace_that_does_not_fit_is_torchs_own_error():
+    """64 x 2^20 tokens of four heads, all of them the same one in memory: the partial sums alone would take 256 GB."""
+    x, g, B = (torch.zeros((1, 1, 1, *n), device="cuda").expand(64, 1 << 20, h, *n) for n, h in (((64,), 4), ((), 4), ((128,), 1)))
+    with pytest.raises(torch.cuda.OutOfMemoryError):
+        fesc.clear_scan_backward(x, g, B, B, x, x, g, B, B)
+    with pytest.raises(fesc.FescError, match="overlap"):          # with a workspace the call is refused: outputs of one token's memory
+        fesc.clear_scan_backward(x, g, B, B, x, x, g, B, B, work=torch.empty(256, dtype=torch.uint8, device="cuda"))
