@@ -43,11 +43,13 @@ __device__ __forceinline__ void team_sum(float& a, float& b, float2* words, uint
     }
 }
 
-// By the approximate exponential and reciprocal (2 units each; the exponent's rounding adds 2^-24 |z|): with the exact ones the backward pass of the
-// gate issues for as long as it moves bytes.
+// For 16-bit rows by the approximate exponential (2 units; its argument's rounding adds 2^-24 |z|): with the exact one the backward pass of the gate
+// issues for as long as it moves bytes.  Float32 rows would lose up to six bits by that (z = -80).  The reciprocal is off by one unit.
+template <class T>
 __device__ __forceinline__ float sigmoid(float z) {
     float e, s;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
+    if constexpr (sizeof(T) == 4) e = expf(-z);
+    else asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.f + e));
     return s;
 }
@@ -102,8 +104,12 @@ __device__ __forceinline__ size_t span8(int left, bool wide) {
     return left <= 0 ? 0 : wide ? 8 * sizeof(T) : (size_t)(min((left - 1) / 32, 7) * 32 + 1) * sizeof(T);
 }
 
+// CTAs of 256 threads on an SM.  Forwards a thread has 64 registers, for float32 rows with gate and residual 80 (16384 x 1536: 60 us, with 64 and what then
+// goes to local memory 85); backwards 80, with a residual, or for float32 rows with a gate, 128 (93 us, with 80 108).
+#define NORM_CTAS(BYTES, GATE, RESIDUAL) ((BYTES) == 4 && (GATE) && (RESIDUAL) ? 3 : 4)
+#define NORM_BACK_CTAS(BYTES, GATE, RESIDUAL) ((RESIDUAL) || ((BYTES) == 4 && (GATE)) ? 2 : 3)
 template <class T, bool GATE, bool RESIDUAL, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : 4) k_clear_norm(const NormArgs a) {
+__global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : NORM_CTAS(sizeof(T), GATE, RESIDUAL)) k_clear_norm(const NormArgs a) {
     __shared__ float2 words[2][32];
     pdl_begin();
     const uint32_t teams = (blockDim.x >> 5) / a.team_warps, team = (threadIdx.x >> 5) / a.team_warps, first = blockIdx.y * a.width;
@@ -135,7 +141,7 @@ __global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : 4) k_clear_norm(c
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             f2 v = y[e];
-            if (GATE) v = mul2(v, mul2(z[e], {sigmoid(z[e].x), sigmoid(z[e].y)}));
+            if (GATE) v = mul2(v, mul2(z[e], {sigmoid<T>(z[e].x), sigmoid<T>(z[e].y)}));
             if (RESIDUAL) v = a.scale ? fma2(s[e], v, r[e]) : add2(v, r[e]);
             h[e] = v, sums = fma2(v, v, sums);      // zeros behind the row's end
         }
@@ -158,7 +164,7 @@ __global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : 4) k_clear_norm(c
 // dy = dv silu(z);  dz = dv y sigma (1 + z (1 - sigma)) = dv y (sigma + silu(z) (1 - sigma));  dgamma = sum_rows dn h rho
 // RESIDUAL: a residual, dh, or both
 template <class T, bool GATE, bool RESIDUAL, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : RESIDUAL ? 2 : 3) k_clear_norm_backward(const NormArgs a) {
+__global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : NORM_BACK_CTAS(sizeof(T), GATE, RESIDUAL)) k_clear_norm_backward(const NormArgs a) {
     __shared__ float2 words[2][32];
     __shared__ float cols[NORM_WARPS * 256];
     pdl_begin();
@@ -195,7 +201,7 @@ __global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : RESIDUAL ? 2 : 3)
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             f2 v = y[e];
-            if (GATE) sig[e] = {sigmoid(z[e].x), sigmoid(z[e].y)}, v = mul2(v, mul2(z[e], sig[e]));
+            if (GATE) sig[e] = {sigmoid<T>(z[e].x), sigmoid<T>(z[e].y)}, v = mul2(v, mul2(z[e], sig[e]));
             if (RESIDUAL) v = a.scale ? fma2(s[e], v, r[e]) : add2(v, r[e]);
             h[e] = v;
             sums = fma2(v, v, sums), dots = fma2(mul2(g[e], w[e]), v, dots);
@@ -326,12 +332,10 @@ static auto by_type(uint32_t type, F f) {
     return type == FESC_BF16 ? f(__nv_bfloat16()) : type == FESC_F16 ? f(__half()) : f(float());
 }
 
-// CTAs per group of channels, to which rows are dealt out: as many as are resident (a thread has up to 64 registers forwards, 80 backwards, 128
-// backwards with a residual or dh).
-// Backwards their column sums are added up afterwards.
-static uint32_t norm_ctas(const fesc_clear_norm_desc* desc, const NormShape& s, bool backward, bool residual) {
+// CTAs per group of channels, to which rows are dealt out: as many as are resident, by the registers of a thread.  Backwards their column sums are added up afterwards.
+static uint32_t norm_ctas(const fesc_clear_norm_desc* desc, const NormShape& s, uint32_t registers) {
     const uint64_t all = (desc->rows + s.teams - 1) / s.teams;
-    const uint32_t threads = s.warps * s.teams * 32, resident = threads > 256 ? (threads > 512 ? 1 : 2) : 65536 / (threads * (!backward ? 64 : residual ? 128 : 80));
+    const uint32_t threads = s.warps * s.teams * 32, resident = threads > 256 ? (threads > 512 ? 1 : 2) : 65536 / (threads * registers);
     return all < 148 * resident ? (uint32_t)all : 148 * resident;
 }
 
@@ -362,14 +366,14 @@ extern "C" int fesc_clear_norm(const fesc_clear_norm_desc* desc, const void* d_y
     auto kernel = by_type(desc->type, [&](auto t) {
         return s.warps > NORM_WARPS ? norm_kernel<decltype(t), 1024>(d_gate, d_residual) : norm_kernel<decltype(t), 256>(d_gate, d_residual);
     });
-    CLEAR_CUDA(launch(kernel, dim3(norm_ctas(desc, s, false, d_residual), desc->groups), dim3(s.teams * s.warps * 32), 0, (cudaStream_t)stream, a));
+    CLEAR_CUDA(launch(kernel, dim3(norm_ctas(desc, s, NORM_CTAS(bytes, d_gate, d_residual) == 3 ? 80 : 64), desc->groups), dim3(s.teams * s.warps * 32), 0, (cudaStream_t)stream, a));
     return FESC_OK;
 }
 
 extern "C" size_t fesc_clear_norm_backward_work(const fesc_clear_norm_desc* desc) {
     const char* what;
     if (!desc || norm_check(desc, &what) != FESC_OK) return 0;
-    return (size_t)norm_ctas(desc, norm_shape(desc), true, false) * 2 * desc->d * sizeof(float);
+    return (size_t)norm_ctas(desc, norm_shape(desc), 80) * 2 * desc->d * sizeof(float);
 }
 
 extern "C" int fesc_clear_norm_backward(const fesc_clear_norm_desc* desc, const void* d_y, const float* d_gamma, const void* d_gate,
@@ -417,7 +421,7 @@ extern "C" int fesc_clear_norm_backward(const fesc_clear_norm_desc* desc, const 
     const NormShape s = norm_shape(desc);
     a.team_warps = s.warps;
     const bool both = d_residual || d_dh;
-    const uint32_t ctas = norm_ctas(desc, s, true, both);
+    const uint32_t ctas = norm_ctas(desc, s, NORM_BACK_CTAS(bytes, d_gate, both) == 2 ? 128 : 80);
     auto kernel = by_type(desc->type, [&](auto t) {
         return s.warps > NORM_WARPS ? norm_backward_kernel<decltype(t), 1024>(d_gate, both) : norm_backward_kernel<decltype(t), 256>(d_gate, both);
     });

@@ -122,3 +122,25 @@ def test_a_workspace_that_does_not_fit_is_torchs_own_error():
         fesc.clear_scan_backward(x, g, B, B, x, x, g, B, B)
     with pytest.raises(fesc.FescError, match="overlap"):          # with a workspace the call is refused: outputs of one token's memory
         fesc.clear_scan_backward(x, g, B, B, x, x, g, B, B, work=torch.empty(256, dtype=torch.uint8, device="cuda"))
+
+
+def test_the_gate_of_float32_rows_is_as_exact_as_float32():
+    """h = y z / (1 + exp(-z)) over the gate's range: the exponential and the reciprocal are off by one unit (2^-23) at most, the sum and the two products
+    by half a unit each: 3.5 x 2^-23 < 2^-21.  Backwards sigma (1 + z (1 - sigma)) as well, with 1 - sigma and the sum around it off by units of terms that do not exceed 1 + |z|."""
+    gen = torch.Generator(device="cuda").manual_seed(34)
+    d = 4096
+    z = (torch.rand((2, d), generator=gen, device="cuda") * 100 - 80)
+    y, dh = (torch.randn((2, d), generator=gen, device="cuda") for _ in range(2))
+    gamma, n, h = torch.ones(d, device="cuda"), torch.empty_like(y), torch.empty_like(y)
+    fesc.clear_norm(y, gamma, n, 1e-5, gate=z, h=h)
+    sig = 1 / (1 + torch.exp(-z.double()))
+    want = y.double() * z.double() * sig
+    assert ((h.double() - want).abs() <= 2.0 ** -21 * want.abs() + 2.0 ** -149).all()
+    # dn of zero: dy = dh silu(z), dz = dh y sigma (1 + z (1 - sigma))
+    dy, dgamma, dz = torch.empty_like(y), torch.empty_like(gamma), torch.empty_like(y)
+    fesc.clear_norm_backward(y, gamma, torch.zeros_like(y), dy, dgamma, 1e-5, gate=z, dgate=dz, dh=dh)
+    want = dh.double() * z.double() * sig
+    assert ((dy.double() - want).abs() <= 2.0 ** -21 * want.abs() + 2.0 ** -149).all()
+    want = dh.double() * y.double() * sig * (1 + z.double() * (1 - sig))
+    size = (dh.double() * y.double()).abs() * sig * (1 + z.double().abs())
+    assert ((dz.double() - want).abs() <= 2.0 ** -21 * size + 2.0 ** -149).all()
