@@ -303,17 +303,18 @@ static ScanShape scan_shape(const fesc_clear_scan_desc* d, bool backward) {
     s.tiles = (d->P + SCAN_TILE - 1) / SCAN_TILE, s.vheads = d->H * s.tiles, s.np = s.tc || d->N > 64 ? 128 : 64;
     const uint64_t pieces = ((uint64_t)d->L + 127) / 128, ctas = (uint64_t)d->batch * s.vheads, sweeps = backward ? 3 : 1;
     const double START = s.tc ? 2.0 : 0.5, CHAIN = s.tc ? 1.5 : 0.5, STATE = s.tc ? 0.35 : 0.5;
-    // CTAs of a sweep on an SM, by registers and shared memory
-    const uint64_t places = 148 * (s.tc ? 1 : d->type == FESC_BF16 ? (d->N > 64 ? 2 : 3) : d->type == FESC_F32 && d->N > 64 ? 1 : 2);
+    // CTAs on an SM, by registers and shared memory: of the state pass, of the sweeps (as their launch bounds have it)
+    const bool broad = d->N > 64;
+    const uint64_t of_state = 148 * (s.tc || (broad && d->type == FESC_F32) ? 1 : 2), places = broad && backward ? 148 : of_state;
     uint64_t each = pieces ? pieces : 1, last = 0;
     double least = 1e300;
     for (uint64_t want = 1; want <= pieces && want <= 1024; want++) {
         const uint64_t of = (pieces + want - 1) / want, segments = (pieces + of - 1) / of;
         if (segments == last) continue;
         last = segments;
-        auto rounds = [&](uint64_t n) { return (double)((n * ctas * segments + places - 1) / places); };
-        double time = rounds(sweeps) * (START + of);
-        if (segments > 1) time += rounds(backward ? 2 : 1) * (START + STATE * of) + CHAIN;
+        auto rounds = [&](uint64_t n, uint64_t at_once) { return (double)((n * ctas * segments + at_once - 1) / at_once); };
+        double time = rounds(sweeps, places) * (START + of);
+        if (segments > 1) time += rounds(backward ? 2 : 1, of_state) * (START + STATE * of) + CHAIN;
         if (time < least) each = of, least = time;
         if (ctas * segments > 8 * places) break;          // more only adds rounds
     }
