@@ -339,12 +339,12 @@ __device__ __forceinline__ void tc_sweep(const ScanArgs& a, uint32_t block, TcSh
                 d.grow[4 * lane + i] = ex2((float)v), d.fade[4 * lane + i] = ex2((float)(total - v)), d.tail[4 * lane + i] = ex2((float)(end - v));
             }
             if ((lane & 7) == 7) d.ref[lane >> 3] = make_float2((float)end, (float)(end - (float)end));
-            if (lane == 0) d.keep = ex2((float)total);
+            if (lane == 0) d.keep = exp2_near(total);
             through += total;
             __syncwarp();
             if (lane == 0) mbar_arrive(b_g + 8 * (c & 1));
         }
-        if (MODE == MODE_STATE && lane == 0 && tile == 0) a.decay[slot * a.H + head] = ex2((float)through) * ex2((float)(through - (float)through));
+        if (MODE == MODE_STATE && lane == 0 && tile == 0) a.decay[slot * a.H + head] = exp2_near(through);
     } else if (warp > TC_WARPS + 1) {
         // Copies.  A thread has one 16-byte chunk of every eighth row: its place in a panel moves by 1024 bytes from row to row.
         const uint32_t me = tid - 32 * (TC_WARPS + 2), r0 = me >> 3, col = (me & 7) * 8, to = base + panel_at(r0, me & 7);
