@@ -4,6 +4,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <type_traits>
 #include <utility>
 
@@ -17,7 +18,17 @@ int clear_fail(int code, const char* what);
         if (e_ != cudaSuccess) return clear_fail(FESC_ECUDA, cudaGetErrorString(e_)); \
     } while (0)
 
-static inline bool same_buffer(const void* a, const void* b) { return a && a == b; }
+// an output at the address of an input or of another output
+static inline bool same_buffer(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins) {
+    for (auto o = outs.begin(); o != outs.end(); o++) {
+        if (!*o) continue;
+        for (const void* i : ins)
+            if (*o == i) return true;
+        for (auto other = outs.begin(); other != o; other++)
+            if (*o == *other) return true;
+    }
+    return false;
+}
 
 template <class T>
 struct ClearType;

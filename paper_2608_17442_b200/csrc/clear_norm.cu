@@ -351,7 +351,7 @@ extern "C" int fesc_clear_norm(const fesc_clear_norm_desc* desc, const void* d_y
         !norm_stride(desc, d_residual, desc->residual_stride, false) || !norm_stride(desc, d_n, desc->n_stride, true) ||
         !norm_stride(desc, d_h, desc->h_stride, true))
         return clear_fail(FESC_EINVAL, "clear_norm: a row stride is negative, or rows of an output overlap");
-    if (d_n == d_y || d_n == d_gate || d_n == d_residual || d_n == d_h || same_buffer(d_h, d_y) || same_buffer(d_h, d_gate) || same_buffer(d_h, d_residual))
+    if (same_buffer({d_n, d_h}, {d_y, d_gate, d_residual, d_gamma, d_scale}))
         return clear_fail(FESC_EINVAL, "clear_norm: an output is an input or another output");
     const uint32_t bytes = clear_type_bytes(desc->type), width = desc->d / desc->groups;
     NormArgs a = {};
@@ -397,14 +397,8 @@ extern "C" int fesc_clear_norm_backward(const fesc_clear_norm_desc* desc, const 
         !norm_stride(desc, d_dh, desc->dh_stride, false) || !norm_stride(desc, d_dy, desc->dy_stride, true) ||
         !norm_stride(desc, d_dgate, desc->dgate_stride, true) || !norm_stride(desc, d_dresidual, desc->dresidual_stride, true))
         return clear_fail(FESC_EINVAL, "clear_norm_backward: a row stride is negative, or rows of an output overlap");
-    const void* outs[5] = {d_dy, d_dgate, d_dresidual, d_dgamma, d_dscale};
-    const void* ins[7] = {d_y, d_gate, d_residual, d_dn, d_dh, d_gamma, d_scale};
-    for (int i = 0; i < 5; i++) {
-        for (int j = 0; j < 7; j++)
-            if (same_buffer(outs[i], ins[j])) return clear_fail(FESC_EINVAL, "clear_norm_backward: an output is an input");
-        for (int j = 0; j < i; j++)
-            if (same_buffer(outs[i], outs[j])) return clear_fail(FESC_EINVAL, "clear_norm_backward: two outputs are the same");
-    }
+    if (same_buffer({d_dy, d_dgate, d_dresidual, d_dgamma, d_dscale}, {d_y, d_gate, d_residual, d_dn, d_dh, d_gamma, d_scale}))
+        return clear_fail(FESC_EINVAL, "clear_norm_backward: an output is an input, or two outputs are the same");
     const size_t need = fesc_clear_norm_backward_work(desc);
     if (!d_work || ((size_t)d_work & 15) || work_bytes < need) return clear_fail(FESC_EINVAL, "clear_norm_backward: the workspace is too small or not aligned to 16 bytes");
     const uint32_t bytes = clear_type_bytes(desc->type), width = desc->d / desc->groups;

@@ -6,8 +6,6 @@
 //   dg_t = <h_t, dh_t>' summed back from the segment's end:  R_t = R_{t+1} + row_t - col_t,  R behind a segment = <h, dh> there,
 // so no state has to be kept per token.  Rounding adds up over a segment only, whose ends are computed from the states themselves.
 #define FESC_DBG_FILE 20   // file id in the sites a debug build reports
-#include <initializer_list>
-
 #include "clear_scan.cuh"
 
 static thread_local std::string clear_error;
@@ -437,8 +435,7 @@ extern "C" int fesc_clear_scan(const fesc_clear_scan_desc* desc, const void* d_x
         !scan_strides(d.C, d.batch, d.L, d.G, d.N, false) || !scan_strides(d.y, d.batch, d.L, d.H, d.P, true))
         return clear_fail(FESC_EINVAL, "clear_scan: a stride is negative or beyond 2^40, or elements of y overlap");
     if (d.L && (!d_x || !d_g || !d_B || !d_C || !d_y)) return clear_fail(FESC_EINVAL, "clear_scan: x, g, B, C and y have to be given");
-    if (same_buffer(d_y, d_x) || same_buffer(d_y, d_g) || same_buffer(d_y, d_B) || same_buffer(d_y, d_C) || same_buffer(d_h_out, d_h0))
-        return clear_fail(FESC_EINVAL, "clear_scan: an output is an input");
+    if (same_buffer({d_y, d_h_out}, {d_x, d_g, d_B, d_C, d_skip, d_h0, d_lengths})) return clear_fail(FESC_EINVAL, "clear_scan: an output is an input or the other output");
     const ScanShape s = scan_shape(desc, false);
     const size_t need = fesc_clear_scan_work(desc);
     if (need && (!d_work || ((size_t)d_work & 255) || work_bytes < need))
@@ -484,14 +481,8 @@ extern "C" int fesc_clear_scan_backward(const fesc_clear_scan_desc* desc, const 
         return clear_fail(FESC_EINVAL, "clear_scan_backward: a stride is negative or beyond 2^40, or elements of an output overlap");
     if (d.L && (!d_x || !d_g || !d_B || !d_C || !d_dy || !d_dx || !d_dg || !d_dB || !d_dC))
         return clear_fail(FESC_EINVAL, "clear_scan_backward: x, g, B, C, dy, dx, dg, dB and dC have to be given");
-    const void* outs[6] = {d_dx, d_dg, d_dB, d_dC, d_dskip, d_dh0};
-    const void* ins[8] = {d_x, d_g, d_B, d_C, d_skip, d_h0, d_dy, d_dh_out};
-    for (int i = 0; i < 6; i++) {
-        for (int j = 0; j < 8; j++)
-            if (same_buffer(outs[i], ins[j])) return clear_fail(FESC_EINVAL, "clear_scan_backward: an output is an input");
-        for (int j = 0; j < i; j++)
-            if (same_buffer(outs[i], outs[j])) return clear_fail(FESC_EINVAL, "clear_scan_backward: two outputs are the same");
-    }
+    if (same_buffer({d_dx, d_dg, d_dB, d_dC, d_dskip, d_dh0}, {d_x, d_g, d_B, d_C, d_skip, d_h0, d_lengths, d_dy, d_dh_out}))
+        return clear_fail(FESC_EINVAL, "clear_scan_backward: an output is an input, or two outputs are the same");
     const ScanShape s = scan_shape(desc, true);
     const size_t need = fesc_clear_scan_backward_work(desc);
     if (!d_work || ((size_t)d_work & 255) || work_bytes < need)
@@ -559,8 +550,8 @@ extern "C" int fesc_clear_scan_step(const fesc_clear_scan_desc* desc, const void
     if (!scan_strides(d.x, d.batch, 1, d.H, d.P, false) || !scan_strides(d.g, d.batch, 1, d.H, 1, false) || !scan_strides(d.B, d.batch, 1, d.G, d.N, false) ||
         !scan_strides(d.C, d.batch, 1, d.G, d.N, false) || !scan_strides(d.y, d.batch, 1, d.H, d.P, true))
         return clear_fail(FESC_EINVAL, "clear_scan_step: a stride is negative or beyond 2^40, or elements of y overlap");
-    if (same_buffer(d_y, d_x) || same_buffer(d_y, d_g) || same_buffer(d_y, d_B) || same_buffer(d_y, d_C))
-        return clear_fail(FESC_EINVAL, "clear_scan_step: y is an input");
+    if (same_buffer({d_y, d_state_out}, {d_x, d_g, d_B, d_C, d_skip}) || d_y == d_state)
+        return clear_fail(FESC_EINVAL, "clear_scan_step: y is an input or a state, or the new state an input other than the old");
     if ((uint64_t)d.batch * d.H >= (1ull << 31)) return clear_fail(FESC_EINVAL, "clear_scan_step: too many sequences and heads for one call");
     StepArgs a = {d_x, d_B, d_C, d_g, d_skip, d_state, d_state_out, d_y, d.x[0], d.x[2], d.B[0], d.B[2], d.C[0], d.C[2], d.g[0], d.g[2], d.y[0], d.y[2],
                   d.H, d.P, d.N, d.G};
