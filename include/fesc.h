@@ -520,7 +520,7 @@ int fesc_clear_selftest_wait_limit(void* stream);
  * Gated linear recurrence (Sec. 5.4, Eqs. fesc_recurrence / fesc_contract; g = log a), per sequence and head, h in R^{P x N}:
  *   h_t = exp(g_t) h_{t-1} + x_t B_t^T,    y_t = h_t C_t + D x_t.
  *   d_x, d_y [batch][L][H][P]   d_g [batch][L][H]   d_B, d_C [batch][L][G][N], G dividing H: heads h*G/H share a group's rows
- *   d_skip   [H], D, or NULL (0)
+ *   d_skip   [H], D, or NULL (0); it multiplies the x that enters the state.  Where the state takes dt x and the skip x itself, give dt x and no skip
  *   d_h0     [batch][H][P][N], the states before the first token, or NULL (0)
  *   d_lengths int32 [batch] (DEVICE), tokens of every sequence, taken into [0, L], or NULL (L): tokens behind are neither read nor written
  *   d_h_out  [batch][H][P][N], the states behind the last token (length 0: before the first), or NULL; not d_h0

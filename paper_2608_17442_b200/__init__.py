@@ -426,7 +426,8 @@ def clear_selftest_wait_limit():
 
 def clear_scan(x, g, B, C, y, skip=None, h0=None, h_out=None, lengths=None, work=None):
     """Gated linear recurrence h_t = exp(g_t) h_{t-1} + x_t B_t^T, y_t = h_t C_t + skip x_t into y (and the last states into h_out).
-    x, y [batch, L, H, P]; g [batch, L, H] float32; B, C [batch, L, G, N]; skip [H], h0, h_out [batch, H, P, N] float32; lengths [batch] int32."""
+    x, y [batch, L, H, P]; g [batch, L, H] float32; B, C [batch, L, G, N]; skip [H], h0, h_out [batch, H, P, N] float32; lengths [batch] int32.
+    The skip multiplies the x that enters the state: where the state takes dt x and the skip x, give dt x and leave skip out."""
     (_ext or _binding()).clear_scan(x, g, B, C, y, skip, h0, h_out, lengths, work)
 
 

@@ -5,10 +5,11 @@
 // One pass: a thread holds eight channels of a row (neighbours where 16-byte accesses are possible, every 32nd otherwise), as many warps as a
 // group of channels needs form a team (3 for 768 channels, 6 for 1536), sums go through shuffles and one exchange in shared memory, and what
 // depends on them is written from the registers.  Rows are dealt out to the CTAs that are resident, and the next row's loads are under way while a
-// row is computed.  Bound by memory forwards (32768 x 768 with residual: 201 MB in 35 us, 0.89 of the copy rate); the gate's backward pass issues some 40
-// instructions per channel and is bound by that and by one exchange per row (16384 x 1536: 252 MB in 61 us).
-// The gradients of gamma and s are sums over rows: a CTA adds up its own rows in a fixed order, a second kernel adds up the CTAs, so the
-// results do not depend on the order in which CTAs run.
+// row is computed.  Bound by memory forwards (32768 x 768 with residual: 201 MB in 35 us, 0.89 of the copy rate).  The gate's backward pass (16384 x 1536:
+// 252 MB in 61 us) fills neither memory (44 %) nor issue (64 %): 22 warps an SM wait for exponentials, reciprocals and shuffles, for one
+// another at the row's exchange, and for the instruction before.
+// The gradients of gamma and s are sums over rows: a thread adds up its own rows in float32, a CTA its teams, in a fixed order, a second kernel the CTAs in
+// float64, so the results do not depend on the order in which CTAs run.
 #define FESC_DBG_FILE 16   // file id in the sites a debug build reports
 #include "clear.cuh"
 
@@ -321,7 +322,8 @@ static void (*norm_kernel(bool gate, bool residual))(NormArgs) {
     return gate ? residual ? k_clear_norm<T, true, true, THREADS> : k_clear_norm<T, true, false, THREADS>
                 : residual ? k_clear_norm<T, false, true, THREADS> : k_clear_norm<T, false, false, THREADS>;
 }
-// CTAs of more than 256 threads (rows of more than 2048 channels) have 64 registers a thread and keep some of a row's words in local memory
+// Some of a row's words go to local memory: in CTAs of more than 256 threads (rows of more than 2048 channels, 64 registers a thread), in 16-bit rows with a
+// gate (40 bytes at 80 registers) and in float32 rows with gate and residual (96 bytes at 128).
 template <class T, int THREADS>
 static void (*norm_backward_kernel(bool gate, bool residual))(NormArgs) {
     return gate ? residual ? k_clear_norm_backward<T, true, true, THREADS> : k_clear_norm_backward<T, true, false, THREADS>

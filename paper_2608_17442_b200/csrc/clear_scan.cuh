@@ -10,7 +10,7 @@
 // multiplies q without going through memory.
 // A long sequence is cut into segments when there are too few heads to fill the SMs: the sweep in MODE_STATE gives what every segment adds to
 // its state, k_clear_combine chains the segments, and every segment then runs with the state before it.
-// Measured (24 heads, 128 columns, 2048 tokens): float16 93 us, float32 113; 8 x 1024 tokens of 12 heads in float32 210.  A chunk is loads, scores,
+// Measured (24 heads, 128 columns, 2048 tokens): float16 95 us, float32 113; 8 x 1024 tokens of 12 heads in float32 192.  A chunk is loads, scores,
 // products, outputs one after the other, with three to six matrix instructions per product of float32 planes; what bounds it are those chains.
 //
 // Operands are sums of bfloat16 numbers ("planes"): bfloat16 inputs one, float16 two (exact), float32 three (24 bits).  What the kernel
@@ -56,7 +56,7 @@ struct ScanArgs {
     float* dots;                     // MODE_GRAD: [b][head tile][L], u . out
     const float* meet;               // MODE_GRAD forwards: states of the sweep backwards, as `init`; their product with this one's at the segments' ends
     float* ends;                     //   [b][segment][head tile]; backwards: of h0 (meet) with the gradient before the first token, segment 0
-    float* diag;                     //   sum over a segment's tokens of q . k, [b][segment][head tile]
+    float* diag;                     //   sum over a segment's tokens of q . k, [b][segment][head tile]; segments are added up in 64 bits
     uint32_t b, L, H, P, G, N, tiles, segments, seg_chunks, backwards;
 };
 
@@ -105,9 +105,6 @@ __device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr) {
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
@@ -208,7 +205,7 @@ struct ScanShared {
     static constexpr int K_STR = DK + SCAN_PAD, V_STR = DV + SCAN_PAD, S_STR = SCAN_Q + SCAN_PAD;
     static constexpr int k = 0, v = k + NI * SCAN_Q * K_STR, q = v + NI * SCAN_Q * V_STR, s = q + (MODE ? NI * SCAN_Q * K_STR : 0);
     static constexpr int words = s + (MODE ? NO * SCAN_Q * S_STR : 0);                        // in bfloat16 numbers
-    static constexpr int O_STR = DV + 4;                                                       // floats; the outputs' rows lie over v .. s
+    static constexpr int O_STR = DV + 4;                                                       // floats; the outputs' rows lie over q and the scores
     static_assert(!MODE || (words - q) * 2 >= SCAN_Q * O_STR * 4, "outputs fit over q and the scores");
     static constexpr int H_STR = (MODE == MODE_GRAD ? DV : DK) + 4;                           // floats; states pass through all of it, 64 rows
     static constexpr size_t bytes = std::max((size_t)words * 2, (size_t)SCAN_TILE * H_STR * 4);
@@ -661,8 +658,9 @@ cudaError_t scan_launch(const ScanSet& s, int mode, cudaStream_t st) {
 extern template cudaError_t scan_launch<__nv_bfloat16>(const ScanSet&, int, cudaStream_t);
 extern template cudaError_t scan_launch<__half>(const ScanSet&, int, cudaStream_t);
 extern template cudaError_t scan_launch<float>(const ScanSet&, int, cudaStream_t);
-// The same on tcgen05: bfloat16, operands with 16-byte rows (clear_scan_tc.cu; others are copied into such rows first; states of 8 columns take as long as
-// states of 64 there, and still less than on mma.sync).
+// The same on tcgen05: bfloat16, operands with 16-byte rows (clear_scan_tc.cu; states of 8 columns take as long as states of 64 there, and still less than
+// on mma.sync).  Operands whose strides or widths are not of 16 bytes are copied into such rows first.  Those whose strides are but whose address is not
+// (the workspace is sized without addresses) take mma.sync, element by element: 2048 tokens of 24 heads 221 us, where 28 are possible.
 // part is [b][head tile][segment][chunk of 128][16384] in an order of its own there, and dots is left to the kernel that sums it up over heads.
 cudaError_t scan_tc_launch(const ScanSet& s, int mode, cudaStream_t st);
 struct TcSums {

@@ -57,6 +57,7 @@ struct alignas(16) TcDecays {      // read four words at a time
     float keep;              // over the chunk
 };
 
+// off by two units at most, and the rounding of x: what a 16-bit output or a sum over a chunk takes once; the chunk's decay goes by exp2_near
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -104,16 +105,6 @@ __device__ __forceinline__ void tc_ld16(uint32_t (&r)[16], uint32_t addr) {
                    "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(addr)
                  : "memory");
-}
-__device__ __forceinline__ void tc_ld32(uint32_t (&r)[32], uint32_t addr) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, "
-        "%24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
-          "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]),
-          "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(addr)
-        : "memory");
 }
 __device__ __forceinline__ void tc_st8(uint32_t addr, const uint32_t (&r)[8]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]),
@@ -767,7 +758,7 @@ cudaError_t scan_tc_launch(const ScanSet& s, int mode, cudaStream_t st) {
 }
 
 // Copies operands whose rows do not allow 16-byte accesses into rows that do, with zeros behind their columns: at the price of one pass over them the
-// sweeps run on tcgen05 (2048 tokens of 24 heads and 127 columns 98 -> 37 us).  A warp takes a token, blockIdx.z an operand.
+// sweeps run on tcgen05 (2048 tokens of 24 heads and 127 columns 98 -> 40 us).  A warp takes a token, blockIdx.z an operand.
 __global__ void __launch_bounds__(256) k_clear_scan_pack(const TcPack a) {
     pdl_begin();
     const auto& o = a.o[blockIdx.z];
