@@ -525,9 +525,9 @@ int fesc_clear_selftest_wait_limit(void* stream);
  *   d_lengths int32 [batch] (DEVICE), tokens of every sequence, taken into [0, L], or NULL (L): tokens behind are neither read nor written
  *   d_h_out  [batch][H][P][N], the states behind the last token (length 0: before the first), or NULL; not d_h0
  * Log decays are not positive; -inf (any below -300) drops the state.  N <= 128, P <= 4096, L < 2^30, batch <= 65535.
- * A decay that is zero in float32, of a token or over the tokens between, leaves nothing of a state or of its gradient, also where these are
- * infinite or NaN.  Tokens are multiplied with zeros in chunks of up to 128: an infinity or NaN in a token reaches the other tokens of its chunk, and the state
- * behind it.  An infinite state may give NaN.
+ * A token's decay that is zero in float32 leaves nothing of the state before it, nor of the gradient behind it, also where these are infinite or NaN.
+ * Tokens are multiplied with zeros in chunks of up to 128: an infinity or NaN in a token reaches the other tokens of its chunk, and the state behind it.  An
+ * infinite state may give NaN.
  * Workspace: fesc_clear_scan_work(desc) bytes, aligned to 256 (0: none needed).
  */
 typedef struct fesc_clear_scan_desc {
